@@ -339,6 +339,39 @@ int fusco_segments_copy(const void *d_src, uint64_t src_bytes, const fusco_segme
                         uint64_t stream_capacity, uint64_t slice_bytes, uint32_t *d_slice_fill, int32_t *d_status,
                         void *stream);
 
+/*
+ * Products of the experts, on the rows that fusco_dispatch wrote and a layout's plan describes: expert e has the rows
+ * [exp_off[e], exp_off[e+1]) and weights of its own.  All tensors are bf16 and contiguous; sums are held in fp32 and rounded
+ * once (nearest even).  Rows that no expert owns (a plan of invalid ids) are neither read nor written.  Every row size must
+ * be a multiple of 16 bytes and at most FUSCO_MAX_ROW_BYTES, one expert's weights must lie below 2032 MiB.
+ *
+ * fusco_experts_gated: h[r, i] = silu(g) * u with g = sum_c x[r, c] w[e, i, c] and u = sum_c x[r, c] w[e, I + i, c],
+ * silu(g) = g / (1 + exp(-g)).  d_x [P, H], d_w [E, 2 I, H], d_h [P, I].  d_pre, if not NULL, receives g and u,
+ * [P, 2 I] with g first: what the gradient needs.
+ *
+ * fusco_experts_linear: y[r, m] = sum_c x[r, c] w[e, m, c].  d_x [P, C], d_w [E, M, C], d_y [P, M].
+ */
+int fusco_experts_gated(const fusco_layout *L, const void *d_x, const void *d_w, void *d_h, void *d_pre, int32_t H, int32_t I,
+                        void *stream);
+int fusco_experts_linear(const fusco_layout *L, const void *d_x, const void *d_w, void *d_y, int32_t C, int32_t M,
+                         void *stream);
+
+/*
+ * Gradients of these products (tensors, sizes and rounding as there).
+ *
+ * fusco_experts_input_grad: dx[r, c] = sum_m dy[r, m] w[e, m, c].  d_dy [P, M], d_w [E, M, C], d_dx [P, C].
+ * With d_pre not NULL (the [P, 2 C] tensor of fusco_experts_gated with I = C, whose h was this product's input) the gradient
+ * of the activation is taken as well, in fp32 before the only rounding, and d_dx is the gradient of pre, [P, 2 C]:
+ *     dg = dh u sig(g) (1 + g (1 - sig(g))),   du = dh g sig(g),   sig(g) = 1 / (1 + exp(-g)).
+ *
+ * fusco_experts_weight_grad: dw[e, m, c] = sum over the expert's rows of dy[r, m] x[r, c]; zeros for an expert without rows.
+ * d_dy [P, M], d_x [P, C], d_dw [E, M, C] of dw_dtype (FUSCO_BF16 or FUSCO_F32).
+ */
+int fusco_experts_input_grad(const fusco_layout *L, const void *d_dy, const void *d_w, void *d_dx, const void *d_pre,
+                             int32_t M, int32_t C, void *stream);
+int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const void *d_x, void *d_dw, int dw_dtype, int32_t M,
+                              int32_t C, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

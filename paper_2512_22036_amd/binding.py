@@ -24,7 +24,8 @@ _LIB_PATH = os.path.join(_HERE, "libfusco.so")
 EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_scratch_bytes",
            "fusco_layout_bind", "fusco_plan", "fusco_plan_static", "fusco_dispatch", "fusco_dispatch_in_transfer_order", "fusco_combine", "fusco_plan_dispatch", "fusco_probe_copy", "fusco_probe_rows", "fusco_probe_pieces", "fusco_probe_consume_slices", "fusco_probe_time_next_call", "fusco_probe_source_chunk_bytes", "fusco_probe_dispatch_kernel", "fusco_probe_dispatch_occupancy", "fusco_probe_dispatch_pull", "fusco_probe_dispatch_walk", "fusco_probe_dispatch_route", "fusco_probe_plan_through", "fusco_probe_plan_dispatch_through", "fusco_probe_segments_wide",
            "fusco_combine_two_hop", "fusco_balance_groups", "fusco_cross_node_load", "fusco_segments_scan", "fusco_segments_copy",
-           "fusco_disaggregated_plan", "fusco_disaggregated_dispatch", "fusco_disaggregated_combine")
+           "fusco_disaggregated_plan", "fusco_disaggregated_dispatch", "fusco_disaggregated_combine",
+           "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad")
 
 
 class FuscoError(RuntimeError):
@@ -131,6 +132,14 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_disaggregated_dispatch.argtypes = [lp, lp, vp, sz, vp, vp, vp, vp]
     lib.fusco_disaggregated_combine.restype = ctypes.c_int
     lib.fusco_disaggregated_combine.argtypes = [lp, lp, vp, ctypes.c_int, vp, vp, vp, vp, ctypes.c_int, i32, vp]
+    lib.fusco_experts_gated.restype = ctypes.c_int
+    lib.fusco_experts_gated.argtypes = [lp, vp, vp, vp, vp, i32, i32, vp]
+    lib.fusco_experts_linear.restype = ctypes.c_int
+    lib.fusco_experts_linear.argtypes = [lp, vp, vp, vp, i32, i32, vp]
+    lib.fusco_experts_input_grad.restype = ctypes.c_int
+    lib.fusco_experts_input_grad.argtypes = [lp, vp, vp, vp, vp, i32, i32, vp]
+    lib.fusco_experts_weight_grad.restype = ctypes.c_int
+    lib.fusco_experts_weight_grad.argtypes = [lp, vp, vp, vp, ctypes.c_int, i32, i32, vp]
     _lib = lib
     _fast = _bind_fastcall(lib)
     return lib
@@ -338,6 +347,69 @@ def fusco_combine(layout: Layout, y: torch.Tensor, w: torch.Tensor, out: torch.T
     _check(load_library().fusco_combine(ctypes.byref(layout.c), y.data_ptr(), _dtype_code(y, "y"), w.data_ptr(),
                                         out.data_ptr(), _dtype_code(out, "out"), H, 0, _stream(stream)),
            "fusco_combine")
+
+
+def _bf16(t: torch.Tensor, name: str, shape) -> torch.Tensor:
+    if not t.is_cuda or t.dtype != torch.bfloat16 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise FuscoError("%s must be a contiguous bfloat16 device tensor of shape %s" % (name, list(shape)))
+    return t
+
+
+def _weights(layout: Layout, w: torch.Tensor, name: str):
+    if w.dim() != 3 or w.shape[0] != layout.E:
+        raise FuscoError("%s must have three dimensions, the first of them the %d experts" % (name, layout.E))
+    return _bf16(w, name, w.shape)
+
+
+def fusco_experts_gated(layout: Layout, x: torch.Tensor, w: torch.Tensor, h: torch.Tensor, pre: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    """h = silu(x Wg^T) * (x Wu^T), expert by expert: x [P, H] as fusco_dispatch wrote it, w [E, 2 I, H] with the gate rows
+    first, h [P, I], all bfloat16.  pre [P, 2 I]: also keep both factors before the activation, for the gradient."""
+    _weights(layout, w, "w")
+    I, H = w.shape[1] // 2, w.shape[2]
+    if w.shape[1] % 2:
+        raise FuscoError("w must have an even number of rows per expert")
+    _bf16(x, "x", (layout.P, H))
+    _bf16(h, "h", (layout.P, I))
+    if pre is not None:
+        _bf16(pre, "pre", (layout.P, 2 * I))
+    _check(load_library().fusco_experts_gated(ctypes.byref(layout.c), x.data_ptr(), w.data_ptr(), h.data_ptr(), _ptr(pre), H, I,
+                                              _stream(stream)), "fusco_experts_gated")
+
+
+def fusco_experts_linear(layout: Layout, x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, stream=None) -> None:
+    """y = x W^T, expert by expert: x [P, C], w [E, M, C], y [P, M], all bfloat16."""
+    _weights(layout, w, "w")
+    M, C = w.shape[1], w.shape[2]
+    _bf16(x, "x", (layout.P, C))
+    _bf16(y, "y", (layout.P, M))
+    _check(load_library().fusco_experts_linear(ctypes.byref(layout.c), x.data_ptr(), w.data_ptr(), y.data_ptr(), C, M,
+                                               _stream(stream)), "fusco_experts_linear")
+
+
+def fusco_experts_input_grad(layout: Layout, dy: torch.Tensor, w: torch.Tensor, dx: torch.Tensor,
+                             pre: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx = dy W, expert by expert: dy [P, M], w [E, M, C], dx [P, C], all bfloat16.  With pre [P, 2 C] (from
+    fusco_experts_gated) dx is the gradient of pre, [P, 2 C]."""
+    _weights(layout, w, "w")
+    M, C = w.shape[1], w.shape[2]
+    _bf16(dy, "dy", (layout.P, M))
+    _bf16(dx, "dx", (layout.P, C if pre is None else 2 * C))
+    if pre is not None:
+        _bf16(pre, "pre", (layout.P, 2 * C))
+    _check(load_library().fusco_experts_input_grad(ctypes.byref(layout.c), dy.data_ptr(), w.data_ptr(), dx.data_ptr(), _ptr(pre),
+                                                   M, C, _stream(stream)), "fusco_experts_input_grad")
+
+
+def fusco_experts_weight_grad(layout: Layout, dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, stream=None) -> None:
+    """dw = dy^T x, expert by expert: dy [P, M], x [P, C] bfloat16, dw [E, M, C] bfloat16 or float32."""
+    if not dw.is_cuda or dw.dim() != 3 or dw.shape[0] != layout.E or not dw.is_contiguous():
+        raise FuscoError("dw must be a contiguous device tensor of three dimensions, the first of them the %d experts" % layout.E)
+    M, C = dw.shape[1], dw.shape[2]
+    _bf16(dy, "dy", (layout.P, M))
+    _bf16(x, "x", (layout.P, C))
+    _check(load_library().fusco_experts_weight_grad(ctypes.byref(layout.c), dy.data_ptr(), x.data_ptr(), dw.data_ptr(),
+                                                    _dtype_code(dw, "dw"), M, C, _stream(stream)), "fusco_experts_weight_grad")
 
 
 def fusco_combine_two_hop(layout: Layout, y: torch.Tensor, w: torch.Tensor, partial: torch.Tensor,

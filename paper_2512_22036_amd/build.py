@@ -7,7 +7,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "fusco.hip")
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("fusco.hip", "block.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfusco.so")
 
@@ -23,7 +23,7 @@ def build_library(verbose: bool = False) -> str:
            # packed fp32 instructions are kept out of the generated code
            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
            "-Wno-unused-command-line-argument",
-           "-I", INCLUDE, "-o", tmp, SRC, "-Wl,-rpath,/opt/rocm/lib"]
+           "-parallel-jobs=%d" % len(SOURCES), "-I", INCLUDE, "-o", tmp, *SOURCES, "-Wl,-rpath,/opt/rocm/lib"]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -1,4 +1,4 @@
-// Types, limits and small host helpers shared by every part of the library (one translation unit).
+// Types, limits and small host helpers shared by every part of the library (both translation units).
 #ifndef FUSCO_CSRC_COMMON_H
 #define FUSCO_CSRC_COMMON_H
 
@@ -31,7 +31,7 @@ static_assert(kMaxBins <= kPlanThreads, "the planner gives every bin a thread");
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-bool sizes_ok(int32_t N, int32_t k, int32_t E, int32_t D)
+inline bool sizes_ok(int32_t N, int32_t k, int32_t E, int32_t D)
 {
     if (N < 0 || k < 1 || k > FUSCO_MAX_K || E < 1 || E > FUSCO_MAX_E || D < 1 || D > E) return false;
     if (E % D != 0) return false;
@@ -83,6 +83,24 @@ inline int num_chunks(int n_tiles)
 {
     const int c = chunk_tiles_for(n_tiles);
     return c ? (n_tiles + c - 1) / c : 0;
+}
+
+inline bool layout_ok(const fusco_layout *L)
+{
+    if (!L || !sizes_ok(L->N, L->k, L->E, L->D)) return false;
+    if ((int64_t)L->P != (int64_t)L->N * L->k) return false;
+    const int rounds = plan_rounds(L->N, L->k);
+    if (L->tile_tokens != tokens_per_tile(L->k, rounds) || L->tile_count != num_tiles(L->N, L->k, rounds)) return false;
+    return L->exp_count && L->exp_off && L->send_count && L->send_off && L->pair_slot && L->slot_pair &&
+           L->slot_token && L->send_src && L->pair_send_row && L->slot_send_row && L->pair_first && L->status &&
+           L->tile_slots;
+}
+
+inline bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+inline int launch_status()
+{
+    return hipGetLastError() == hipSuccess ? FUSCO_OK : FUSCO_ERR_HIP;
 }
 
 }   // namespace

@@ -8,8 +8,9 @@
 // are built around 16-byte coalesced global accesses, the planner around LDS counters and
 // wave64 ballots.
 //
-// One translation unit: the kernels live in the headers next to this file (planner.h, movers.h,
-// segments.h, probes.h), the host-side helpers in launch.h, the C entry points below.
+// The kernels live in the headers next to this file (planner.h, movers.h, segments.h, probes.h), the
+// host-side helpers in launch.h, the C entry points below.  The operators around the shuffle (routing,
+// norms, the experts' products, the combine's gradient) are a translation unit of their own, block.hip.
 #include "launch.h"
 #include <atomic>
 #include <mutex>
@@ -89,17 +90,6 @@ int fusco_layout_bind(fusco_layout *L, int32_t N, int32_t k, int32_t E, int32_t 
     if (bytes < layout_carve(nullptr, N, k, E, D, nullptr)) return FUSCO_ERR_WORKSPACE;
     layout_carve(L, N, k, E, D, (char *)d_mem);
     return FUSCO_OK;
-}
-
-static bool layout_ok(const fusco_layout *L)
-{
-    if (!L || !sizes_ok(L->N, L->k, L->E, L->D)) return false;
-    if ((int64_t)L->P != (int64_t)L->N * L->k) return false;
-    const int rounds = plan_rounds(L->N, L->k);
-    if (L->tile_tokens != tokens_per_tile(L->k, rounds) || L->tile_count != num_tiles(L->N, L->k, rounds)) return false;
-    return L->exp_count && L->exp_off && L->send_count && L->send_off && L->pair_slot && L->slot_pair &&
-           L->slot_token && L->send_src && L->pair_send_row && L->slot_send_row && L->pair_first && L->status &&
-           L->tile_slots;
 }
 
 static PlanArgs plan_args(const fusco_layout *L, const int32_t *d_topk_idx, void *d_scratch, int rounds)

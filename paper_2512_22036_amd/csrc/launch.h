@@ -10,8 +10,6 @@
 
 namespace {
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
 // odd multiplier close to frac * n that shares no factor with n: i -> i * mul mod n is a bijection of
 // [0, n) that sends neighbours far apart
 uint32_t coprime_near(uint32_t n, double frac)
@@ -26,11 +24,6 @@ uint32_t coprime_near(uint32_t n, double frac)
 }
 
 int round_up(int v, int m) { return (v + m - 1) / m * m; }
-
-int launch_status()
-{
-    return hipGetLastError() == hipSuccess ? FUSCO_OK : FUSCO_ERR_HIP;
-}
 
 // Events armed by fusco_probe_time_next_call for the calling thread (null when not armed), and their
 // hand-over to the call that consumes them.

@@ -1,0 +1,416 @@
+// Products of the experts' rows with the experts' weights on the matrix cores.
+//
+// One kernel computes, expert by expert, D[a, b] = sum over c of A(a, c) * B(b, c) and stores it with a contiguous:
+//   forward          a = weight row, b = token row,  c = column of both      (both operands are contiguous along c)
+//   input gradient   a = weight column, b = token row, c = weight row        (A is contiguous along a)
+//   weight gradient  a = weight column, b = weight row, c = token row        (both are contiguous along a and b)
+// Rows lie expert-major (layout's exp_off); an expert's segment is cut into tiles of BB rows.
+#ifndef FUSCO_CSRC_PRODUCTS_H
+#define FUSCO_CSRC_PRODUCTS_H
+
+#include "common.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char lds_byte;
+typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
+
+constexpr int kCus = 256;              // compute units of an MI355X
+constexpr int kTileC = 64;             // elements of the summed dimension per stage
+constexpr int kTileThreads = 512;
+constexpr int kTileA = 256;
+constexpr uint32_t kNowhere = 0x7f000000u;   // byte offset past every buffer: such a load gives zeros
+
+// How the tiles of one product lie in memory
+enum { kAlongC, kAcross };             // operand contiguous along the summed dimension, or across it
+enum { kStoreBf16, kStoreF32, kStoreGated, kStoreGatedGrad };
+
+struct ProductArgs {
+    const int32_t *exp_off;            // [E + 1]
+    const char *rows;                  // B operand of forward and input gradient, [P, C]; A operand of the weight gradient, [P, NA]
+    const char *other;                 // weights [E, ...]; B operand of the weight gradient, [P, NB]
+    char *out;                         // [P, NA], or [E, NB, NA]
+    char *pre;                         // gated forms: pre-activations [P, 2 * units] (written by forward where not null, read by the gradient)
+    int32_t E, NA, NB, C;              // NA: outputs along a (gated forward: units); NB, C: weight gradient has NB outputs along b, others sum over C
+};
+
+__device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+
+// The bounds-checked view of `bytes` bytes from p: loads outside give zeros
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t view(const char *p, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(bytes < 0 ? 0 : bytes), 0x00020000);
+}
+
+// 16 bytes per lane straight to LDS: the wave's 64 chunks lie behind one another from `to` on
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *__restrict__ to, uint32_t offset, int uniform)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 16, (int)offset, uniform, 0, 0);
+}
+
+// One operand of a tile: where a stage of it comes from and how it lies in LDS.
+//   kAlongC: LDS rows of 64 elements (128 bytes), the 16-byte chunk q of row r at place q ^ (r & 7): eight lanes that read the same chunk of
+//            eight rows hit all banks.
+//   kAcross: LDS rows of W elements, one per c; pairs of chunks (16 elements) of row c at place pair ^ f(c), f(c) = (c & 3) + 4 * bit 3 of c:
+//            the transposing read takes 32 bytes of each of the rows c .. c + 3 and c + 8 .. c + 11 at once.
+template <int MODE, int W>
+struct Operand {
+    static constexpr int kLoads = W * kTileC * 2 / 16 / kTileThreads;   // loads per thread and stage
+    static constexpr int kBytes = W * kTileC * 2;
+    const char *base;
+    int64_t ld;            // bytes from row to row
+    int64_t limit;         // kAlongC: readable bytes from base; kAcross: bytes that are missing from a whole last row
+    int32_t c_size;        // elements (kAlongC) or rows (kAcross) of the summed dimension
+    uint32_t at[kLoads];   // this thread's byte offsets
+
+    __device__ __forceinline__ void stage(int step, char *__restrict__ lds, int wave, int lane) const
+    {
+        if (MODE == kAlongC) {
+            const __amdgpu_buffer_rsrc_t v = view(base, limit);
+            const int chunk = (lane & 7) ^ (lane >> 3);
+            const bool in = step * kTileC + chunk * 8 < c_size;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                to_lds(v, lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, step * kTileC * 2);
+        } else {
+            int left = c_size - step * kTileC;
+            left = left > kTileC ? kTileC : left;
+            const __amdgpu_buffer_rsrc_t v = view(base + (int64_t)step * kTileC * ld, left > 0 ? left * ld - limit : 0);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                to_lds(v, lds + (i * kTileThreads + wave * kWave) * 16, at[i], 0);
+        }
+    }
+
+    // byte offset of this lane's part of fragment 0, first half of a stage
+    static __device__ __forceinline__ uint32_t lane_at(int lane)
+    {
+        if (MODE == kAlongC) return (lane & 15) * (kTileC * 2) + (((lane >> 4) ^ (lane & 7)) << 4);
+        const int g = lane >> 4, i = lane & 15;
+        return (g * 8 + (i >> 2)) * (W * 2) + ((i & 3) >> 1) * 16 + (i & 1) * 8;
+    }
+
+    // fragment f (16 outputs) of half `ks` (32 elements of the summed dimension): element j of lane l is (f * 16 + l % 16, ks * 32 + l / 16 * 8 + j)
+    static __device__ __forceinline__ bf16x8 fragment(const char *__restrict__ lds, uint32_t lane_off, int lane, int f, int ks)
+    {
+        if (MODE == kAlongC) return *(const bf16x8 *)(lds + (lane_off ^ (ks * 64)) + f * 16 * kTileC * 2);
+        const int swz = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
+        const char *p = lds + lane_off + ((f ^ swz) << 5) + ks * 32 * W * 2;
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 4 * W * 2));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+// Everything a wave keeps over a tile
+template <int AMODE, int BMODE, int BB, int FA, int FB>
+struct TileState {
+    Operand<AMODE, kTileA> a;
+    Operand<BMODE, BB> b;
+    uint32_t a_lane, b_lane;
+    int a_frag, b_frag, wave, lane;
+};
+
+// First part of a stage: all fragments but the last group's are multiplied, the rest of the next stage is asked for, and the last
+// group's fragments are read.  Ends with the barrier after which the stage's LDS is free and the next stage's is whole.
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
+__device__ __forceinline__ void stage_first(const TileState<AMODE, BMODE, BB, FA, FB> &s, const char *__restrict__ cur, char *__restrict__ nxt, int step,
+                                            bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+{
+    constexpr int kHalves = FA / 4, kGroups = 2 * kHalves, kABytes = Operand<AMODE, kTileA>::kBytes;
+    s.b.stage(step + 1, nxt + kABytes, s.wave, s.lane);
+    __builtin_amdgcn_sched_barrier(0);
+    if (ACTIVE) {
+#pragma unroll
+        for (int g = 0; g < kGroups - 1; ++g) {
+            const int ks = g / kHalves, ks1 = (g + 1) / kHalves, h = g % kHalves, h1 = (g + 1) % kHalves;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (ks1 != ks && i < FB) b[ks1][i] = s.b.fragment(cur + kABytes, s.b_lane, s.lane, s.b_frag + i, ks1);
+                a[(g + 1) & 1][i] = s.a.fragment(cur, s.a_lane, s.lane, s.a_frag + h1 * 4 + i, ks1);
+#pragma unroll
+                for (int j = 0; j < FB; ++j)
+                    acc[h * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g & 1][i], b[ks][j], acc[h * 4 + i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): the next stage has arrived, nothing of this one is still being read
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Last part: the last group is multiplied while the next stage's first fragments are read and the stage after it is asked for
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
+__device__ __forceinline__ void stage_last(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ cur, const char *__restrict__ nxt, int step,
+                                           bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+{
+    constexpr int kHalves = FA / 4, kABytes = Operand<AMODE, kTileA>::kBytes;
+    s.a.stage(step + 2, cur, s.wave, s.lane);
+    __builtin_amdgcn_sched_barrier(0);
+    if (ACTIVE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i < FB) b[0][i] = s.b.fragment(nxt + kABytes, s.b_lane, s.lane, s.b_frag + i, 0);
+            a[0][i] = s.a.fragment(nxt, s.a_lane, s.lane, s.a_frag + i, 0);
+#pragma unroll
+            for (int j = 0; j < FB; ++j)
+                acc[(kHalves - 1) * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][i], b[1][j], acc[(kHalves - 1) * 4 + i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
+__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ lds0, char *__restrict__ lds1, int steps, f32x4 (&acc)[FA][FB])
+{
+    constexpr int kABytes = Operand<AMODE, kTileA>::kBytes;
+    s.a.stage(0, lds0, s.wave, s.lane);
+    s.b.stage(0, lds0 + kABytes, s.wave, s.lane);
+    s.a.stage(1, lds1, s.wave, s.lane);
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    bf16x8 a[2][4], b[2][FB];
+    if (ACTIVE) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[0][i] = s.a.fragment(lds0, s.a_lane, s.lane, s.a_frag + i, 0);
+#pragma unroll
+        for (int j = 0; j < FB; ++j) b[0][j] = s.b.fragment(lds0 + kABytes, s.b_lane, s.lane, s.b_frag + j, 0);
+    }
+    for (int step = 0;;) {
+        stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
+        stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
+        if (++step >= steps) break;
+        stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
+        stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
+        if (++step >= steps) break;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // nothing may still be on its way to LDS when the next tile begins
+    __builtin_amdgcn_s_barrier();
+}
+
+__device__ __forceinline__ void store4(char *out, int64_t element, f32x4 v)
+{
+    bf16x4 o;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
+    *(bf16x4 *)(out + element * 2) = o;
+}
+
+// Exclusive prefix sums of the experts' tile counts, [E + 1] ints in LDS
+__device__ __forceinline__ void tile_prefix(const int32_t *__restrict__ exp_off, int E, int BB, int *__restrict__ prefix, int *__restrict__ part)
+{
+    static_assert(FUSCO_MAX_E <= 2 * kTileThreads, "two experts per thread");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = 2 * tid;
+    const int o0 = exp_off[e < E ? e : E], o1 = exp_off[e + 1 < E ? e + 1 : E], o2 = exp_off[e + 2 < E ? e + 2 : E];
+    const int n0 = (o1 - o0 + BB - 1) / BB, n1 = (o2 - o1 + BB - 1) / BB;
+    int sum = n0 + n1;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+    }
+    if (lane == 63) part[wave] = sum;
+    __syncthreads();
+    int before = sum - n0 - n1;
+    for (int w = 0; w < wave; ++w) before += part[w];
+    if (e <= E) prefix[e] = before;
+    if (e + 1 <= E) prefix[e + 1] = before + n0;
+    if (E == 2 * kTileThreads && tid == kTileThreads - 1) prefix[E] = before + n0 + n1;
+    __syncthreads();
+}
+
+// Tiles of BB token rows of one expert are taken in groups of four with all tiles along a: 32 neighbours (what one XCD's compute units
+// work on at a time) then share 4 tiles of rows and 8 tiles of weights in their L2.
+constexpr int kGroupB = 4;
+
+// Workgroup g of `groups` takes tiles of the list in runs of 32 per XCD: workgroups are dealt to the XCDs in turn.
+__device__ __forceinline__ int tile_in_list(int i)
+{
+    const int per_xcd = kCus / kXcds, g = blockIdx.x;
+    const int round = g / kCus, in = g % kCus;
+    return ((i * (int)(gridDim.x / kCus) + round) * kXcds + in % kXcds) * per_xcd + in / kXcds;
+}
+
+// FA x FB fragments of 16 x 16 outputs per wave, kTileA / (16 * FA) waves along a
+template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
+__global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
+{
+    constexpr int kStage = Operand<AMODE, kTileA>::kBytes + Operand<BMODE, BB>::kBytes;
+    constexpr int kWavesA = kTileA / (16 * FA), kWavesB = BB / (16 * FB);
+    constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
+    constexpr bool kGated = STORE == kStoreGated;
+    constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
+    static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
+    static_assert(FA % 4 == 0 && FB <= 4, "groups of four fragments along a");
+    __shared__ __align__(1024) char lds[2 * kStage];
+    __shared__ int prefix[FUSCO_MAX_E + 1];
+    __shared__ int part[kTileThreads / kWave];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wa = wave % kWavesA, wb = wave / kWavesA;
+    const int tiles_a = (p.NA + kUnitsA - 1) / kUnitsA;
+    const int tiles_b = kByRows ? 0 : (p.NB + BB - 1) / BB;
+    int total;
+    if (kByRows) {
+        tile_prefix(p.exp_off, p.E, BB, prefix, part);
+        total = prefix[p.E] * tiles_a;
+    } else {
+        total = p.E * tiles_a * tiles_b;
+    }
+
+    TileState<AMODE, BMODE, BB, FA, FB> s;
+    s.wave = wave;
+    s.lane = lane;
+    s.a_lane = Operand<AMODE, kTileA>::lane_at(lane);
+    s.b_lane = Operand<BMODE, BB>::lane_at(lane);
+    s.a_frag = wa * FA;
+    s.b_frag = wb * FB;
+
+    for (int i = 0;; ++i) {
+        const int t = tile_in_list(i);
+        if (t >= total) break;   // later tiles of this workgroup lie behind it
+        // which expert, which tiles
+        int e, ta, tb, first, rows;
+        {
+            int at, in_e;
+            if (kByRows) {
+                int lo = 0, hi = p.E;   // the last expert whose first tile is not behind t
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (prefix[mid] * tiles_a <= t) lo = mid;
+                    else hi = mid;
+                }
+                e = __builtin_amdgcn_readfirstlane(lo);
+                at = t - __builtin_amdgcn_readfirstlane(prefix[e]) * tiles_a;
+                in_e = __builtin_amdgcn_readfirstlane(prefix[e + 1] - prefix[e]);
+            } else {
+                e = t / (tiles_a * tiles_b);
+                at = t - e * tiles_a * tiles_b;
+                in_e = tiles_b;
+            }
+            const int g = at / (kGroupB * tiles_a), wide = in_e - g * kGroupB < kGroupB ? in_e - g * kGroupB : kGroupB;
+            at -= g * kGroupB * tiles_a;
+            ta = at / wide;
+            tb = g * kGroupB + at % wide;
+            first = __builtin_amdgcn_readfirstlane(p.exp_off[e]);
+            rows = __builtin_amdgcn_readfirstlane(p.exp_off[e + 1]) - first;
+        }
+        const int a0 = ta * kUnitsA, b0 = tb * BB;
+        const int b_left = (kByRows ? rows : p.NB) - b0, a_left = p.NA - a0;
+        int steps;
+        // operand A
+        if (AMODE == kAlongC) {   // forward: weight rows
+            const int rows_e = kGated ? 2 * p.NA : p.NA;
+            s.a.ld = (int64_t)p.C * 2;
+            s.a.base = p.other + ((int64_t)e * rows_e + a0) * s.a.ld;
+            s.a.limit = (rows_e - a0) * s.a.ld;
+            s.a.c_size = p.C;
+#pragma unroll
+            for (int j = 0; j < Operand<AMODE, kTileA>::kLoads; ++j) {
+                const int r = j * (kTileThreads / 8) + tid / 8;
+                int unit = r, up = 0;
+                if (kGated) {   // a wave's rows: FA * 8 gate rows, then the up rows of the same units
+                    unit = r / (16 * FA) * (8 * FA) + r % (8 * FA);
+                    up = r / (8 * FA) % 2;
+                }
+                s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (((lane & 7) ^ (lane >> 3)) << 4) : kNowhere;
+            }
+        } else {
+            s.a.ld = (int64_t)p.NA * 2;
+            s.a.limit = (int64_t)a0 * 2;
+            s.a.c_size = kByRows ? p.C : rows;
+            s.a.base = (kByRows ? p.other + (int64_t)e * p.C * s.a.ld : p.rows + first * s.a.ld) + s.a.limit;
+#pragma unroll
+            for (int j = 0; j < Operand<AMODE, kTileA>::kLoads; ++j) {
+                const int c = j * (kTileThreads / 32) + tid / 32, swz = (c & 3) | ((c >> 3 & 1) << 2);
+                const int col = ((tid & 31) ^ (swz << 1)) * 8;
+                s.a.at[j] = col < a_left ? (uint32_t)(c * s.a.ld) + col * 2 : kNowhere;
+            }
+        }
+        // operand B
+        if (BMODE == kAlongC) {
+            s.b.ld = (int64_t)p.C * 2;
+            s.b.base = p.rows + ((int64_t)first + b0) * s.b.ld;
+            s.b.limit = (b_left < BB ? b_left : BB) * s.b.ld;
+            s.b.c_size = p.C;
+#pragma unroll
+            for (int j = 0; j < Operand<BMODE, BB>::kLoads; ++j)
+                s.b.at[j] = (uint32_t)((j * (kTileThreads / 8) + tid / 8) * s.b.ld) + (((lane & 7) ^ (lane >> 3)) << 4);
+            steps = (p.C + kTileC - 1) / kTileC;
+        } else {
+            constexpr int kChunks = BB / 8;
+            s.b.ld = (int64_t)p.NB * 2;
+            s.b.limit = (int64_t)b0 * 2;
+            s.b.base = p.other + first * s.b.ld + s.b.limit;
+            s.b.c_size = rows;
+#pragma unroll
+            for (int j = 0; j < Operand<BMODE, BB>::kLoads; ++j) {
+                const int c = j * (kTileThreads / kChunks) + tid / kChunks, swz = (c & 3) | ((c >> 3 & 1) << 2);
+                const int col = ((tid & (kChunks - 1)) ^ (swz << 1)) * 8;
+                s.b.at[j] = col < b_left ? (uint32_t)(c * s.b.ld) + col * 2 : kNowhere;
+            }
+            steps = (rows + kTileC - 1) / kTileC;
+        }
+
+        f32x4 acc[FA][FB];
+#pragma unroll
+        for (int f = 0; f < FA; ++f)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) acc[f][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (steps > 0) {
+            if (wb * FB * 16 < b_left) tile_sum<AMODE, BMODE, BB, FA, FB, true>(s, lds, lds + kStage, steps, acc);
+            else tile_sum<AMODE, BMODE, BB, FA, FB, false>(s, lds, lds + kStage, steps, acc);   // rows past the segment: loads and barriers only
+        }
+
+        // lane l holds, of fragment (f, j), the outputs a = 16 * f + l / 16 * 4 + 0 .. 3 of b = 16 * j + l % 16
+        const int a_lane = wa * (kGated ? FA / 2 : FA) * 16 + (lane >> 4) * 4, b_lane = wb * FB * 16 + (lane & 15);
+        const int64_t row0 = kByRows ? (int64_t)first + b0 : (int64_t)e * p.NB + b0;
+#pragma unroll
+        for (int j = 0; j < FB; ++j) {
+            const int b = b_lane + j * 16;
+            if (b >= b_left) continue;
+#pragma unroll
+            for (int f = 0; f < (kGated ? FA / 2 : FA); ++f) {
+                const int a = a_lane + f * 16;
+                if (a >= a_left) continue;
+                const f32x4 v = acc[f][j];
+                if (STORE == kStoreBf16) {
+                    store4(p.out, (row0 + b) * p.NA + a0 + a, v);
+                } else if (STORE == kStoreF32) {
+                    *(f32x4 *)(p.out + ((row0 + b) * p.NA + a0 + a) * 4) = v;
+                } else if (STORE == kStoreGated) {
+                    const f32x4 up = acc[f + FA / 2][j];
+                    f32x4 h;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) h[q] = silu(v[q]) * up[q];
+                    store4(p.out, (row0 + b) * p.NA + a0 + a, h);
+                    if (p.pre) {
+                        store4(p.pre, (row0 + b) * 2 * p.NA + a0 + a, v);
+                        store4(p.pre, ((row0 + b) * 2 + 1) * p.NA + a0 + a, up);
+                    }
+                } else {
+                    const bf16x4 gate = *(const bf16x4 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
+                    const bf16x4 up = *(const bf16x4 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
+                    f32x4 dgate, dup;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float g = (float)gate[q], sig = 1.0f / (1.0f + __expf(-g));
+                        dup[q] = v[q] * g * sig;
+                        dgate[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
+                    }
+                    store4(p.out, (row0 + b) * 2 * p.NA + a0 + a, dgate);
+                    store4(p.out, ((row0 + b) * 2 + 1) * p.NA + a0 + a, dup);
+                }
+            }
+        }
+    }
+}
+
+}   // namespace
+
+#endif
