@@ -49,6 +49,17 @@ extern "C" {
 #define FUSCO_BF16 0
 #define FUSCO_F32 1
 
+/* scores of fusco_route */
+#define FUSCO_SCORE_SOFTMAX 0
+#define FUSCO_SCORE_SIGMOID 1
+#define FUSCO_MAX_GROUPS 64 /* groups of experts */
+
+/* gate of fusco_norm_after */
+#define FUSCO_GATE_NONE 0
+#define FUSCO_GATE_CHANNEL 1 /* one value per column, shared by all tokens */
+#define FUSCO_GATE_TOKEN 2   /* one value per token, shared by all columns */
+#define FUSCO_MAX_NORM_H 32768 /* columns of the norms */
+
 /* flags of fusco_dispatch (no tensor flag means FUSCO_DISPATCH_EXPERT) */
 #define FUSCO_DISPATCH_EXPERT 1u /* write the expert-activation tensor (level 2 result)       */
 #define FUSCO_DISPATCH_WIRE 2u   /* write the deduplicated per-device receive tensors (level 1) */
@@ -338,6 +349,89 @@ int fusco_segments_copy(const void *d_src, uint64_t src_bytes, const fusco_segme
                         uint64_t dst_bytes, const fusco_segment *d_dst_desc, const uint64_t *d_cum, int64_t n,
                         uint64_t stream_capacity, uint64_t slice_bytes, uint32_t *d_slice_fill, int32_t *d_status,
                         void *stream);
+
+/*
+ * Gradient of fusco_combine (d_y, d_w and the layout as given to it, d_dout the gradient of its output):
+ *     dy[pair_slot[t*k+j], :] = w[t, j] * dout[t, :]             rounded once when y_dtype is FUSCO_BF16
+ *     dw[t, j] = sum over h of dout[t, h] * y[pair_slot[t*k+j], h]   held in fp32
+ * d_dy: [P, H] of y_dtype, every assigned row is written; d_dw: [N, k] fp32, 0 for a pair without a slot.  d_dout: [N, H] of
+ * dout_dtype.  H: a multiple of 8, at most 32768.  The gradient of fusco_dispatch needs no call of its own: it is fusco_combine with
+ * weights of 1.
+ */
+int fusco_combine_backward(const fusco_layout *L, const void *d_y, int y_dtype, const float *d_w, const void *d_dout,
+                           int dout_dtype, void *d_dy, float *d_dw, int32_t H, void *stream);
+
+/*
+ * Routing to experts: from a token's logits to the k experts and weights that fusco_plan and fusco_combine take.
+ *     s[e] = 1 / (1 + exp(-l[e]))  (FUSCO_SCORE_SIGMOID)   or   exp(l[e] - max l) / sum exp(l - max l)  (FUSCO_SCORE_SOFTMAX)
+ *     b[e] = s[e] + bias[e]        what experts compete by: a bias keeps the load balanced and does not enter the weights
+ *     groups > 1: group g holds the E / groups experts from g * E / groups on and counts as much as its group_best (1 or 2) largest b
+ *     together; only experts of the keep_groups best groups compete (with groups on devices: a token goes to few devices)
+ *     topk_idx[j]: the expert with the j-th largest b, j = 0 .. k-1
+ *     w[j] = scale * s[topk_idx[j]] / sum_i s[topk_idx[i]]  with renorm, scale * s[topk_idx[j]] without
+ * Equal values go to the lower index, for groups as for experts.  Without a bias the softmax's denominator, the same for the whole
+ * row, is left out where scores are compared.  Logits of -infinity (experts that are not allowed) have score 0; a row without any
+ * allowed expert gets the experts that its ties name, with weights 0.  A NaN score ranks below every number; a softmax row with a NaN
+ * or +infinity has weights NaN.  topk_idx always holds k distinct experts.
+ * d_logits: [N, E] of logits_dtype (FUSCO_BF16 or FUSCO_F32), rows logits_stride elements apart (at least E; any alignment of its
+ * type).  d_bias: [E] fp32 or NULL.  d_topk_idx: [N, k] int32, d_w: [N, k] fp32.  k <= keep_groups * (E / groups), E a multiple of
+ * groups, group_best <= E / groups.
+ */
+typedef struct fusco_router {
+    int32_t N, E, k;
+    int32_t score;              /* FUSCO_SCORE_*                                    */
+    int32_t groups, keep_groups, group_best;   /* 1, 1, 1 for a choice among all    */
+    int32_t renorm;             /* 0 or 1                                           */
+    int32_t logits_dtype;
+    float scale;
+    int64_t logits_stride;
+} fusco_router;
+int fusco_route(const fusco_router *R, const void *d_logits, const float *d_bias, int32_t *d_topk_idx, float *d_w, void *stream);
+
+/*
+ * Gradient of fusco_route's weights with respect to the logits (the choice itself has none, nor has the bias): d_dw [N, k] fp32 is
+ * the gradient of the weights, d_dlogits [N, E] of logits_dtype (contiguous) is written whole.  Groups and bias play no part.
+ */
+int fusco_route_backward(const fusco_router *R, const void *d_logits, const int32_t *d_topk_idx, const float *d_dw, void *d_dlogits,
+                         void *stream);
+
+/*
+ * Norms before and after a block (an attention or an MoE block) on a residual stream, inv(x) = 1 / sqrt(mean(x^2) + eps) per row:
+ *     before:  out  = x * inv(x) * gain
+ *     after:   out  = r + scale * gate * (y * inv(y) * gain)          and, if d_next is not NULL,
+ *              next = out * inv(out) * next_gain                      (the norm before the next block, of the unrounded out)
+ * y is the block's output, r the stream before it; gate is a value per column, a value per token or 1.  Sums are held in fp32, results
+ * are rounded once.  Streams (r, x, out of fusco_norm_after and their gradients) are of stream_dtype, what goes into and comes out
+ * of blocks (y, next, out of fusco_norm_before and their gradients) of block_dtype; gains and gate of gain_dtype; FUSCO_BF16 with a
+ * block_dtype of FUSCO_F32 is not offered for the stream (FUSCO_ERR_UNSUPPORTED).  All tensors [N, H] contiguous, H a multiple of 8 and
+ * at most FUSCO_MAX_NORM_H; eps > 0.  out may be the buffer of r, next that of y (where their types are the same).
+ */
+typedef struct fusco_norm {
+    int32_t N, H;
+    int32_t stream_dtype, block_dtype, gain_dtype;
+    int32_t gate_kind;          /* FUSCO_GATE_*, fusco_norm_after and its gradient only */
+    float scale, eps;
+} fusco_norm;
+int fusco_norm_before(const fusco_norm *n, const void *d_x, const void *d_gain, void *d_out, void *stream);
+int fusco_norm_after(const fusco_norm *n, const void *d_r, const void *d_y, const void *d_gain, const void *d_gate, void *d_out,
+                     const void *d_next_gain, void *d_next, void *stream);
+
+/*
+ * Their gradients.  Gradients of gains and gate are fp32, added up over the rows in a fixed order (two launches; partial sums in
+ * d_scratch, fusco_norm_scratch_bytes() bytes, contents irrelevant before and after).
+ * before:  dx = dres + gradient through the norm; d_dout is the gradient of out, d_dres [N, H] of stream_dtype (NULL: 0) what reaches x
+ *          past the block; d_dgain [H].
+ * after:   d_dout is the gradient of out (NULL: 0), d_dnext that of next (NULL if next was not asked for; then d_out, d_next_gain
+ *          and d_dnext_gain are not used), d_out the out that fusco_norm_after wrote.  Results: d_dr, d_dy [N, H], d_dgain [H],
+ *          d_dgate [H] or [N] by gate_kind, d_dnext_gain [H].
+ */
+size_t fusco_norm_scratch_bytes(int32_t N, int32_t H);
+int fusco_norm_before_backward(const fusco_norm *n, const void *d_dout, const void *d_x, const void *d_gain, const void *d_dres,
+                               void *d_dx, float *d_dgain, void *d_scratch, size_t scratch_bytes, void *stream);
+int fusco_norm_after_backward(const fusco_norm *n, const void *d_dout, const void *d_dnext, const void *d_y, const void *d_out,
+                              const void *d_gain, const void *d_gate, const void *d_next_gain, void *d_dr, void *d_dy,
+                              float *d_dgain, float *d_dgate, float *d_dnext_gain, void *d_scratch, size_t scratch_bytes,
+                              void *stream);
 
 /*
  * Products of the experts, on the rows that fusco_dispatch wrote and a layout's plan describes: expert e has the rows

@@ -12,6 +12,8 @@ from .binding import (BF16, F32, DISPATCH_EXPERT, DISPATCH_WIRE, DISPATCH_TWO_HO
                       fusco_combine_two_hop, fusco_balance_groups, fusco_cross_node_load, fusco_segments_scan,
                       fusco_segments_copy, fusco_disaggregated_plan, fusco_disaggregated_dispatch,
                       fusco_disaggregated_combine,
+                      fusco_combine_backward, fusco_route, fusco_route_backward, fusco_norm_before, fusco_norm_after, fusco_norm_scratch_bytes,
+                      fusco_norm_before_backward, fusco_norm_after_backward, SCORE_SOFTMAX, SCORE_SIGMOID, GATE_NONE, GATE_CHANNEL, GATE_TOKEN,
                       fusco_experts_gated, fusco_experts_linear, fusco_experts_input_grad, fusco_experts_weight_grad)
 
 __all__ = ["BF16", "F32", "DISPATCH_EXPERT", "DISPATCH_WIRE", "DISPATCH_TWO_HOP", "DISPATCH_STREAMING", "FuscoError", "Layout",
@@ -20,4 +22,6 @@ __all__ = ["BF16", "F32", "DISPATCH_EXPERT", "DISPATCH_WIRE", "DISPATCH_TWO_HOP"
            "fusco_probe_copy", "fusco_probe_rows", "fusco_probe_pieces", "fusco_probe_consume_slices", "fusco_probe_time_next_call", "fusco_probe_source_chunk_bytes", "fusco_probe_dispatch_kernel", "fusco_probe_dispatch_occupancy", "fusco_probe_dispatch_pull", "fusco_probe_dispatch_walk", "fusco_probe_dispatch_route", "fusco_probe_plan_through", "fusco_probe_plan_dispatch_through", "fusco_probe_segments_wide", "fusco_combine_two_hop", "fusco_balance_groups", "fusco_cross_node_load",
            "fusco_segments_scan", "fusco_segments_copy", "fusco_disaggregated_plan", "fusco_disaggregated_dispatch",
            "fusco_disaggregated_combine",
+           "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
+           "fusco_norm_before_backward", "fusco_norm_after_backward", "SCORE_SOFTMAX", "SCORE_SIGMOID", "GATE_NONE", "GATE_CHANNEL", "GATE_TOKEN",
            "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad"]

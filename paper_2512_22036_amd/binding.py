@@ -17,6 +17,8 @@ import torch
 
 BF16, F32 = 0, 1
 DISPATCH_EXPERT, DISPATCH_WIRE, DISPATCH_TWO_HOP, DISPATCH_STREAMING = 1, 2, 4, 8
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfusco.so")
@@ -25,6 +27,8 @@ EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_
            "fusco_layout_bind", "fusco_plan", "fusco_plan_static", "fusco_dispatch", "fusco_dispatch_in_transfer_order", "fusco_combine", "fusco_plan_dispatch", "fusco_probe_copy", "fusco_probe_rows", "fusco_probe_pieces", "fusco_probe_consume_slices", "fusco_probe_time_next_call", "fusco_probe_source_chunk_bytes", "fusco_probe_dispatch_kernel", "fusco_probe_dispatch_occupancy", "fusco_probe_dispatch_pull", "fusco_probe_dispatch_walk", "fusco_probe_dispatch_route", "fusco_probe_plan_through", "fusco_probe_plan_dispatch_through", "fusco_probe_segments_wide",
            "fusco_combine_two_hop", "fusco_balance_groups", "fusco_cross_node_load", "fusco_segments_scan", "fusco_segments_copy",
            "fusco_disaggregated_plan", "fusco_disaggregated_dispatch", "fusco_disaggregated_combine",
+           "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
+           "fusco_norm_before_backward", "fusco_norm_after_backward",
            "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad")
 
 
@@ -43,6 +47,18 @@ class _CLayout(ctypes.Structure):
                 ("pair_send_row", ctypes.c_void_p), ("slot_send_row", ctypes.c_void_p),
                 ("pair_first", ctypes.c_void_p), ("status", ctypes.c_void_p),
                 ("tile_slots", ctypes.c_void_p), ("tile_tokens", ctypes.c_int32), ("tile_count", ctypes.c_int32)]
+
+
+class _CRouter(ctypes.Structure):
+    """Mirror of struct fusco_router."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "E", "k", "score", "groups", "keep_groups", "group_best", "renorm", "logits_dtype")] + [
+        ("scale", ctypes.c_float), ("logits_stride", ctypes.c_int64)]
+
+
+class _CNorm(ctypes.Structure):
+    """Mirror of struct fusco_norm."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "H", "stream_dtype", "block_dtype", "gain_dtype", "gate_kind")] + [
+        ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -132,6 +148,23 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_disaggregated_dispatch.argtypes = [lp, lp, vp, sz, vp, vp, vp, vp]
     lib.fusco_disaggregated_combine.restype = ctypes.c_int
     lib.fusco_disaggregated_combine.argtypes = [lp, lp, vp, ctypes.c_int, vp, vp, vp, vp, ctypes.c_int, i32, vp]
+    rp, np_ = ctypes.POINTER(_CRouter), ctypes.POINTER(_CNorm)
+    lib.fusco_combine_backward.restype = ctypes.c_int
+    lib.fusco_combine_backward.argtypes = [lp, vp, ctypes.c_int, vp, vp, ctypes.c_int, vp, vp, i32, vp]
+    lib.fusco_route.restype = ctypes.c_int
+    lib.fusco_route.argtypes = [rp, vp, vp, vp, vp, vp]
+    lib.fusco_route_backward.restype = ctypes.c_int
+    lib.fusco_route_backward.argtypes = [rp, vp, vp, vp, vp, vp]
+    lib.fusco_norm_scratch_bytes.restype = sz
+    lib.fusco_norm_scratch_bytes.argtypes = [i32, i32]
+    lib.fusco_norm_before.restype = ctypes.c_int
+    lib.fusco_norm_before.argtypes = [np_, vp, vp, vp, vp]
+    lib.fusco_norm_after.restype = ctypes.c_int
+    lib.fusco_norm_after.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.fusco_norm_before_backward.restype = ctypes.c_int
+    lib.fusco_norm_before_backward.argtypes = [np_, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.fusco_norm_after_backward.restype = ctypes.c_int
+    lib.fusco_norm_after_backward.argtypes = [np_] + [vp] * 13 + [sz, vp]
     lib.fusco_experts_gated.restype = ctypes.c_int
     lib.fusco_experts_gated.argtypes = [lp, vp, vp, vp, vp, i32, i32, vp]
     lib.fusco_experts_linear.restype = ctypes.c_int
@@ -347,6 +380,177 @@ def fusco_combine(layout: Layout, y: torch.Tensor, w: torch.Tensor, out: torch.T
     _check(load_library().fusco_combine(ctypes.byref(layout.c), y.data_ptr(), _dtype_code(y, "y"), w.data_ptr(),
                                         out.data_ptr(), _dtype_code(out, "out"), H, 0, _stream(stream)),
            "fusco_combine")
+
+
+def fusco_combine_backward(layout: Layout, y: torch.Tensor, w: torch.Tensor, dout: torch.Tensor, dy: torch.Tensor,
+                           dw: torch.Tensor, stream=None) -> None:
+    """Gradients of fusco_combine: dout [N, H] in, dy [P, H] (of y's type) and dw [N, k] float32 out."""
+    _rows(y, "y", layout.P)
+    _rows(dy, "dy", layout.P)
+    _rows(dout, "dout", layout.N)
+    H = y.shape[1]
+    if dy.dtype != y.dtype or dy.shape[1] != H or dout.shape[1] != H:
+        raise FuscoError("dy must be of y's type, dy and dout must have %d columns" % H)
+    for t, name in ((w, "w"), (dw, "dw")):
+        _fp32(t, name, (layout.N, layout.k))
+    _check(load_library().fusco_combine_backward(ctypes.byref(layout.c), y.data_ptr(), _dtype_code(y, "y"), w.data_ptr(),
+                                                 dout.data_ptr(), _dtype_code(dout, "dout"), dy.data_ptr(), dw.data_ptr(), H,
+                                                 _stream(stream)), "fusco_combine_backward")
+
+
+def _fp32(t: torch.Tensor, name: str, shape) -> torch.Tensor:
+    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise FuscoError("%s must be a contiguous float32 device tensor of shape %s" % (name, list(shape)))
+    return t
+
+
+def _router(logits: torch.Tensor, topk_idx: torch.Tensor, score: int, groups: int, keep_groups: int, group_best: int,
+            renorm: bool, scale: float) -> _CRouter:
+    if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise FuscoError("logits must be a 2-D device tensor whose rows are contiguous")
+    N, E = logits.shape
+    if (not topk_idx.is_cuda or topk_idx.dtype != torch.int32 or not topk_idx.is_contiguous() or topk_idx.dim() != 2
+            or topk_idx.shape[0] != N):
+        raise FuscoError("topk_idx must be a contiguous int32 device tensor of shape [N, k]")
+    stride = logits.stride(0) if N > 1 else max(E, 1)
+    return _CRouter(N, E, topk_idx.shape[1], score, groups, keep_groups, group_best, int(bool(renorm)), _dtype_code(logits, "logits"),
+                    scale, stride)
+
+
+def fusco_route(logits: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                score: int = SCORE_SOFTMAX, groups: int = 1, keep_groups: int = 1, group_best: int = 1, renorm: bool = True,
+                scale: float = 1.0, stream=None) -> None:
+    """Routing: logits [N, E] (bfloat16 or float32, rows may lie apart) to topk_idx [N, k] int32 and w [N, k] float32, as
+    fusco_plan and fusco_combine take them.  bias: float32 [E], added to the scores for the choice alone."""
+    R = _router(logits, topk_idx, score, groups, keep_groups, group_best, renorm, scale)
+    _fp32(w, "w", topk_idx.shape)
+    if bias is not None:
+        _fp32(bias, "bias", (R.E,))
+    _check(load_library().fusco_route(ctypes.byref(R), logits.data_ptr(), _ptr(bias), topk_idx.data_ptr(), w.data_ptr(),
+                                      _stream(stream)), "fusco_route")
+
+
+def fusco_route_backward(logits: torch.Tensor, topk_idx: torch.Tensor, dw: torch.Tensor, dlogits: torch.Tensor,
+                         score: int = SCORE_SOFTMAX, renorm: bool = True, scale: float = 1.0, stream=None) -> None:
+    """Gradient of fusco_route's weights: dw [N, k] float32 to dlogits [N, E], contiguous and of logits' type."""
+    R = _router(logits, topk_idx, score, 1, 1, 1, renorm, scale)
+    _fp32(dw, "dw", topk_idx.shape)
+    if not dlogits.is_cuda or dlogits.dtype != logits.dtype or dlogits.shape != logits.shape or not dlogits.is_contiguous():
+        raise FuscoError("dlogits must be a contiguous device tensor of logits' shape and type")
+    _check(load_library().fusco_route_backward(ctypes.byref(R), logits.data_ptr(), topk_idx.data_ptr(), dw.data_ptr(),
+                                               dlogits.data_ptr(), _stream(stream)), "fusco_route_backward")
+
+
+def _norm(stream: torch.Tensor, block_dtype: torch.dtype, params, gate: Optional[torch.Tensor], gate_kind: Optional[int],
+          scale: float, eps: float) -> _CNorm:
+    """The struct for rows like `stream` [N, H]; params: (name, tensor or None) of [H] each, of one type with the gate."""
+    if not stream.is_cuda or stream.dim() != 2 or not stream.is_contiguous():
+        raise FuscoError("the stream must be a contiguous 2-D device tensor")
+    N, H = stream.shape
+    given = [(n, t) for n, t in params if t is not None]
+    kind = GATE_NONE
+    if gate is not None:
+        kind = gate_kind
+        if kind is None:
+            if N == H:
+                raise FuscoError("gate [%d] may be per channel or per token: give gate_kind" % N)
+            kind = GATE_TOKEN if gate.dim() == 1 and gate.shape[0] == N else GATE_CHANNEL
+        if kind not in (GATE_CHANNEL, GATE_TOKEN):
+            raise FuscoError("gate_kind must be GATE_CHANNEL or GATE_TOKEN")
+    for name, t in given + ([("gate", gate)] if gate is not None else []):
+        want = N if name == "gate" and kind == GATE_TOKEN else H
+        if not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != (want,) or t.dtype != given[0][1].dtype:
+            raise FuscoError("%s must be a contiguous device tensor of shape [%d], gains and gate of one type" % (name, want))
+    code = {torch.bfloat16: BF16, torch.float32: F32}
+    if stream.dtype not in code or block_dtype not in code or given[0][1].dtype not in code:
+        raise FuscoError("tensors must be bfloat16 or float32")
+    return _CNorm(N, H, code[stream.dtype], code[block_dtype], code[given[0][1].dtype], kind, scale, eps)
+
+
+def _like(n: _CNorm, dtype: torch.dtype, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != (n.N, n.H)):
+            raise FuscoError("%s must be a contiguous %s device tensor of shape [%d, %d]" % (name, dtype, n.N, n.H))
+
+
+def fusco_norm_before(x: torch.Tensor, gain: torch.Tensor, out: torch.Tensor, eps: float = 1e-6, stream=None) -> None:
+    """out = x / sqrt(mean(x^2) + eps) * gain, row by row: the norm before a block; x is the residual stream."""
+    n = _norm(x, out.dtype, [("gain", gain)], None, None, 1.0, eps)
+    _like(n, out.dtype, out=out)
+    _check(load_library().fusco_norm_before(ctypes.byref(n), x.data_ptr(), gain.data_ptr(), out.data_ptr(), _stream(stream)),
+           "fusco_norm_before")
+
+
+def fusco_norm_after(r: torch.Tensor, y: torch.Tensor, gain: torch.Tensor, out: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                     scale: float = 1.0, next_gain: Optional[torch.Tensor] = None, next_out: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, gate_kind: Optional[int] = None, stream=None) -> None:
+    """out = r + scale * gate * norm(y) * gain: the norm after a block, its gate and the sum with the residual stream r; with
+    next_out also the norm before the next block, norm(out) * next_gain.  gate: [H] (per channel) or [N] (per token);
+    gate_kind says which where N == H."""
+    if (next_gain is None) != (next_out is None):
+        raise FuscoError("next_gain and next_out go together")
+    n = _norm(r, y.dtype, [("gain", gain), ("next_gain", next_gain)], gate, gate_kind, scale, eps)
+    _like(n, r.dtype, out=out)
+    _like(n, y.dtype, y=y, next_out=next_out)
+    _check(load_library().fusco_norm_after(ctypes.byref(n), r.data_ptr(), y.data_ptr(), gain.data_ptr(), _ptr(gate), out.data_ptr(),
+                                           _ptr(next_gain), _ptr(next_out), _stream(stream)), "fusco_norm_after")
+
+
+def fusco_norm_scratch_bytes(N: int, H: int) -> int:
+    return load_library().fusco_norm_scratch_bytes(N, H)
+
+
+def _norm_scratch(n: _CNorm, scratch: Optional[torch.Tensor], device) -> torch.Tensor:
+    if scratch is None:
+        return torch.empty(fusco_norm_scratch_bytes(n.N, n.H), dtype=torch.uint8, device=device)
+    if not scratch.is_cuda or not scratch.is_contiguous():
+        raise FuscoError("scratch must be a contiguous device tensor")
+    return scratch
+
+
+def fusco_norm_before_backward(dout: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, dx: torch.Tensor, dgain: torch.Tensor,
+                               dres: Optional[torch.Tensor] = None, eps: float = 1e-6, scratch: Optional[torch.Tensor] = None,
+                               stream=None) -> None:
+    """Gradients of fusco_norm_before: dx = dres + what comes through the norm, dgain float32 [H].  dres: the gradient that
+    reaches x past the block.  scratch: fusco_norm_scratch_bytes(N, H) bytes, made here if not given."""
+    n = _norm(x, dout.dtype, [("gain", gain)], None, None, 1.0, eps)
+    _like(n, dout.dtype, dout=dout)
+    _like(n, x.dtype, dx=dx, dres=dres)
+    _fp32(dgain, "dgain", (n.H,))
+    scratch = _norm_scratch(n, scratch, x.device)
+    _check(load_library().fusco_norm_before_backward(ctypes.byref(n), dout.data_ptr(), x.data_ptr(), gain.data_ptr(), _ptr(dres),
+                                                     dx.data_ptr(), dgain.data_ptr(), scratch.data_ptr(),
+                                                     scratch.numel() * scratch.element_size(), _stream(stream)),
+           "fusco_norm_before_backward")
+
+
+def fusco_norm_after_backward(dout: Optional[torch.Tensor], y: torch.Tensor, gain: torch.Tensor, dr: torch.Tensor, dy: torch.Tensor,
+                              dgain: torch.Tensor, gate: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                              scale: float = 1.0, dnext: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                              next_gain: Optional[torch.Tensor] = None, dnext_gain: Optional[torch.Tensor] = None,
+                              eps: float = 1e-6, gate_kind: Optional[int] = None, scratch: Optional[torch.Tensor] = None,
+                              stream=None) -> None:
+    """Gradients of fusco_norm_after: dr and dy [N, H], dgain, dgate and dnext_gain float32.  dnext, out (as fusco_norm_after
+    wrote it), next_gain and dnext_gain go together; dout may be None beside them."""
+    asked = [t is not None for t in (dnext, out, next_gain, dnext_gain)]
+    if any(asked) != all(asked) or (dout is None and dnext is None):
+        raise FuscoError("dnext, out, next_gain and dnext_gain go together, and dout or dnext must be given")
+    if (gate is None) != (dgate is None):
+        raise FuscoError("gate and dgate go together")
+    n = _norm(dr, y.dtype, [("gain", gain), ("next_gain", next_gain)], gate, gate_kind, scale, eps)
+    _like(n, dr.dtype, dout=dout, out=out)
+    _like(n, y.dtype, y=y, dy=dy, dnext=dnext)
+    _fp32(dgain, "dgain", (n.H,))
+    if dnext is not None:
+        _fp32(dnext_gain, "dnext_gain", (n.H,))
+    if gate is not None:
+        _fp32(dgate, "dgate", gate.shape)
+    scratch = _norm_scratch(n, scratch, dr.device)
+    _check(load_library().fusco_norm_after_backward(ctypes.byref(n), _ptr(dout), _ptr(dnext), y.data_ptr(), _ptr(out), gain.data_ptr(),
+                                                    _ptr(gate), _ptr(next_gain), dr.data_ptr(), dy.data_ptr(), dgain.data_ptr(),
+                                                    _ptr(dgate), _ptr(dnext_gain), scratch.data_ptr(),
+                                                    scratch.numel() * scratch.element_size(), _stream(stream)),
+           "fusco_norm_after_backward")
 
 
 def _bf16(t: torch.Tensor, name: str, shape) -> torch.Tensor:

@@ -1,6 +1,11 @@
 // The operators around the token shuffle of an MoE block for MI355X (gfx950): the experts' products on the dispatched rows
-// (products.h).  C entry points, declared in fusco.h.
+// (products.h), routing (routing.h), the norms around the block (norms.h) and the gradient of the combine (gradients.h).  C entry
+// points, declared in fusco.h.
 #include "products.h"
+#include "routing.h"
+#include "norms.h"
+#include "gradients.h"
+#include <math.h>
 
 namespace {
 
@@ -36,9 +41,277 @@ int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
     return launch_status();
 }
 
+// ---- rows of one workgroup each
+
+bool dtype_ok(int t) { return t == FUSCO_BF16 || t == FUSCO_F32; }
+
+// threads of a workgroup whose threads take `cpt` chunks each
+unsigned row_threads(int chunks, int cpt) { return (unsigned)((chunks + cpt * kWave - 1) / (cpt * kWave) * kWave); }
+
+// chunks per thread: few rows spread each over as many threads as there are chunks, up to 512; more in flight per thread otherwise
+int row_cpt(int chunks, bool few)
+{
+    if (few) return chunks <= 512 ? 1 : chunks <= 1024 ? 2 : 4;
+    return chunks <= 64 ? 1 : chunks <= 1024 ? 2 : 4;
+}
+
+// calls f(integral constant CPT)
+template <typename F>
+void with_cpt(int cpt, F f)
+{
+    if (cpt == 1) f(std::integral_constant<int, 1>());
+    else if (cpt == 2) f(std::integral_constant<int, 2>());
+    else f(std::integral_constant<int, 4>());
+}
+
+// calls f(stream is bf16, block is bf16) for the pairs of types that are offered
+template <typename F>
+void with_types(const fusco_norm *n, F f)
+{
+    if (n->stream_dtype == FUSCO_BF16) f(std::true_type(), std::true_type());
+    else if (n->block_dtype == FUSCO_BF16) f(std::false_type(), std::true_type());
+    else f(std::false_type(), std::false_type());
+}
+
+int norm_check(const fusco_norm *n)
+{
+    if (!n || n->N < 0 || n->H < 8 || n->H % 8 != 0 || n->H > FUSCO_MAX_NORM_H || !(n->eps > 0.0f) || !isfinite(n->eps)) return FUSCO_ERR_INVALID_ARG;
+    if (!dtype_ok(n->stream_dtype) || !dtype_ok(n->block_dtype) || !dtype_ok(n->gain_dtype)) return FUSCO_ERR_UNSUPPORTED;
+    if (n->stream_dtype == FUSCO_BF16 && n->block_dtype != FUSCO_BF16) return FUSCO_ERR_UNSUPPORTED;
+    return FUSCO_OK;
+}
+
+int gate_check(const fusco_norm *n, const void *d_gate)
+{
+    if (n->gate_kind != FUSCO_GATE_NONE && n->gate_kind != FUSCO_GATE_CHANNEL && n->gate_kind != FUSCO_GATE_TOKEN) return FUSCO_ERR_UNSUPPORTED;
+    const bool empty = n->N == 0 && n->gate_kind == FUSCO_GATE_TOKEN;
+    return (n->gate_kind == FUSCO_GATE_NONE || empty || d_gate) && aligned16(d_gate) ? FUSCO_OK : FUSCO_ERR_INVALID_ARG;
+}
+
+// workgroups of the norms' gradients, each of which leaves a row of partial sums per parameter
+constexpr int kNormGroups = 512;
+int norm_groups(int N) { return N < kNormGroups ? (N < 1 ? 1 : N) : kNormGroups; }
+
+template <bool AFTER>
+int launch_norm(const fusco_norm *n, const NormArgs &a, hipStream_t s)
+{
+    const int cpt = row_cpt(a.chunks, n->N < 1024);
+    const dim3 grid((unsigned)n->N), block(row_threads(a.chunks, cpt));
+    with_types(n, [&](auto st, auto bl) {
+        with_cpt(cpt, [&](auto c) { hipLaunchKernelGGL((norm_kernel<decltype(st)::value, decltype(bl)::value, decltype(c)::value, AFTER>), grid, block, 0, s, a); });
+    });
+    return launch_status();
+}
+
+template <bool AFTER, bool NEXT, bool CHANNEL>
+void launch_norm_grad(const fusco_norm *n, const NormGradArgs &a, hipStream_t s)
+{
+    const int cpt = row_cpt(a.chunks, n->N < 1024);
+    const dim3 grid((unsigned)norm_groups(n->N)), block(row_threads(a.chunks, cpt));
+    with_types(n, [&](auto st, auto bl) {
+        with_cpt(cpt, [&](auto c) { hipLaunchKernelGGL((norm_grad_kernel<decltype(st)::value, decltype(bl)::value, decltype(c)::value, AFTER, NEXT, CHANNEL>), grid, block, 0, s, a); });
+    });
+}
+
+void launch_norm_join(const fusco_norm *n, const NormGradArgs &a, float *first, float *second, float *third, hipStream_t s)
+{
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((n->H + kJoinCols - 1) / kJoinCols), (unsigned)a.sums), dim3(kJoinThreads), 0, s, a.partial, norm_groups(n->N), a.sums,
+                       n->H, first, second, third);
+}
+
+// ---- routing
+
+int route_check(const fusco_router *R)
+{
+    if (!R || R->N < 0 || R->E < 1 || R->E > FUSCO_MAX_E || R->k < 1 || R->k > FUSCO_MAX_K || R->k > R->E || (int64_t)R->N * R->k >= (int64_t)1 << 31) return FUSCO_ERR_INVALID_ARG;
+    if (R->logits_stride < R->E || !isfinite(R->scale)) return FUSCO_ERR_INVALID_ARG;
+    if (!dtype_ok(R->logits_dtype) || (R->score != FUSCO_SCORE_SOFTMAX && R->score != FUSCO_SCORE_SIGMOID) || (R->renorm != 0 && R->renorm != 1)) return FUSCO_ERR_UNSUPPORTED;
+    if (R->groups < 1 || R->groups > FUSCO_MAX_GROUPS || R->E % R->groups != 0 || R->keep_groups < 1 || R->keep_groups > R->groups) return FUSCO_ERR_INVALID_ARG;
+    if (R->group_best < 1 || R->group_best > 2 || R->group_best > R->E / R->groups || R->k > R->keep_groups * (R->E / R->groups)) return FUSCO_ERR_INVALID_ARG;
+    return FUSCO_OK;
+}
+
+RouteArgs route_args(const fusco_router *R, const void *d_logits)
+{
+    RouteArgs a = {};
+    a.logits = (const char *)d_logits;
+    a.stride = R->logits_stride;
+    a.N = R->N; a.E = R->E; a.k = R->k;
+    a.groups = R->groups; a.keep_groups = R->keep_groups; a.group_best = R->group_best; a.group_size = R->E / R->groups;
+    a.bf16 = R->logits_dtype == FUSCO_BF16;
+    a.sigmoid = R->score == FUSCO_SCORE_SIGMOID;
+    a.renorm = R->renorm;
+    a.scale = R->scale;
+    return a;
+}
+
+// calls f(lanes per row, values per lane)
+template <typename F>
+void with_route_shape(const fusco_router *R, F f)
+{
+    const int per_lane = (R->E + 63) / 64;
+    if (per_lane <= 1) f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+    else if (per_lane <= 2) f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
+    else if (per_lane <= 4) f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+    else if (per_lane <= 8) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+}
+
+bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
 }   // namespace
 
 extern "C" {
+
+int fusco_route(const fusco_router *R, const void *d_logits, const float *d_bias, int32_t *d_topk_idx, float *d_w, void *stream)
+{
+    const int rc = route_check(R);
+    if (rc != FUSCO_OK) return rc;
+    const bool empty = R->N == 0;
+    if ((!empty && (!d_logits || !d_topk_idx || !d_w)) || !aligned(d_logits, R->logits_dtype == FUSCO_BF16 ? 2 : 4) || !aligned(d_bias, 4) || !aligned16(d_topk_idx) || !aligned16(d_w))
+        return FUSCO_ERR_INVALID_ARG;
+    if (empty) return FUSCO_OK;
+    RouteArgs a = route_args(R, d_logits);
+    a.bias = d_bias;
+    a.chosen = d_topk_idx;
+    a.w = d_w;
+    with_route_shape(R, [&](auto lanes, auto vpl) {
+        constexpr int kRows = kRouteThreads / decltype(lanes)::value;
+        hipLaunchKernelGGL((route_kernel<decltype(lanes)::value, decltype(vpl)::value>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kRouteThreads), 0, (hipStream_t)stream, a);
+    });
+    return launch_status();
+}
+
+int fusco_route_backward(const fusco_router *R, const void *d_logits, const int32_t *d_topk_idx, const float *d_dw, void *d_dlogits, void *stream)
+{
+    const int rc = route_check(R);
+    if (rc != FUSCO_OK) return rc;
+    const bool empty = R->N == 0;
+    if ((!empty && (!d_logits || !d_topk_idx || !d_dw || !d_dlogits)) || !aligned(d_logits, R->logits_dtype == FUSCO_BF16 ? 2 : 4) || !aligned16(d_topk_idx) || !aligned16(d_dw) ||
+        !aligned16(d_dlogits))
+        return FUSCO_ERR_INVALID_ARG;
+    if (empty) return FUSCO_OK;
+    RouteArgs a = route_args(R, d_logits);
+    a.chosen = const_cast<int32_t *>(d_topk_idx);
+    a.dw = d_dw;
+    a.dlogits = (char *)d_dlogits;
+    with_route_shape(R, [&](auto lanes, auto vpl) {
+        constexpr int kRows = kRouteThreads / decltype(lanes)::value;
+        hipLaunchKernelGGL((route_grad_kernel<decltype(lanes)::value, decltype(vpl)::value>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kRouteThreads), 0, (hipStream_t)stream, a);
+    });
+    return launch_status();
+}
+
+int fusco_norm_before(const fusco_norm *n, const void *d_x, const void *d_gain, void *d_out, void *stream)
+{
+    const int rc = norm_check(n);
+    if (rc != FUSCO_OK) return rc;
+    const void *const rows[] = {d_x, d_out}, *const shared[] = {d_gain};
+    if (check_pointers(n->N == 0, rows, 2) != FUSCO_OK || check_pointers(false, shared, 1) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (n->N == 0) return FUSCO_OK;
+    NormArgs a = {};
+    a.r = (const char *)d_x; a.next_gain = (const char *)d_gain; a.next = (char *)d_out;
+    a.N = n->N; a.chunks = n->H / kEight; a.gain_bf16 = n->gain_dtype == FUSCO_BF16;
+    a.eps = n->eps; a.inv_h = 1.0f / n->H;
+    return launch_norm<false>(n, a, (hipStream_t)stream);
+}
+
+int fusco_norm_after(const fusco_norm *n, const void *d_r, const void *d_y, const void *d_gain, const void *d_gate, void *d_out, const void *d_next_gain, void *d_next, void *stream)
+{
+    int rc = norm_check(n);
+    if (rc == FUSCO_OK) rc = gate_check(n, d_gate);
+    if (rc != FUSCO_OK) return rc;
+    if (!isfinite(n->scale)) return FUSCO_ERR_INVALID_ARG;
+    const void *const rows[] = {d_r, d_y, d_out}, *const shared[] = {d_gain};
+    if (check_pointers(n->N == 0, rows, 3) != FUSCO_OK || check_pointers(false, shared, 1) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (!aligned16(d_next) || !aligned16(d_next_gain) || (d_next && !d_next_gain)) return FUSCO_ERR_INVALID_ARG;
+    if (n->N == 0) return FUSCO_OK;
+    NormArgs a = {};
+    a.r = (const char *)d_r; a.y = (const char *)d_y; a.gain = (const char *)d_gain; a.gate = (const char *)d_gate; a.next_gain = (const char *)d_next_gain;
+    a.out = (char *)d_out; a.next = (char *)d_next;
+    a.N = n->N; a.chunks = n->H / kEight; a.gate_kind = n->gate_kind; a.gain_bf16 = n->gain_dtype == FUSCO_BF16;
+    a.scale = n->scale; a.eps = n->eps; a.inv_h = 1.0f / n->H;
+    return launch_norm<true>(n, a, (hipStream_t)stream);
+}
+
+size_t fusco_norm_scratch_bytes(int32_t N, int32_t H)
+{
+    if (N < 0 || H < 8 || H % 8 != 0 || H > FUSCO_MAX_NORM_H) return 0;
+    return (size_t)norm_groups(N) * 3 * (size_t)H * 4;
+}
+
+int fusco_norm_before_backward(const fusco_norm *n, const void *d_dout, const void *d_x, const void *d_gain, const void *d_dres, void *d_dx, float *d_dgain, void *d_scratch,
+                               size_t scratch_bytes, void *stream)
+{
+    const int rc = norm_check(n);
+    if (rc != FUSCO_OK) return rc;
+    const void *const rows[] = {d_dout, d_x, d_dx}, *const shared[] = {d_gain, d_dgain, d_scratch};
+    if (check_pointers(n->N == 0, rows, 3) != FUSCO_OK || check_pointers(false, shared, 3) != FUSCO_OK || !aligned16(d_dres)) return FUSCO_ERR_INVALID_ARG;
+    if (scratch_bytes < fusco_norm_scratch_bytes(n->N, n->H)) return FUSCO_ERR_WORKSPACE;
+    NormGradArgs a = {};
+    a.dout = (const char *)d_dres; a.dnext = (const char *)d_dout; a.out = (const char *)d_x; a.next_gain = (const char *)d_gain;
+    a.dr = (char *)d_dx;
+    a.partial = (float *)d_scratch;
+    a.N = n->N; a.chunks = n->H / kEight; a.sums = 1; a.gain_bf16 = n->gain_dtype == FUSCO_BF16;
+    a.scale = 1.0f; a.eps = n->eps; a.inv_h = 1.0f / n->H;
+    launch_norm_grad<false, true, false>(n, a, (hipStream_t)stream);
+    launch_norm_join(n, a, d_dgain, nullptr, nullptr, (hipStream_t)stream);
+    return launch_status();
+}
+
+int fusco_norm_after_backward(const fusco_norm *n, const void *d_dout, const void *d_dnext, const void *d_y, const void *d_out, const void *d_gain, const void *d_gate,
+                              const void *d_next_gain, void *d_dr, void *d_dy, float *d_dgain, float *d_dgate, float *d_dnext_gain, void *d_scratch, size_t scratch_bytes, void *stream)
+{
+    int rc = norm_check(n);
+    if (rc == FUSCO_OK) rc = gate_check(n, d_gate);
+    if (rc != FUSCO_OK) return rc;
+    if (!isfinite(n->scale)) return FUSCO_ERR_INVALID_ARG;
+    const bool empty = n->N == 0, channel = n->gate_kind == FUSCO_GATE_CHANNEL, token = n->gate_kind == FUSCO_GATE_TOKEN, next = d_dnext != nullptr || (empty && d_dnext_gain);
+    const void *const rows[] = {d_y, d_dr, d_dy}, *const shared[] = {d_gain, d_dgain, d_scratch};
+    if (check_pointers(empty, rows, 3) != FUSCO_OK || check_pointers(false, shared, 3) != FUSCO_OK || !aligned16(d_dout)) return FUSCO_ERR_INVALID_ARG;
+    const void *const after[] = {d_out}, *const after_shared[] = {d_next_gain, d_dnext_gain}, *const gates[] = {d_dgate};
+    if (next && (check_pointers(empty, after, 1) != FUSCO_OK || check_pointers(false, after_shared, 2) != FUSCO_OK || !aligned16(d_dnext))) return FUSCO_ERR_INVALID_ARG;
+    if ((channel || token) && check_pointers(empty && token, gates, 1) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (!next && !d_dout && !empty) return FUSCO_ERR_INVALID_ARG;
+    if (scratch_bytes < fusco_norm_scratch_bytes(n->N, n->H)) return FUSCO_ERR_WORKSPACE;
+    NormGradArgs a = {};
+    a.dout = (const char *)d_dout; a.dnext = (const char *)d_dnext; a.y = (const char *)d_y; a.out = (const char *)d_out;
+    a.gain = (const char *)d_gain; a.gate = (const char *)d_gate; a.next_gain = (const char *)d_next_gain;
+    a.dr = (char *)d_dr; a.dy = (char *)d_dy;
+    a.dgate_token = token ? d_dgate : nullptr;
+    a.partial = (float *)d_scratch;
+    a.N = n->N; a.chunks = n->H / kEight; a.sums = 1 + (next ? 1 : 0) + (channel ? 1 : 0);
+    a.gate_kind = n->gate_kind; a.gain_bf16 = n->gain_dtype == FUSCO_BF16;
+    a.scale = n->scale; a.eps = n->eps; a.inv_h = 1.0f / n->H;
+    hipStream_t s = (hipStream_t)stream;
+    if (next && channel) launch_norm_grad<true, true, true>(n, a, s);
+    else if (next) launch_norm_grad<true, true, false>(n, a, s);
+    else if (channel) launch_norm_grad<true, false, true>(n, a, s);
+    else launch_norm_grad<true, false, false>(n, a, s);
+    if (next) launch_norm_join(n, a, d_dnext_gain, d_dgain, d_dgate, s);
+    else launch_norm_join(n, a, d_dgain, d_dgate, nullptr, s);
+    return launch_status();
+}
+
+int fusco_combine_backward(const fusco_layout *L, const void *d_y, int y_dtype, const float *d_w, const void *d_dout, int dout_dtype, void *d_dy, float *d_dw, int32_t H, void *stream)
+{
+    if (!layout_ok(L) || H < 8 || H % 8 != 0 || H > FUSCO_MAX_NORM_H) return FUSCO_ERR_INVALID_ARG;
+    if (!dtype_ok(y_dtype) || !dtype_ok(dout_dtype)) return FUSCO_ERR_UNSUPPORTED;
+    const void *const p[] = {d_y, d_w, d_dout, d_dy, d_dw};
+    if (check_pointers(L->N == 0, p, 5) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (L->N == 0) return FUSCO_OK;
+    const CombineGradArgs a = {L->pair_slot, (const char *)d_y, (const char *)d_dout, d_w, (char *)d_dy, d_dw, L->N, L->k, H / kEight};
+    const int cpt = row_cpt(a.chunks, L->N < 1024);
+    const dim3 grid((unsigned)L->N), block(row_threads(a.chunks, cpt));
+    with_cpt(cpt, [&](auto c) {
+        constexpr int kCpt = decltype(c)::value, kJu = kCpt == 4 ? 2 : 4;
+        if (y_dtype == FUSCO_BF16 && dout_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<true, true, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
+        else if (y_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<true, false, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
+        else if (dout_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<false, true, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
+        else hipLaunchKernelGGL((combine_grad_kernel<false, false, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
+    });
+    return launch_status();
+}
 
 int fusco_experts_gated(const fusco_layout *L, const void *d_x, const void *d_w, void *d_h, void *d_pre, int32_t H, int32_t I, void *stream)
 {

@@ -1,0 +1,123 @@
+// What the kernels that work row by row share: eight elements of bf16 or fp32 at a time, sums over a wave and a workgroup.
+#ifndef FUSCO_CSRC_ROWS_H
+#define FUSCO_CSRC_ROWS_H
+
+#include "common.h"
+
+namespace {
+
+constexpr int kEight = 8;   // elements per thread and access: 16 bytes of bf16, two times 16 bytes of fp32
+
+typedef __bf16 rows_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float rows_f32x4 __attribute__((ext_vector_type(4)));
+
+struct Eight {
+    float v[kEight];
+};
+
+template <bool BF16>
+struct RawEight;                     // as it lies in memory
+template <>
+struct RawEight<true> {
+    rows_bf16x8 a;
+};
+template <>
+struct RawEight<false> {
+    rows_f32x4 a, b;
+};
+
+template <bool BF16>
+__device__ __forceinline__ RawEight<BF16> load_raw(const char *p, size_t element)
+{
+    RawEight<BF16> r;
+    if constexpr (BF16) {
+        r.a = __builtin_nontemporal_load((const rows_bf16x8 *)(p + element * 2));
+    } else {
+        r.a = __builtin_nontemporal_load((const rows_f32x4 *)(p + element * 4));
+        r.b = __builtin_nontemporal_load((const rows_f32x4 *)(p + element * 4 + 16));
+    }
+    return r;
+}
+
+template <bool BF16>
+__device__ __forceinline__ Eight wide(const RawEight<BF16> &r)
+{
+    Eight e;
+#pragma unroll
+    for (int i = 0; i < kEight; ++i) {
+        if constexpr (BF16) e.v[i] = (float)r.a[i];
+        else e.v[i] = i < 4 ? r.a[i & 3] : r.b[i & 3];
+    }
+    return e;
+}
+
+// eight parameters that every row uses again (cached): bf16 or fp32 by a value that is the same for the whole launch
+__device__ __forceinline__ Eight load_shared(const char *p, bool bf16, size_t element)
+{
+    Eight e;
+    if (bf16) {
+        const rows_bf16x8 a = *(const rows_bf16x8 *)(p + element * 2);
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) e.v[i] = (float)a[i];
+    } else {
+        const rows_f32x4 a = *(const rows_f32x4 *)(p + element * 4), b = *(const rows_f32x4 *)(p + element * 4 + 16);
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) e.v[i] = i < 4 ? a[i & 3] : b[i & 3];
+    }
+    return e;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void store_eight(char *p, size_t element, const Eight &e)
+{
+    if constexpr (BF16) {
+        rows_bf16x8 a;
+#pragma unroll
+        for (int i = 0; i < kEight; ++i) a[i] = (__bf16)e.v[i];
+        __builtin_nontemporal_store(a, (rows_bf16x8 *)(p + element * 2));
+    } else {
+        rows_f32x4 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            a[i] = e.v[i];
+            b[i] = e.v[i + 4];
+        }
+        __builtin_nontemporal_store(a, (rows_f32x4 *)(p + element * 4));
+        __builtin_nontemporal_store(b, (rows_f32x4 *)(p + element * 4 + 16));
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+constexpr int kMaxWaves = 16;   // of a workgroup
+
+// Sums of n values over the workgroup, in every thread; `part` is LDS of n * kMaxWaves floats.  The same part may be used again once
+// every thread has passed another barrier.
+template <int n>
+__device__ __forceinline__ void group_sums(float (&v)[n], float *part, int waves)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = wave_sum(v[i]);
+    if (waves == 1) return;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) part[i * kMaxWaves + wave] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        float s = 0.0f;
+        for (int w = 0; w < waves; ++w) s += part[i * kMaxWaves + w];
+        v[i] = s;
+    }
+}
+
+}   // namespace
+
+#endif
