@@ -30,14 +30,31 @@ void launch_product(K kernel, int64_t tiles, int per_cu, const ProductArgs &a, h
     hipLaunchKernelGGL(kernel, dim3(kCus * sets), dim3(kTileThreads), 0, s, a);
 }
 
-// Products whose tiles are rows of one expert: the tile's height goes by the mean number of rows of an expert
+// Few rows per expert: a workgroup per tile of 16 token rows and block of weight rows; tiles that do not exist leave at once
+template <int WAVES, int STORE>
+int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
+{
+    constexpr int kF = 2, kUnits = STORE == kStoreGated ? 8 * kF : 16 * kF;
+    const int64_t blocks = (a.NA + kUnits - 1) / kUnits, spread = L->P / 16 + L->E, tiles = spread < L->P ? spread : L->P;
+    if (tiles * blocks > (int64_t)1 << 30) return FUSCO_ERR_INVALID_ARG;
+    hipLaunchKernelGGL((few_rows_kernel<kF, WAVES, STORE>), dim3((unsigned)(tiles * blocks)), dim3(WAVES * kWave), 0, s, a);
+    return launch_status();
+}
+
+// Products whose tiles are rows of one expert: the tile's height goes by the mean number of rows of an expert.  Measured, 128 experts of
+// 4096 x (2 x 1280) gated and 1280 x 4096, us, few / 64 / 128 / 256:  mean 4: 442 / 441 / - / -, 8: 482 / 453 / 531 / 591, 32: - / 488 / 535 / 601,
+// 64: - / 671 / 574 / 619, 128: - / 996 / 826 / 703.
 template <int AMODE, int STORE>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
     const int64_t mean = L->P / L->E, tiles_a = (a.NA + kTileA - 1) / kTileA;
-    if (mean >= 160) launch_product(product_kernel<AMODE, kAlongC, 256, 8, 4, STORE>, (L->P / 256 + L->E) * tiles_a, 1, a, s);
+    if constexpr (AMODE == kAlongC) {
+        // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
+        if (mean < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
+    }
+    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 8, 4, STORE>, (L->P / 256 + L->E) * tiles_a, 1, a, s);
     else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 4, 4, STORE>, (L->P / 128 + L->E) * tiles_a, 1, a, s);
-    else launch_product(product_kernel<AMODE, kAlongC, 64, 4, 2, STORE>, (L->P / 64 + L->E) * tiles_a, 1, a, s);
+    else launch_product(product_kernel<AMODE, kAlongC, 64, 4, 2, STORE>, (L->P / 64 + L->E) * tiles_a, 2, a, s);
     return launch_status();
 }
 

@@ -112,6 +112,14 @@ struct TileState {
     Operand<BMODE, BB> b;
     uint32_t a_lane, b_lane;
     int a_frag, b_frag, wave, lane;
+    int steps, turn;
+
+    // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one nothing is loaded
+    __device__ __forceinline__ int stage_of(int step) const
+    {
+        const int i = step + turn;
+        return step >= steps ? steps : i >= steps ? i - steps : i;
+    }
 };
 
 // First part of a stage: all fragments but the last group's are multiplied, the rest of the next stage is asked for, and the last
@@ -121,7 +129,7 @@ __device__ __forceinline__ void stage_first(const TileState<AMODE, BMODE, BB, FA
                                             bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
 {
     constexpr int kHalves = FA / 4, kGroups = 2 * kHalves, kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.b.stage(step + 1, nxt + kABytes, s.wave, s.lane);
+    s.b.stage(s.stage_of(step + 1), nxt + kABytes, s.wave, s.lane);
     __builtin_amdgcn_sched_barrier(0);
     if (ACTIVE) {
 #pragma unroll
@@ -149,7 +157,7 @@ __device__ __forceinline__ void stage_last(const TileState<AMODE, BMODE, BB, FA,
                                            bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
 {
     constexpr int kHalves = FA / 4, kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.a.stage(step + 2, cur, s.wave, s.lane);
+    s.a.stage(s.stage_of(step + 2), cur, s.wave, s.lane);
     __builtin_amdgcn_sched_barrier(0);
     if (ACTIVE) {
 #pragma unroll
@@ -165,12 +173,12 @@ __device__ __forceinline__ void stage_last(const TileState<AMODE, BMODE, BB, FA,
 }
 
 template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
-__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ lds0, char *__restrict__ lds1, int steps, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ lds0, char *__restrict__ lds1, f32x4 (&acc)[FA][FB])
 {
     constexpr int kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.a.stage(0, lds0, s.wave, s.lane);
-    s.b.stage(0, lds0 + kABytes, s.wave, s.lane);
-    s.a.stage(1, lds1, s.wave, s.lane);
+    s.a.stage(s.stage_of(0), lds0, s.wave, s.lane);
+    s.b.stage(s.stage_of(0), lds0 + kABytes, s.wave, s.lane);
+    s.a.stage(s.stage_of(1), lds1, s.wave, s.lane);
     __builtin_amdgcn_s_waitcnt(0x0070);
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
@@ -184,10 +192,10 @@ __device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, F
     for (int step = 0;;) {
         stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
         stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
-        if (++step >= steps) break;
+        if (++step >= s.steps) break;
         stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
         stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
-        if (++step >= steps) break;
+        if (++step >= s.steps) break;
     }
     __builtin_amdgcn_s_waitcnt(0x0070);   // nothing may still be on its way to LDS when the next tile begins
     __builtin_amdgcn_s_barrier();
@@ -302,7 +310,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         }
         const int a0 = ta * kUnitsA, b0 = tb * BB;
         const int b_left = (kByRows ? rows : p.NB) - b0, a_left = p.NA - a0;
-        int steps;
         // operand A
         if (AMODE == kAlongC) {   // forward: weight rows
             const int rows_e = kGated ? 2 * p.NA : p.NA;
@@ -341,7 +348,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 #pragma unroll
             for (int j = 0; j < Operand<BMODE, BB>::kLoads; ++j)
                 s.b.at[j] = (uint32_t)((j * (kTileThreads / 8) + tid / 8) * s.b.ld) + (((lane & 7) ^ (lane >> 3)) << 4);
-            steps = (p.C + kTileC - 1) / kTileC;
+            s.steps = (p.C + kTileC - 1) / kTileC;
         } else {
             constexpr int kChunks = BB / 8;
             s.b.ld = (int64_t)p.NB * 2;
@@ -354,7 +361,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                 const int col = ((tid & (kChunks - 1)) ^ (swz << 1)) * 8;
                 s.b.at[j] = col < b_left ? (uint32_t)(c * s.b.ld) + col * 2 : kNowhere;
             }
-            steps = (rows + kTileC - 1) / kTileC;
+            s.steps = (rows + kTileC - 1) / kTileC;
         }
 
         f32x4 acc[FA][FB];
@@ -362,9 +369,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         for (int f = 0; f < FA; ++f)
 #pragma unroll
             for (int j = 0; j < FB; ++j) acc[f][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (steps > 0) {
-            if (wb * FB * 16 < b_left) tile_sum<AMODE, BMODE, BB, FA, FB, true>(s, lds, lds + kStage, steps, acc);
-            else tile_sum<AMODE, BMODE, BB, FA, FB, false>(s, lds, lds + kStage, steps, acc);   // rows past the segment: loads and barriers only
+        // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
+        s.turn = s.steps > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.steps) : 0;
+        if (s.steps > 0) {
+            if (wb * FB * 16 < b_left) tile_sum<AMODE, BMODE, BB, FA, FB, true>(s, lds, lds + kStage, acc);
+            else tile_sum<AMODE, BMODE, BB, FA, FB, false>(s, lds, lds + kStage, acc);   // rows past the segment: loads and barriers only
         }
 
         // lane l holds, of fragment (f, j), the outputs a = 16 * f + l / 16 * 4 + 0 .. 3 of b = 16 * j + l % 16
@@ -407,6 +416,162 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                     store4(p.out, ((row0 + b) * 2 + 1) * p.NA + a0 + a, dup);
                 }
             }
+        }
+    }
+}
+
+// ---- Few rows per expert: bound by the weights, every one of which is read once for a handful of rows.
+//
+// A block is 16 * F weight rows (gated: 16 * F / 2 units with their gate and up rows) of one expert for up to 16 of its token rows.  The
+// WAVES waves of a workgroup share the summed dimension: wave v has the pieces v, v + WAVES, ... of 64 elements, and the waves' sums are
+// added up in LDS in the order of the waves.  Fragments go straight from memory to registers, a piece ahead of their use: many waves keep
+// enough bytes in flight, and deeper prefetch costs waves (measured 6.1 TB/s with one piece ahead, 5.8 with three).  One block per
+// workgroup: with two to eight neighbouring blocks, the next one's first piece under way while the sums are added up, 5.8 to 5.6 TB/s.
+// Measured, 128 experts of 4096 x (2 x 1280), 32 tokens with 8 experts each: 383 us, 6.14 TB/s of weights; a single token 36 us, 4.7 TB/s.
+template <int WAVES>
+struct FewTile {
+    int e, first, rows;
+
+    // Which rows of which expert: the tiles of 16 rows of all experts lie one after the other.  False if there are fewer tiles.
+    __device__ __forceinline__ bool find(const int32_t *__restrict__ exp_off, int E, int tile, int *__restrict__ part)
+    {
+        // every thread counts the tiles of a few neighbouring experts; the one whose range holds `tile` says so
+        constexpr int kThreads = WAVES * kWave, kEach = FUSCO_MAX_E / kThreads;
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        int at[kEach + 1];
+#pragma unroll
+        for (int i = 0; i <= kEach; ++i) {
+            const int x = tid * kEach + i;
+            at[i] = exp_off[x < E ? x : E];
+        }
+        int own = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) own += (at[i + 1] - at[i] + 15) / 16;
+        int sum = own;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        if (lane == 63) part[wave] = sum;
+        if (tid == 0) part[WAVES] = -1;
+        __syncthreads();
+        int before = sum - own;
+        for (int w = 0; w < wave; ++w) before += part[w];
+        if (tile >= before && tile < before + own) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int n = (at[i + 1] - at[i] + 15) / 16;
+                if (tile >= before && tile < before + n) {
+                    part[WAVES] = tid * kEach + i;
+                    part[WAVES + 1] = at[i] + (tile - before) * 16;
+                    part[WAVES + 2] = at[i + 1];
+                }
+                before += n;
+            }
+        }
+        __syncthreads();
+        e = __builtin_amdgcn_readfirstlane(part[WAVES]);
+        first = __builtin_amdgcn_readfirstlane(part[WAVES + 1]);
+        rows = __builtin_amdgcn_readfirstlane(part[WAVES + 2]) - first;
+        rows = rows < 16 ? rows : 16;
+        return e >= 0;
+    }
+};
+
+__device__ __forceinline__ bf16x8 load_fragment(__amdgpu_buffer_rsrc_t from, uint32_t offset)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(bf16x8, (words)__builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0));
+}
+
+template <int F, int WAVES, int STORE>
+__global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
+{
+    constexpr bool kGated = STORE == kStoreGated;
+    constexpr int kUnits = kGated ? 8 * F : 16 * F;       // outputs along a of a block
+    constexpr int kOut = kGated ? F / 2 : F;
+    __shared__ int part[WAVES + 3];
+    __shared__ f32x4 sums[WAVES][F][kWave];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int blocks = (p.NA + kUnits - 1) / kUnits;
+    const int tile = blockIdx.x / blocks, block = blockIdx.x - tile * blocks, a0 = block * kUnits;
+    FewTile<WAVES> at;
+    if (!at.find(p.exp_off, p.E, tile, part)) return;
+
+    const int64_t ld = (int64_t)p.C * 2;
+    const int rows_e = kGated ? 2 * p.NA : p.NA;
+    const int pieces = (p.C + kTileC - 1) / kTileC, mine = (pieces - wave + WAVES - 1) / WAVES;
+    const __amdgpu_buffer_rsrc_t vx = view(p.rows + at.first * ld, at.rows * ld);
+    const uint32_t in_row = (lane >> 4) * 16, x_at = (uint32_t)((lane & 15) * ld) + in_row;
+    const __amdgpu_buffer_rsrc_t vw = view(p.other + ((int64_t)at.e * rows_e + a0) * ld, (rows_e - a0) * ld);
+    uint32_t w_at[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+        const int unit = (kGated ? f % kOut : f) * 16 + (lane & 15);
+        w_at[f] = a0 + unit < p.NA ? (uint32_t)((unit + (kGated && f >= kOut ? p.NA : 0)) * ld) + in_row : kNowhere;
+    }
+    // Blocks begin at different pieces: rows whose size is a multiple of a large power of two lie on the same memory channels piece by
+    // piece (rows of 8 KiB: 6.1 TB/s, 5.0 without).  The order of a sum depends on the weights' place alone, not on the batch.
+    const int turn = mine > 0 ? (int)(((uint32_t)(block + at.e * blocks) * 2654435761u >> 12) % (uint32_t)mine) : 0;
+    bf16x8 w[F][2], x[2];
+    auto load = [&](int i) {
+        int j = i + turn;
+        j = j >= mine ? j - mine : j;
+        const int c0 = (wave + j * WAVES) * kTileC;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const int c = c0 + ks * 32;
+            const bool in = i < mine && c + (lane >> 4) * 8 < p.C;   // past the end: zeros, and no traffic
+#pragma unroll
+            for (int f = 0; f < F; ++f) w[f][ks] = load_fragment(vw, in ? w_at[f] + c * 2 : kNowhere);
+            x[ks] = load_fragment(vx, in ? x_at + c * 2 : kNowhere);
+        }
+    };
+    load(0);
+    f32x4 acc[F];
+#pragma unroll
+    for (int f = 0; f < F; ++f) acc[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < mine; ++i) {
+        bf16x8 wn[F][2], xn[2];
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) wn[f][ks] = w[f][ks];
+            xn[ks] = x[ks];
+        }
+        if (i + 1 < mine) load(i + 1);
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+            for (int f = 0; f < F; ++f) acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wn[f][ks], xn[ks], acc[f], 0, 0, 0);
+    }
+#pragma unroll
+    for (int f = 0; f < F; ++f) sums[wave][f][lane] = acc[f];
+    __syncthreads();
+    for (int f = wave; f < kOut; f += WAVES) {
+        const int b = lane & 15, a = a0 + f * 16 + (lane >> 4) * 4;
+        f32x4 v = sums[0][f][lane], up = v;
+#pragma unroll
+        for (int s = 1; s < WAVES; ++s) v += sums[s][f][lane];
+        if (kGated) {
+            up = sums[0][f + kOut][lane];
+#pragma unroll
+            for (int s = 1; s < WAVES; ++s) up += sums[s][f + kOut][lane];
+        }
+        if (b >= at.rows || a >= p.NA) continue;
+        const int64_t row = (int64_t)at.first + b;
+        if (kGated) {
+            f32x4 h;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) h[q] = silu(v[q]) * up[q];
+            store4(p.out, row * p.NA + a, h);
+            if (p.pre) {
+                store4(p.pre, row * 2 * p.NA + a, v);
+                store4(p.pre, (row * 2 + 1) * p.NA + a, up);
+            }
+        } else {
+            store4(p.out, row * p.NA + a, v);
         }
     }
 }
