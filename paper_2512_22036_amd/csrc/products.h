@@ -19,7 +19,7 @@ typedef __attribute__((address_space(3))) char lds_byte;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int kCus = 256;              // compute units of an MI355X
-constexpr int kTileC = 64;             // elements of the summed dimension per stage
+constexpr int kTileC = 32;             // elements of the summed dimension per stage
 constexpr int kTileThreads = 512;
 constexpr int kTileA = 256;
 constexpr uint32_t kNowhere = 0x7f000000u;   // byte offset past every buffer: such a load gives zeros
@@ -46,59 +46,58 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t view(const char *p, int64_t by
 }
 
 // 16 bytes per lane straight to LDS: the wave's 64 chunks lie behind one another from `to` on
-__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *__restrict__ to, uint32_t offset, int uniform)
+__device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, uint32_t offset, int uniform)
 {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 16, (int)offset, uniform, 0, 0);
 }
 
 // One operand of a tile: where a stage of it comes from and how it lies in LDS.
-//   kAlongC: LDS rows of 64 elements (128 bytes), the 16-byte chunk q of row r at place q ^ (r & 7): eight lanes that read the same chunk of
-//            eight rows hit all banks.
+//   kAlongC: LDS rows of 32 elements (64 bytes), the 16-byte chunk q of row r at place q ^ (r >> 1 & 3): eight lanes that read the same chunk
+//            of eight rows hit all banks.
 //   kAcross: LDS rows of W elements, one per c; pairs of chunks (16 elements) of row c at place pair ^ f(c), f(c) = (c & 3) + 4 * bit 3 of c:
 //            the transposing read takes 32 bytes of each of the rows c .. c + 3 and c + 8 .. c + 11 at once.
 template <int MODE, int W>
 struct Operand {
-    static constexpr int kLoads = W * kTileC * 2 / 16 / kTileThreads;   // loads per thread and stage
     static constexpr int kBytes = W * kTileC * 2;
+    static constexpr int kChunks = kBytes / 16, kLoads = (kChunks + kTileThreads - 1) / kTileThreads;   // loads per thread and stage
+    static constexpr int kLoadWaves = kChunks < kTileThreads ? kChunks / kWave : kTileThreads / kWave;  // waves that take part in a load
     const char *base;
     int64_t ld;            // bytes from row to row
     int64_t limit;         // kAlongC: readable bytes from base; kAcross: bytes that are missing from a whole last row
     int32_t c_size;        // elements (kAlongC) or rows (kAcross) of the summed dimension
     uint32_t at[kLoads];   // this thread's byte offsets
 
-    __device__ __forceinline__ void stage(int step, char *__restrict__ lds, int wave, int lane) const
+    __device__ __forceinline__ void load(int stage, int i, char *lds, int wave, int lane) const
     {
+        if (kLoadWaves < kTileThreads / kWave && wave >= kLoadWaves) return;
         if (MODE == kAlongC) {
-            const __amdgpu_buffer_rsrc_t v = view(base, limit);
-            const int chunk = (lane & 7) ^ (lane >> 3);
-            const bool in = step * kTileC + chunk * 8 < c_size;
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                to_lds(v, lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, step * kTileC * 2);
+            const bool in = stage * kTileC + chunk_of(lane) * 8 < c_size;
+            to_lds(view(base, limit), lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, stage * kTileC * 2);
         } else {
-            int left = c_size - step * kTileC;
-            left = left > kTileC ? kTileC : left;
-            const __amdgpu_buffer_rsrc_t v = view(base + (int64_t)step * kTileC * ld, left > 0 ? left * ld - limit : 0);
-#pragma unroll
-            for (int i = 0; i < kLoads; ++i)
-                to_lds(v, lds + (i * kTileThreads + wave * kWave) * 16, at[i], 0);
+            const int left = min(max(c_size - stage * kTileC, 0), kTileC);
+            const int bytes = __builtin_amdgcn_readfirstlane(max(left * (int)ld - (int)limit, 0));
+            to_lds(__builtin_amdgcn_make_buffer_rsrc((void *)(base + (int64_t)stage * (int64_t)(kTileC * (int)ld)), 0, bytes, 0x00020000),
+                   lds + (i * kTileThreads + wave * kWave) * 16, at[i], 0);
         }
     }
 
-    // byte offset of this lane's part of fragment 0, first half of a stage
+    // kAlongC: the chunk of its row that this lane loads; a row is loaded by four lanes
+    static __device__ __forceinline__ int chunk_of(int lane) { return (lane & 3) ^ (lane >> 3 & 3); }
+
+    // byte offset of this lane's part of fragment 0
     static __device__ __forceinline__ uint32_t lane_at(int lane)
     {
-        if (MODE == kAlongC) return (lane & 15) * (kTileC * 2) + (((lane >> 4) ^ (lane & 7)) << 4);
+        if (MODE == kAlongC) return (lane & 15) * (kTileC * 2) + (((lane >> 4) ^ (lane >> 1 & 3)) << 4);
         const int g = lane >> 4, i = lane & 15;
         return (g * 8 + (i >> 2)) * (W * 2) + ((i & 3) >> 1) * 16 + (i & 1) * 8;
     }
 
-    // fragment f (16 outputs) of half `ks` (32 elements of the summed dimension): element j of lane l is (f * 16 + l % 16, ks * 32 + l / 16 * 8 + j)
-    static __device__ __forceinline__ bf16x8 fragment(const char *__restrict__ lds, uint32_t lane_off, int lane, int f, int ks)
+    // fragment f (16 outputs): element j of lane l is (f * 16 + l % 16, l / 16 * 8 + j)
+    static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t lane_off, int lane, int f)
     {
-        if (MODE == kAlongC) return *(const bf16x8 *)(lds + (lane_off ^ (ks * 64)) + f * 16 * kTileC * 2);
+        if (MODE == kAlongC) return *(const bf16x8 *)(lds + lane_off + f * 16 * kTileC * 2);
         const int swz = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
-        const char *p = lds + lane_off + ((f ^ swz) << 5) + ks * 32 * W * 2;
+        const char *p = lds + lane_off + ((f ^ swz) << 5);
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 4 * W * 2));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -106,96 +105,125 @@ struct Operand {
 };
 
 // Everything a wave keeps over a tile
+constexpr int kSlots = 4;              // stages in LDS: one is multiplied while three are on their way
 template <int AMODE, int BMODE, int BB, int FA, int FB>
 struct TileState {
-    Operand<AMODE, kTileA> a;
-    Operand<BMODE, BB> b;
+    typedef Operand<AMODE, kTileA> A;
+    typedef Operand<BMODE, BB> B;
+    static constexpr int kStageBytes = A::kBytes + B::kBytes;
+    A a;
+    B b;
     uint32_t a_lane, b_lane;
     int a_frag, b_frag, wave, lane;
-    int steps, turn;
+    int stages, turn;
 
-    // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one nothing is loaded
-    __device__ __forceinline__ int stage_of(int step) const
+    // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one loads fetch nothing, but they are made, so that
+    // the number of loads behind a stage is always the same
+    __device__ __forceinline__ int stage_of(int s) const
     {
-        const int i = step + turn;
-        return step >= steps ? steps : i >= steps ? i - steps : i;
+        const int i = s + turn;
+        return s >= stages ? stages : i >= stages ? i - stages : i;
+    }
+    __device__ __forceinline__ void load(int s, int i, char *slot) const
+    {
+        const int at = stage_of(s);
+        if (i < A::kLoads) a.load(at, i, slot, wave, lane);
+        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, lane);
+    }
+    // waits until at most the loads of `behind` stages are on their way and nothing is being read from LDS
+    template <int behind>
+    __device__ __forceinline__ void wait() const
+    {
+        constexpr int kAll = (A::kLoads + B::kLoads) * behind, kSome = A::kLoads * behind;
+        if (B::kLoadWaves == kTileThreads / kWave || wave < B::kLoadWaves) __builtin_amdgcn_s_waitcnt((kAll & 15) | (kAll >> 4) << 14 | 0x70);
+        else __builtin_amdgcn_s_waitcnt((kSome & 15) | (kSome >> 4) << 14 | 0x70);
     }
 };
 
-// First part of a stage: all fragments but the last group's are multiplied, the rest of the next stage is asked for, and the last
-// group's fragments are read.  Ends with the barrier after which the stage's LDS is free and the next stage's is whole.
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
-__device__ __forceinline__ void stage_first(const TileState<AMODE, BMODE, BB, FA, FB> &s, const char *__restrict__ cur, char *__restrict__ nxt, int step,
-                                            bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+// One stage has two parts.  First all of `cur`'s fragments but those of the last group (four fragments along a) are multiplied, while the last
+// group's are read; then comes the barrier behind which `cur` is free and `nxt` is whole, and the last group is multiplied while nxt's
+// first fragments are read and the stage that will take cur's place is asked for.  PAR: parity of the stage, for registers that change places.
+template <int PAR, bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
+__device__ __forceinline__ void tile_first(const TileState<AMODE, BMODE, BB, FA, FB> &t, const char *cur, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
 {
-    constexpr int kHalves = FA / 4, kGroups = 2 * kHalves, kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.b.stage(s.stage_of(step + 1), nxt + kABytes, s.wave, s.lane);
-    __builtin_amdgcn_sched_barrier(0);
-    if (ACTIVE) {
+    if (!ACTIVE || FA == 4) return;
 #pragma unroll
-        for (int g = 0; g < kGroups - 1; ++g) {
-            const int ks = g / kHalves, ks1 = (g + 1) / kHalves, h = g % kHalves, h1 = (g + 1) % kHalves;
+    for (int i = 0; i < 4; ++i) {
+        a[1][i] = t.a.fragment(cur, t.a_lane, t.lane, t.a_frag + 4 + i);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (ks1 != ks && i < FB) b[ks1][i] = s.b.fragment(cur + kABytes, s.b_lane, s.lane, s.b_frag + i, ks1);
-                a[(g + 1) & 1][i] = s.a.fragment(cur, s.a_lane, s.lane, s.a_frag + h1 * 4 + i, ks1);
-#pragma unroll
-                for (int j = 0; j < FB; ++j)
-                    acc[h * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[g & 1][i], b[ks][j], acc[h * 4 + i][j], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        }
+        for (int j = 0; j < FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0][i], b[PAR][j], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0): the next stage has arrived, nothing of this one is still being read
+}
+
+template <int PAR, bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
+__device__ __forceinline__ void tile_last(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *cur, const char *nxt, int s, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+{
+    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
+    constexpr int kLast = FA == 8 ? 1 : PAR, kNext = FA == 8 ? 0 : 1 - PAR, kRow = FA - 4;   // which a[], which rows of acc
+    t.template wait<kSlots - 2>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-}
-
-// Last part: the last group is multiplied while the next stage's first fragments are read and the stage after it is asked for
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
-__device__ __forceinline__ void stage_last(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ cur, const char *__restrict__ nxt, int step,
-                                           bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
-{
-    constexpr int kHalves = FA / 4, kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.a.stage(s.stage_of(step + 2), cur, s.wave, s.lane);
-    __builtin_amdgcn_sched_barrier(0);
-    if (ACTIVE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < FB) b[0][i] = s.b.fragment(nxt + kABytes, s.b_lane, s.lane, s.b_frag + i, 0);
-            a[0][i] = s.a.fragment(nxt, s.a_lane, s.lane, s.a_frag + i, 0);
+    for (int i = 0; i < 4; ++i) {
+        t.load(s + kSlots, i, cur);
+        if (ACTIVE) {
+            if (i < FB) b[1 - PAR][i] = t.b.fragment(nxt + kABytes, t.b_lane, t.lane, t.b_frag + i);
+            a[kNext][i] = t.a.fragment(nxt, t.a_lane, t.lane, t.a_frag + i);
 #pragma unroll
-            for (int j = 0; j < FB; ++j)
-                acc[(kHalves - 1) * 4 + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[1][i], b[1][j], acc[(kHalves - 1) * 4 + i][j], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int j = 0; j < FB; ++j) acc[kRow + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[kLast][i], b[PAR][j], acc[kRow + i][j], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool ACTIVE>
-__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &s, char *__restrict__ lds0, char *__restrict__ lds1, f32x4 (&acc)[FA][FB])
+// The slots are arrays of their own: the compiler then knows that a fragment's read waits for its own slot's loads only.
+template <bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
+__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x4 (&acc)[FA][FB])
 {
-    constexpr int kABytes = Operand<AMODE, kTileA>::kBytes;
-    s.a.stage(s.stage_of(0), lds0, s.wave, s.lane);
-    s.b.stage(s.stage_of(0), lds0 + kABytes, s.wave, s.lane);
-    s.a.stage(s.stage_of(1), lds1, s.wave, s.lane);
-    __builtin_amdgcn_s_waitcnt(0x0070);
+    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t.load(0, i, slot0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t.load(1, i, slot1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t.load(2, i, slot2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) t.load(3, i, slot3);
+    t.template wait<kSlots - 1>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 a[2][4], b[2][FB];
     if (ACTIVE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[0][i] = s.a.fragment(lds0, s.a_lane, s.lane, s.a_frag + i, 0);
+        for (int i = 0; i < 4; ++i) a[0][i] = t.a.fragment(slot0, t.a_lane, t.lane, t.a_frag + i);
 #pragma unroll
-        for (int j = 0; j < FB; ++j) b[0][j] = s.b.fragment(lds0 + kABytes, s.b_lane, s.lane, s.b_frag + j, 0);
+        for (int j = 0; j < FB; ++j) b[0][j] = t.b.fragment(slot0 + kABytes, t.b_lane, t.lane, t.b_frag + j);
     }
-    for (int step = 0;;) {
-        stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
-        stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds0, lds1, step, a, b, acc);
-        if (++step >= s.steps) break;
-        stage_first<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
-        stage_last<AMODE, BMODE, BB, FA, FB, ACTIVE>(s, lds1, lds0, step, a, b, acc);
-        if (++step >= s.steps) break;
+    // Whole turns through the slots, then what is left: a loop with one way out, since at the head of one with several the compiler would
+    // take loads of the present turn to be still under way.
+    int s = 0;
+    for (const int whole = t.stages & ~(kSlots - 1); s < whole; s += kSlots) {
+        tile_first<0, ACTIVE>(t, slot0, a, b, acc);
+        tile_last<0, ACTIVE>(t, slot0, slot1, s, a, b, acc);
+        tile_first<1, ACTIVE>(t, slot1, a, b, acc);
+        tile_last<1, ACTIVE>(t, slot1, slot2, s + 1, a, b, acc);
+        tile_first<0, ACTIVE>(t, slot2, a, b, acc);
+        tile_last<0, ACTIVE>(t, slot2, slot3, s + 2, a, b, acc);
+        tile_first<1, ACTIVE>(t, slot3, a, b, acc);
+        tile_last<1, ACTIVE>(t, slot3, slot0, s + 3, a, b, acc);
+    }
+    if (s < t.stages) {
+        tile_first<0, ACTIVE>(t, slot0, a, b, acc);
+        tile_last<0, ACTIVE>(t, slot0, slot1, s, a, b, acc);
+        if (s + 1 < t.stages) {
+            tile_first<1, ACTIVE>(t, slot1, a, b, acc);
+            tile_last<1, ACTIVE>(t, slot1, slot2, s + 1, a, b, acc);
+            if (s + 2 < t.stages) {
+                tile_first<0, ACTIVE>(t, slot2, a, b, acc);
+                tile_last<0, ACTIVE>(t, slot2, slot3, s + 2, a, b, acc);
+            }
+        }
     }
     __builtin_amdgcn_s_waitcnt(0x0070);   // nothing may still be on its way to LDS when the next tile begins
     __builtin_amdgcn_s_barrier();
@@ -246,20 +274,25 @@ __device__ __forceinline__ int tile_in_list(int i)
 
 // FA x FB fragments of 16 x 16 outputs per wave, kTileA / (16 * FA) waves along a
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
-__global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
+__global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel(ProductArgs p)
 {
-    constexpr int kStage = Operand<AMODE, kTileA>::kBytes + Operand<BMODE, BB>::kBytes;
+    typedef TileState<AMODE, BMODE, BB, FA, FB> State;
     constexpr int kWavesA = kTileA / (16 * FA), kWavesB = BB / (16 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
     constexpr bool kGated = STORE == kStoreGated;
     constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(FA % 4 == 0 && FB <= 4, "groups of four fragments along a");
-    __shared__ __align__(1024) char lds[2 * kStage];
+    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[State::kStageBytes], slot3[State::kStageBytes];
     __shared__ int prefix[FUSCO_MAX_E + 1];
     __shared__ int part[kTileThreads / kWave];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63;
+    // Where a slot is written and read from is hidden from the compiler: as long as it cannot tell one place in a slot from another, it lets
+    // reads wait for the loads to their slot; where it could, it would let them wait for all loads.
+    int hidden = tid >> 6;
+    asm volatile("" : "+v"(hidden));
+    const int wave = __builtin_amdgcn_readfirstlane(hidden);
     const int wa = wave % kWavesA, wb = wave / kWavesA;
     const int tiles_a = (p.NA + kUnitsA - 1) / kUnitsA;
     const int tiles_b = kByRows ? 0 : (p.NB + BB - 1) / BB;
@@ -271,11 +304,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         total = p.E * tiles_a * tiles_b;
     }
 
-    TileState<AMODE, BMODE, BB, FA, FB> s;
+    State s;
     s.wave = wave;
     s.lane = lane;
-    s.a_lane = Operand<AMODE, kTileA>::lane_at(lane);
-    s.b_lane = Operand<BMODE, BB>::lane_at(lane);
+    s.a_lane = State::A::lane_at(lane);
+    s.b_lane = State::B::lane_at(lane);
+    asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
     s.a_frag = wa * FA;
     s.b_frag = wb * FB;
 
@@ -318,14 +352,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.a.limit = (rows_e - a0) * s.a.ld;
             s.a.c_size = p.C;
 #pragma unroll
-            for (int j = 0; j < Operand<AMODE, kTileA>::kLoads; ++j) {
-                const int r = j * (kTileThreads / 8) + tid / 8;
+            for (int j = 0; j < State::A::kLoads; ++j) {
+                const int r = j * (kTileThreads / 4) + tid / 4;
                 int unit = r, up = 0;
                 if (kGated) {   // a wave's rows: FA * 8 gate rows, then the up rows of the same units
                     unit = r / (16 * FA) * (8 * FA) + r % (8 * FA);
                     up = r / (8 * FA) % 2;
                 }
-                s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (((lane & 7) ^ (lane >> 3)) << 4) : kNowhere;
+                s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (State::A::chunk_of(lane) << 4) : kNowhere;
             }
         } else {
             s.a.ld = (int64_t)p.NA * 2;
@@ -333,7 +367,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.a.c_size = kByRows ? p.C : rows;
             s.a.base = (kByRows ? p.other + (int64_t)e * p.C * s.a.ld : p.rows + first * s.a.ld) + s.a.limit;
 #pragma unroll
-            for (int j = 0; j < Operand<AMODE, kTileA>::kLoads; ++j) {
+            for (int j = 0; j < State::A::kLoads; ++j) {
                 const int c = j * (kTileThreads / 32) + tid / 32, swz = (c & 3) | ((c >> 3 & 1) << 2);
                 const int col = ((tid & 31) ^ (swz << 1)) * 8;
                 s.a.at[j] = col < a_left ? (uint32_t)(c * s.a.ld) + col * 2 : kNowhere;
@@ -346,9 +380,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.b.limit = (b_left < BB ? b_left : BB) * s.b.ld;
             s.b.c_size = p.C;
 #pragma unroll
-            for (int j = 0; j < Operand<BMODE, BB>::kLoads; ++j)
-                s.b.at[j] = (uint32_t)((j * (kTileThreads / 8) + tid / 8) * s.b.ld) + (((lane & 7) ^ (lane >> 3)) << 4);
-            s.steps = (p.C + kTileC - 1) / kTileC;
+            for (int j = 0; j < State::B::kLoads; ++j)
+                s.b.at[j] = (uint32_t)((j * (kTileThreads / 4) + tid / 4) * s.b.ld) + (State::A::chunk_of(lane) << 4);
+            s.stages = (p.C + kTileC - 1) / kTileC;
         } else {
             constexpr int kChunks = BB / 8;
             s.b.ld = (int64_t)p.NB * 2;
@@ -356,12 +390,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.b.base = p.other + first * s.b.ld + s.b.limit;
             s.b.c_size = rows;
 #pragma unroll
-            for (int j = 0; j < Operand<BMODE, BB>::kLoads; ++j) {
+            for (int j = 0; j < State::B::kLoads; ++j) {
                 const int c = j * (kTileThreads / kChunks) + tid / kChunks, swz = (c & 3) | ((c >> 3 & 1) << 2);
                 const int col = ((tid & (kChunks - 1)) ^ (swz << 1)) * 8;
                 s.b.at[j] = col < b_left ? (uint32_t)(c * s.b.ld) + col * 2 : kNowhere;
             }
-            s.steps = (rows + kTileC - 1) / kTileC;
+            s.stages = (rows + kTileC - 1) / kTileC;
         }
 
         f32x4 acc[FA][FB];
@@ -370,10 +404,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 #pragma unroll
             for (int j = 0; j < FB; ++j) acc[f][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
-        s.turn = s.steps > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.steps) : 0;
-        if (s.steps > 0) {
-            if (wb * FB * 16 < b_left) tile_sum<AMODE, BMODE, BB, FA, FB, true>(s, lds, lds + kStage, acc);
-            else tile_sum<AMODE, BMODE, BB, FA, FB, false>(s, lds, lds + kStage, acc);   // rows past the segment: loads and barriers only
+        s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
+        if (s.stages > 0) {
+            if (wb * FB * 16 < b_left) tile_sum<true>(s, slot0, slot1, slot2, slot3, acc);
+            else tile_sum<false>(s, slot0, slot1, slot2, slot3, acc);   // rows past the segment: loads and barriers only
         }
 
         // lane l holds, of fragment (f, j), the outputs a = 16 * f + l / 16 * 4 + 0 .. 3 of b = 16 * j + l % 16
@@ -428,6 +462,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 // enough bytes in flight, and deeper prefetch costs waves (measured 6.1 TB/s with one piece ahead, 5.8 with three).  One block per
 // workgroup: with two to eight neighbouring blocks, the next one's first piece under way while the sums are added up, 5.8 to 5.6 TB/s.
 // Measured, 128 experts of 4096 x (2 x 1280), 32 tokens with 8 experts each: 383 us, 6.14 TB/s of weights; a single token 36 us, 4.7 TB/s.
+constexpr int kPiece = 64;   // elements
+
 template <int WAVES>
 struct FewTile {
     int e, first, rows;
@@ -501,7 +537,7 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
 
     const int64_t ld = (int64_t)p.C * 2;
     const int rows_e = kGated ? 2 * p.NA : p.NA;
-    const int pieces = (p.C + kTileC - 1) / kTileC, mine = (pieces - wave + WAVES - 1) / WAVES;
+    const int pieces = (p.C + kPiece - 1) / kPiece, mine = (pieces - wave + WAVES - 1) / WAVES;
     const __amdgpu_buffer_rsrc_t vx = view(p.rows + at.first * ld, at.rows * ld);
     const uint32_t in_row = (lane >> 4) * 16, x_at = (uint32_t)((lane & 15) * ld) + in_row;
     const __amdgpu_buffer_rsrc_t vw = view(p.other + ((int64_t)at.e * rows_e + a0) * ld, (rows_e - a0) * ld);
@@ -518,7 +554,7 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
     auto load = [&](int i) {
         int j = i + turn;
         j = j >= mine ? j - mine : j;
-        const int c0 = (wave + j * WAVES) * kTileC;
+        const int c0 = (wave + j * WAVES) * kPiece;
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             const int c = c0 + ks * 32;
