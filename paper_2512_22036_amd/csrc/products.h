@@ -56,7 +56,9 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, ui
 //            of eight rows hit all banks.
 //   kAcross: LDS rows of W elements, one per c; pairs of chunks (16 elements) of row c at place pair ^ f(c), f(c) = (c & 3) + 4 * bit 3 of c:
 //            the transposing read takes 32 bytes of each of the rows c .. c + 3 and c + 8 .. c + 11 at once.
-template <int MODE, int W>
+// PAIRED (kAlongC): the rows of fragments 2 p and 2 p + 1 are dealt out so that a lane's outputs of both are eight neighbours along a (row r of
+// fragment 2 p + h is p * 32 + r / 4 * 8 + h * 4 + r % 4); the place of a chunk follows suit: q ^ (bit 1 of r + 2 * bit 3 of r).
+template <int MODE, int W, bool PAIRED>
 struct Operand {
     static constexpr int kBytes = W * kTileC * 2;
     static constexpr int kChunks = kBytes / 16, kLoads = (kChunks + kTileThreads - 1) / kTileThreads;   // loads per thread and stage
@@ -82,22 +84,25 @@ struct Operand {
     }
 
     // kAlongC: the chunk of its row that this lane loads; a row is loaded by four lanes
-    static __device__ __forceinline__ int chunk_of(int lane) { return (lane & 3) ^ (lane >> 3 & 3); }
+    static __device__ __forceinline__ int chunk_of(int lane) { return (lane & 3) ^ swizzle(lane >> 2); }
+    static __device__ __forceinline__ int swizzle(int row) { return PAIRED ? (row >> 1 & 1) | (row >> 2 & 2) : row >> 1 & 3; }
 
-    // byte offset of this lane's part of fragment 0
-    static __device__ __forceinline__ uint32_t lane_at(int lane)
+    // byte offset of this lane's part of a wave's first fragment, `first`, a multiple of the wave's fragments (a power of two)
+    static __device__ __forceinline__ uint32_t lane_at(int lane, int first)
     {
-        if (MODE == kAlongC) return (lane & 15) * (kTileC * 2) + (((lane >> 4) ^ (lane >> 1 & 3)) << 4);
-        const int g = lane >> 4, i = lane & 15;
-        return (g * 8 + (i >> 2)) * (W * 2) + ((i & 3) >> 1) * 16 + (i & 1) * 8;
+        if (MODE == kAlongC) {
+            const int row = PAIRED ? (lane & 12) * 2 + (lane & 3) : lane & 15;
+            return (first * 16 + row) * (kTileC * 2) + (((lane >> 4) ^ swizzle(row)) << 4);
+        }
+        const int g = lane >> 4, i = lane & 15, place = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
+        return (g * 8 + (i >> 2)) * (W * 2) + ((first ^ place) << 5) + ((i & 3) >> 1) * 16 + (i & 1) * 8;
     }
 
-    // fragment f (16 outputs): element j of lane l is (f * 16 + l % 16, l / 16 * 8 + j)
-    static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t lane_off, int lane, int f)
+    // the wave's fragment f (16 outputs): element j of lane l is (row l % 16 of the fragment, l / 16 * 8 + j)
+    static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t at, int f)
     {
-        if (MODE == kAlongC) return *(const bf16x8 *)(lds + lane_off + f * 16 * kTileC * 2);
-        const int swz = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
-        const char *p = lds + lane_off + ((f ^ swz) << 5);
+        if (MODE == kAlongC) return *(const bf16x8 *)(lds + at + (PAIRED ? (f >> 1) * 32 + (f & 1) * 4 : f * 16) * kTileC * 2);
+        const char *p = lds + (at ^ (f << 5));
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 4 * W * 2));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -108,13 +113,14 @@ struct Operand {
 constexpr int kSlots = 4;              // stages in LDS: one is multiplied while three are on their way
 template <int AMODE, int BMODE, int BB, int FA, int FB>
 struct TileState {
-    typedef Operand<AMODE, kTileA> A;
-    typedef Operand<BMODE, BB> B;
+    static constexpr bool kPaired = AMODE == kAlongC;
+    typedef Operand<AMODE, kTileA, kPaired> A;
+    typedef Operand<BMODE, BB, false> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes;
     A a;
     B b;
     uint32_t a_lane, b_lane;
-    int a_frag, b_frag, wave, lane;
+    int wave, lane;
     int stages, turn;
 
     // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one loads fetch nothing, but they are made, so that
@@ -130,11 +136,12 @@ struct TileState {
         if (i < A::kLoads) a.load(at, i, slot, wave, lane);
         if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, lane);
     }
-    // waits until at most the loads of `behind` stages are on their way and nothing is being read from LDS
-    template <int behind>
+    // waits until at most the loads of `behind` stages and `more` stores are on their way and nothing is being read from LDS
+    template <int behind, int more = 0>
     __device__ __forceinline__ void wait() const
     {
-        constexpr int kAll = (A::kLoads + B::kLoads) * behind, kSome = A::kLoads * behind;
+        constexpr int kAll = (A::kLoads + B::kLoads) * behind + more, kSome = A::kLoads * behind + more;
+        static_assert(kAll < 64, "what the hardware counts");
         if (B::kLoadWaves == kTileThreads / kWave || wave < B::kLoadWaves) __builtin_amdgcn_s_waitcnt((kAll & 15) | (kAll >> 4) << 14 | 0x70);
         else __builtin_amdgcn_s_waitcnt((kSome & 15) | (kSome >> 4) << 14 | 0x70);
     }
@@ -147,29 +154,33 @@ template <int PAR, bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
 __device__ __forceinline__ void tile_first(const TileState<AMODE, BMODE, BB, FA, FB> &t, const char *cur, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
 {
     if (!ACTIVE || FA == 4) return;
+    uint32_t at = t.a_lane;
+    asm volatile("" : "+v"(at));         // fragments' places are worked out where they are used, not kept in registers over the loop
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        a[1][i] = t.a.fragment(cur, t.a_lane, t.lane, t.a_frag + 4 + i);
+        a[1][i] = t.a.fragment(cur, at, 4 + i);
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0][i], b[PAR][j], acc[i][j], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <int PAR, bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
+template <int PAR, bool ACTIVE, int STORES, int AMODE, int BMODE, int BB, int FA, int FB>
 __device__ __forceinline__ void tile_last(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *cur, const char *nxt, int s, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
 {
     constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
     constexpr int kLast = FA == 8 ? 1 : PAR, kNext = FA == 8 ? 0 : 1 - PAR, kRow = FA - 4;   // which a[], which rows of acc
-    t.template wait<kSlots - 2>();
+    t.template wait<kSlots - 2, STORES>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
+    uint32_t a_at = t.a_lane, b_at = t.b_lane;
+    asm volatile("" : "+v"(a_at), "+v"(b_at));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         t.load(s + kSlots, i, cur);
         if (ACTIVE) {
-            if (i < FB) b[1 - PAR][i] = t.b.fragment(nxt + kABytes, t.b_lane, t.lane, t.b_frag + i);
-            a[kNext][i] = t.a.fragment(nxt, t.a_lane, t.lane, t.a_frag + i);
+            if (i < FB) b[1 - PAR][i] = t.b.fragment(nxt + kABytes, b_at, i);
+            a[kNext][i] = t.a.fragment(nxt, a_at, i);
 #pragma unroll
             for (int j = 0; j < FB; ++j) acc[kRow + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[kLast][i], b[PAR][j], acc[kRow + i][j], 0, 0, 0);
         }
@@ -177,11 +188,9 @@ __device__ __forceinline__ void tile_last(const TileState<AMODE, BMODE, BB, FA, 
     }
 }
 
-// The slots are arrays of their own: the compiler then knows that a fragment's read waits for its own slot's loads only.
-template <bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
-__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x4 (&acc)[FA][FB])
+template <int AMODE, int BMODE, int BB, int FA, int FB>
+__device__ __forceinline__ void tile_begin(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3)
 {
-    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) t.load(0, i, slot0);
 #pragma unroll
@@ -190,44 +199,91 @@ __device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, F
     for (int i = 0; i < 2; ++i) t.load(2, i, slot2);
 #pragma unroll
     for (int i = 0; i < 2; ++i) t.load(3, i, slot3);
-    t.template wait<kSlots - 1>();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The sums of a tile whose first stages are under way; after them STORES stores at least were issued (the outputs of the tile before), which
+// the first three stages do not wait for.  The slots are arrays of their own: the compiler then knows that a fragment's read waits for
+// its own slot's loads only.
+template <bool ACTIVE, int STORES, int AMODE, int BMODE, int BB, int FA, int FB>
+__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x4 (&acc)[FA][FB])
+{
+    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
+    if (t.stages == 0) return;
+    t.template wait<kSlots - 1, STORES>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     bf16x8 a[2][4], b[2][FB];
     if (ACTIVE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[0][i] = t.a.fragment(slot0, t.a_lane, t.lane, t.a_frag + i);
+        for (int i = 0; i < 4; ++i) a[0][i] = t.a.fragment(slot0, t.a_lane, i);
 #pragma unroll
-        for (int j = 0; j < FB; ++j) b[0][j] = t.b.fragment(slot0 + kABytes, t.b_lane, t.lane, t.b_frag + j);
+        for (int j = 0; j < FB; ++j) b[0][j] = t.b.fragment(slot0 + kABytes, t.b_lane, j);
     }
-    // Whole turns through the slots, then what is left: a loop with one way out, since at the head of one with several the compiler would
+#define FUSCO_STAGE(n, cur, nxt, stores)                                     \
+    tile_first<(n) % 2, ACTIVE>(t, cur, a, b, acc);                          \
+    tile_last<(n) % 2, ACTIVE, stores>(t, cur, nxt, s + (n), a, b, acc)
+    // Whole turns through the slots, then what is left.  The loop has one way out: at the head of one with several the compiler would
     // take loads of the present turn to be still under way.
     int s = 0;
-    for (const int whole = t.stages & ~(kSlots - 1); s < whole; s += kSlots) {
-        tile_first<0, ACTIVE>(t, slot0, a, b, acc);
-        tile_last<0, ACTIVE>(t, slot0, slot1, s, a, b, acc);
-        tile_first<1, ACTIVE>(t, slot1, a, b, acc);
-        tile_last<1, ACTIVE>(t, slot1, slot2, s + 1, a, b, acc);
-        tile_first<0, ACTIVE>(t, slot2, a, b, acc);
-        tile_last<0, ACTIVE>(t, slot2, slot3, s + 2, a, b, acc);
-        tile_first<1, ACTIVE>(t, slot3, a, b, acc);
-        tile_last<1, ACTIVE>(t, slot3, slot0, s + 3, a, b, acc);
+    const int whole = t.stages & ~(kSlots - 1);
+    if (whole > 0) {
+        FUSCO_STAGE(0, slot0, slot1, STORES);
+        FUSCO_STAGE(1, slot1, slot2, STORES);
+        FUSCO_STAGE(2, slot2, slot3, STORES);
+        FUSCO_STAGE(3, slot3, slot0, 0);
+        s = kSlots;
+    }
+    for (; s < whole; s += kSlots) {
+        FUSCO_STAGE(0, slot0, slot1, 0);
+        FUSCO_STAGE(1, slot1, slot2, 0);
+        FUSCO_STAGE(2, slot2, slot3, 0);
+        FUSCO_STAGE(3, slot3, slot0, 0);
     }
     if (s < t.stages) {
-        tile_first<0, ACTIVE>(t, slot0, a, b, acc);
-        tile_last<0, ACTIVE>(t, slot0, slot1, s, a, b, acc);
+        FUSCO_STAGE(0, slot0, slot1, 0);
         if (s + 1 < t.stages) {
-            tile_first<1, ACTIVE>(t, slot1, a, b, acc);
-            tile_last<1, ACTIVE>(t, slot1, slot2, s + 1, a, b, acc);
+            FUSCO_STAGE(1, slot1, slot2, 0);
             if (s + 2 < t.stages) {
-                tile_first<0, ACTIVE>(t, slot2, a, b, acc);
-                tile_last<0, ACTIVE>(t, slot2, slot3, s + 2, a, b, acc);
+                FUSCO_STAGE(2, slot2, slot3, 0);
             }
         }
     }
-    __builtin_amdgcn_s_waitcnt(0x0070);   // nothing may still be on its way to LDS when the next tile begins
-    __builtin_amdgcn_s_barrier();
+#undef FUSCO_STAGE
 }
+
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+
+// Outputs of a wave: lane l has FA / 2 pairs of fragments along a and FB along b.  Stores go through a bounds-checked view, so that their
+// number is the same for every tile: what lies outside is dropped.
+struct Target {
+    __amdgpu_buffer_rsrc_t to;
+    uint32_t ld;           // bytes from row to row
+    __device__ __forceinline__ void open(char *p, int64_t row0, int64_t row_bytes, int64_t column_bytes, int rows)
+    {
+        ld = (uint32_t)row_bytes;
+        to = view(p + row0 * row_bytes + column_bytes, rows > 0 ? rows * row_bytes - column_bytes : 0);
+    }
+    __device__ __forceinline__ void put8(f32x4 lo, f32x4 hi, uint32_t offset) const
+    {
+        bf16x8 o;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            o[q] = (__bf16)lo[q];
+            o[q + 4] = (__bf16)hi[q];
+        }
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, o), to, (int)offset, 0, 0);
+    }
+    __device__ __forceinline__ void put4(f32x4 v, uint32_t offset) const
+    {
+        bf16x4 o;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(words2, o), to, (int)offset, 0, 0);
+    }
+    __device__ __forceinline__ void put_f32(f32x4 v, uint32_t offset) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, v), to, (int)offset, 0, 0); }
+};
 
 __device__ __forceinline__ void store4(char *out, int64_t element, f32x4 v)
 {
@@ -307,15 +363,17 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     State s;
     s.wave = wave;
     s.lane = lane;
-    s.a_lane = State::A::lane_at(lane);
-    s.b_lane = State::B::lane_at(lane);
+    s.a_lane = State::A::lane_at(lane, wa * FA);
+    s.b_lane = State::B::lane_at(lane, wb * FB);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
-    s.a_frag = wa * FA;
-    s.b_frag = wb * FB;
 
-    for (int i = 0;; ++i) {
-        const int t = tile_in_list(i);
-        if (t >= total) break;   // later tiles of this workgroup lie behind it
+    // the tile at hand
+    int a0 = 0, a_left = 0, b_left = 0;
+    int64_t row0 = 0;
+    auto begin = [&](int t) {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));    // as in store
+        const int lane = tid & 63;
         // which expert, which tiles
         int e, ta, tb, first, rows;
         {
@@ -342,8 +400,11 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             first = __builtin_amdgcn_readfirstlane(p.exp_off[e]);
             rows = __builtin_amdgcn_readfirstlane(p.exp_off[e + 1]) - first;
         }
-        const int a0 = ta * kUnitsA, b0 = tb * BB;
-        const int b_left = (kByRows ? rows : p.NB) - b0, a_left = p.NA - a0;
+        a0 = ta * kUnitsA;
+        const int b0 = tb * BB;
+        b_left = (kByRows ? rows : p.NB) - b0;
+        a_left = p.NA - a0;
+        row0 = kByRows ? (int64_t)first + b0 : (int64_t)e * p.NB + b0;
         // operand A
         if (AMODE == kAlongC) {   // forward: weight rows
             const int rows_e = kGated ? 2 * p.NA : p.NA;
@@ -381,7 +442,7 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             s.b.c_size = p.C;
 #pragma unroll
             for (int j = 0; j < State::B::kLoads; ++j)
-                s.b.at[j] = (uint32_t)((j * (kTileThreads / 4) + tid / 4) * s.b.ld) + (State::A::chunk_of(lane) << 4);
+                s.b.at[j] = (uint32_t)((j * (kTileThreads / 4) + tid / 4) * s.b.ld) + (State::B::chunk_of(lane) << 4);
             s.stages = (p.C + kTileC - 1) / kTileC;
         } else {
             constexpr int kChunks = BB / 8;
@@ -397,61 +458,106 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             }
             s.stages = (rows + kTileC - 1) / kTileC;
         }
+        // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
+        s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
+        tile_begin(s, slot0, slot1, slot2, slot3);
+    };
 
-        f32x4 acc[FA][FB];
+    // Lane l holds, of fragment (f, j), four neighbouring outputs along a of b = 16 * j + l % 16.
+    constexpr int kOutA = kGated ? FA / 2 : FA;
+    f32x4 acc[FA][FB];
+    auto store = [&](int a0, int a_left, int b_left, int64_t row0) {
+        constexpr int kSize = STORE == kStoreF32 ? 4 : 2;
+        const int rows = b_left < BB ? b_left : BB;
+        Target out, pre;
+        out.open(p.out, row0, (int64_t)p.NA * (STORE == kStoreGatedGrad ? 2 : 1) * kSize, (int64_t)a0 * kSize, rows);
+        if (kGated && p.pre) pre.open(p.pre, row0, (int64_t)p.NA * 2 * kSize, (int64_t)a0 * kSize, rows);
+        const uint32_t second = (uint32_t)p.NA * kSize;
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));   // places are worked out here, not kept in registers over the sums
+#pragma unroll
+        for (int j = 0; j < FB; ++j) {
+            const int b = wb * FB * 16 + j * 16 + (lane & 15);
+            if constexpr (State::kPaired) {
+#pragma unroll
+                for (int f = 0; f < kOutA; f += 2) {
+                    const int a = wa * kOutA * 16 + f * 16 + (lane >> 4) * 8;
+                    const uint32_t at = a < a_left && b < b_left ? b * out.ld + a * kSize : kNowhere;
+                    f32x4 lo = acc[f][j], hi = acc[f + 1][j];
+                    if (kGated) {
+                        const f32x4 up_lo = acc[f + FA / 2][j], up_hi = acc[f + 1 + FA / 2][j];
+                        if (p.pre) {
+                            const uint32_t to = a < a_left && b < b_left ? b * pre.ld + a * kSize : kNowhere;
+                            pre.put8(lo, hi, to);
+                            pre.put8(up_lo, up_hi, to + second);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            lo[q] = silu(lo[q]) * up_lo[q];
+                            hi[q] = silu(hi[q]) * up_hi[q];
+                        }
+                    }
+                    out.put8(lo, hi, at);
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < kOutA; ++f) {
+                    const int a = wa * kOutA * 16 + f * 16 + (lane >> 4) * 4;
+                    const bool in = a < a_left && b < b_left;
+                    const uint32_t at = in ? b * out.ld + a * kSize : kNowhere;
+                    const f32x4 v = acc[f][j];
+                    if (STORE == kStoreF32) {
+                        out.put_f32(v, at);
+                    } else if (STORE == kStoreBf16) {
+                        out.put4(v, at);
+                    } else {
+                        bf16x4 gate, up;
+                        if (in) {
+                            gate = *(const bf16x4 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
+                            up = *(const bf16x4 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
+                        }
+                        f32x4 dgate, dup;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float g = (float)gate[q], sig = 1.0f / (1.0f + __expf(-g));
+                            dup[q] = v[q] * g * sig;
+                            dgate[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
+                        }
+                        out.put4(dgate, at);
+                        out.put4(dup, at + second);
+                    }
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto clear = [&] {
 #pragma unroll
         for (int f = 0; f < FA; ++f)
 #pragma unroll
             for (int j = 0; j < FB; ++j) acc[f][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
-        s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
-        if (s.stages > 0) {
-            if (wb * FB * 16 < b_left) tile_sum<true>(s, slot0, slot1, slot2, slot3, acc);
-            else tile_sum<false>(s, slot0, slot1, slot2, slot3, acc);   // rows past the segment: loads and barriers only
-        }
+    };
+    // stores of one tile and wave; the activation's gradient waits for loads in between and counts as none
+    constexpr int kStores = STORE == kStoreGatedGrad ? 0 : State::kPaired ? FB * kOutA / 2 : FB * kOutA;
 
-        // lane l holds, of fragment (f, j), the outputs a = 16 * f + l / 16 * 4 + 0 .. 3 of b = 16 * j + l % 16
-        const int a_lane = wa * (kGated ? FA / 2 : FA) * 16 + (lane >> 4) * 4, b_lane = wb * FB * 16 + (lane & 15);
-        const int64_t row0 = kByRows ? (int64_t)first + b0 : (int64_t)e * p.NB + b0;
-#pragma unroll
-        for (int j = 0; j < FB; ++j) {
-            const int b = b_lane + j * 16;
-            if (b >= b_left) continue;
-#pragma unroll
-            for (int f = 0; f < (kGated ? FA / 2 : FA); ++f) {
-                const int a = a_lane + f * 16;
-                if (a >= a_left) continue;
-                const f32x4 v = acc[f][j];
-                if (STORE == kStoreBf16) {
-                    store4(p.out, (row0 + b) * p.NA + a0 + a, v);
-                } else if (STORE == kStoreF32) {
-                    *(f32x4 *)(p.out + ((row0 + b) * p.NA + a0 + a) * 4) = v;
-                } else if (STORE == kStoreGated) {
-                    const f32x4 up = acc[f + FA / 2][j];
-                    f32x4 h;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) h[q] = silu(v[q]) * up[q];
-                    store4(p.out, (row0 + b) * p.NA + a0 + a, h);
-                    if (p.pre) {
-                        store4(p.pre, (row0 + b) * 2 * p.NA + a0 + a, v);
-                        store4(p.pre, ((row0 + b) * 2 + 1) * p.NA + a0 + a, up);
-                    }
-                } else {
-                    const bf16x4 gate = *(const bf16x4 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
-                    const bf16x4 up = *(const bf16x4 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
-                    f32x4 dgate, dup;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float g = (float)gate[q], sig = 1.0f / (1.0f + __expf(-g));
-                        dup[q] = v[q] * g * sig;
-                        dgate[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
-                    }
-                    store4(p.out, (row0 + b) * 2 * p.NA + a0 + a, dgate);
-                    store4(p.out, ((row0 + b) * 2 + 1) * p.NA + a0 + a, dup);
-                }
-            }
-        }
+    int t = tile_in_list(0);
+    if (t >= total) return;
+    clear();
+    begin(t);
+    store(0, 0, 0, 0);   // nothing, but the stores are counted
+    for (int i = 1;; ++i) {
+        if (wb * FB * 16 < b_left) tile_sum<true, kStores>(s, slot0, slot1, slot2, slot3, acc);
+        else tile_sum<false, kStores>(s, slot0, slot1, slot2, slot3, acc);   // rows past the segment: loads and barriers only
+        const int done_a0 = a0, done_a = a_left, done_b = b_left;
+        const int64_t done_row = row0;
+        t = tile_in_list(i);
+        const bool more = t < total;   // later tiles of this workgroup lie behind it
+        if (more) begin(t);            // under way while this tile's outputs are stored
+        store(done_a0, done_a, done_b, done_row);
+        if (!more) break;
+        clear();
     }
+    __builtin_amdgcn_s_waitcnt(0x0070);   // nothing may be on its way to LDS when the workgroup gives it up
 }
 
 // ---- Few rows per expert: bound by the weights, every one of which is read once for a handful of rows.
