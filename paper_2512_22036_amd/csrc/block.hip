@@ -52,9 +52,9 @@ int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
         // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
         if (mean < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
     }
-    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 8, 4, STORE>, (L->P / 256 + L->E) * tiles_a, 1, a, s);
-    else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 4, 4, STORE>, (L->P / 128 + L->E) * tiles_a, 1, a, s);
-    else launch_product(product_kernel<AMODE, kAlongC, 64, 4, 2, STORE>, (L->P / 64 + L->E) * tiles_a, 2, a, s);
+    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, (L->P / 256 + L->E) * tiles_a, 1, a, s);
+    else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, (L->P / 128 + L->E) * tiles_a, 1, a, s);
+    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, (L->P / 64 + L->E) * tiles_a, 2, a, s);
     return launch_status();
 }
 
@@ -370,8 +370,8 @@ int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const voi
     if (((int64_t)L->E * ((M + 255) / 256)) * ((C + 255) / 256) >= (int64_t)1 << 30) return FUSCO_ERR_INVALID_ARG;
     ProductArgs a = {L->exp_off, (const char *)d_x, (const char *)d_dy, (char *)d_dw, nullptr, L->E, C, M, 0};
     const int64_t tiles = (int64_t)L->E * ((M + 255) / 256) * ((C + 255) / 256);
-    if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 8, 4, kStoreF32>, tiles, 1, a, (hipStream_t)stream);
-    else launch_product(product_kernel<kAcross, kAcross, 256, 8, 4, kStoreBf16>, tiles, 1, a, (hipStream_t)stream);
+    if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32>, tiles, 1, a, (hipStream_t)stream);
+    else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16>, tiles, 1, a, (hipStream_t)stream);
     return launch_status();
 }
 

@@ -15,6 +15,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) char lds_byte;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
@@ -51,14 +52,15 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, ui
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 16, (int)offset, uniform, 0, 0);
 }
 
-// One operand of a tile: where a stage of it comes from and how it lies in LDS.
-//   kAlongC: LDS rows of 32 elements (64 bytes), the 16-byte chunk q of row r at place q ^ (r >> 1 & 3): eight lanes that read the same chunk
-//            of eight rows hit all banks.
-//   kAcross: LDS rows of W elements, one per c; pairs of chunks (16 elements) of row c at place pair ^ f(c), f(c) = (c & 3) + 4 * bit 3 of c:
-//            the transposing read takes 32 bytes of each of the rows c .. c + 3 and c + 8 .. c + 11 at once.
-// PAIRED (kAlongC): the rows of fragments 2 p and 2 p + 1 are dealt out so that a lane's outputs of both are eight neighbours along a (row r of
-// fragment 2 p + h is p * 32 + r / 4 * 8 + h * 4 + r % 4); the place of a chunk follows suit: q ^ (bit 1 of r + 2 * bit 3 of r).
-template <int MODE, int W, bool PAIRED>
+// One operand of a tile: where a stage of it comes from and how it lies in LDS.  A fragment is 32 outputs by 16 elements of the sum, slice `ks`
+// (0 or 1) of the stage; lane l has output l % 32 and elements l / 32 * 8 + 0 .. 7.
+//   OUT (operand A): the outputs of a fragment are dealt out so that the 16 results of a lane are neighbours: output i of the matrix
+//   instruction is the fragment's row (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3).  Operand B keeps its order.
+//   kAlongC: LDS rows of 32 elements (64 bytes), the 16-byte chunk q of row r at place q ^ (r >> 2 & 3): the 16 lanes that are
+//            served together (0-3, 12-15, 20-27 and so on) hit all banks in either order of the rows.
+//   kAcross: LDS rows of W elements, one per c; windows of 32 outputs (64 bytes) of row c at place window ^ (c & 3): the transposing read of 32
+//            lanes takes one window of each of four rows.
+template <int MODE, int W, bool OUT>
 struct Operand {
     static constexpr int kBytes = W * kTileC * 2;
     static constexpr int kChunks = kBytes / 16, kLoads = (kChunks + kTileThreads - 1) / kTileThreads;   // loads per thread and stage
@@ -68,12 +70,13 @@ struct Operand {
     int64_t limit;         // kAlongC: readable bytes from base; kAcross: bytes that are missing from a whole last row
     int32_t c_size;        // elements (kAlongC) or rows (kAcross) of the summed dimension
     uint32_t at[kLoads];   // this thread's byte offsets
+    int32_t chunk;         // kAlongC: the chunk of its row that this thread loads
 
-    __device__ __forceinline__ void load(int stage, int i, char *lds, int wave, int lane) const
+    __device__ __forceinline__ void load(int stage, int i, char *lds, int wave) const
     {
         if (kLoadWaves < kTileThreads / kWave && wave >= kLoadWaves) return;
         if (MODE == kAlongC) {
-            const bool in = stage * kTileC + chunk_of(lane) * 8 < c_size;
+            const bool in = stage * kTileC + chunk * 8 < c_size;
             to_lds(view(base, limit), lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, stage * kTileC * 2);
         } else {
             const int left = min(max(c_size - stage * kTileC, 0), kTileC);
@@ -83,26 +86,29 @@ struct Operand {
         }
     }
 
-    // kAlongC: the chunk of its row that this lane loads; a row is loaded by four lanes
-    static __device__ __forceinline__ int chunk_of(int lane) { return (lane & 3) ^ swizzle(lane >> 2); }
-    static __device__ __forceinline__ int swizzle(int row) { return PAIRED ? (row >> 1 & 1) | (row >> 2 & 2) : row >> 1 & 3; }
+    // Load i of thread tid: which row of the stage's LDS (an output for kAlongC, a c for kAcross), and the first output (kAcross)
+    static __device__ __forceinline__ int row_of(int i, int tid) { return MODE == kAlongC ? i * (kTileThreads / 4) + tid / 4 : (i * kTileThreads + tid) / (W / 8); }
+    static __device__ __forceinline__ int swizzle(int row) { return row >> 2 & 3; }
+    static __device__ __forceinline__ int chunk_of(int tid) { return (tid & 3) ^ swizzle(tid / 4); }
+    static __device__ __forceinline__ int output_of(int i, int tid) { return ((tid & (W / 8 - 1)) ^ ((row_of(i, tid) & 3) << 2)) * 8; }
 
-    // byte offset of this lane's part of a wave's first fragment, `first`, a multiple of the wave's fragments (a power of two)
+    // byte offset of this lane's part of the wave's first fragment, which begins at output `first`, a multiple of all its outputs
     static __device__ __forceinline__ uint32_t lane_at(int lane, int first)
     {
         if (MODE == kAlongC) {
-            const int row = PAIRED ? (lane & 12) * 2 + (lane & 3) : lane & 15;
-            return (first * 16 + row) * (kTileC * 2) + (((lane >> 4) ^ swizzle(row)) << 4);
+            const int i = lane & 31, row = OUT ? (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3) : i;
+            return (first + row) * (kTileC * 2) + (((lane >> 5) ^ swizzle(row)) << 4);
         }
-        const int g = lane >> 4, i = lane & 15, place = ((lane >> 2) & 3) | (((lane >> 4) & 1) << 2);
-        return (g * 8 + (i >> 2)) * (W * 2) + ((first ^ place) << 5) + ((i & 3) >> 1) * 16 + (i & 1) * 8;
+        // a group of 16 lanes reads 4 outputs of 4 rows each, which the transposition gives to 16 outputs of one lane each
+        const int c = (lane >> 5) * 8 + (lane >> 2 & 3), m = lane & 3, half = lane >> 4 & 1;
+        const int output = OUT ? (m & 1) * 16 + (half * 2 + (m >> 1)) * 4 : half * 16 + m * 4;
+        return c * (W * 2) + (((first >> 5) ^ (c & 3)) << 6) + output * 2;
     }
 
-    // the wave's fragment f (16 outputs): element j of lane l is (row l % 16 of the fragment, l / 16 * 8 + j)
-    static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t at, int f)
+    static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t at, int f, int ks)
     {
-        if (MODE == kAlongC) return *(const bf16x8 *)(lds + at + (PAIRED ? (f >> 1) * 32 + (f & 1) * 4 : f * 16) * kTileC * 2);
-        const char *p = lds + (at ^ (f << 5));
+        if (MODE == kAlongC) return *(const bf16x8 *)(lds + (at ^ (ks << 5)) + f * 32 * kTileC * 2);
+        const char *p = lds + (at ^ (f << 6)) + ks * 16 * W * 2;
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 4 * W * 2));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -113,14 +119,13 @@ struct Operand {
 constexpr int kSlots = 4;              // stages in LDS: one is multiplied while three are on their way
 template <int AMODE, int BMODE, int BB, int FA, int FB>
 struct TileState {
-    static constexpr bool kPaired = AMODE == kAlongC;
-    typedef Operand<AMODE, kTileA, kPaired> A;
+    typedef Operand<AMODE, kTileA, true> A;
     typedef Operand<BMODE, BB, false> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes;
     A a;
     B b;
     uint32_t a_lane, b_lane;
-    int wave, lane;
+    int wave;
     int stages, turn;
 
     // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one loads fetch nothing, but they are made, so that
@@ -133,8 +138,8 @@ struct TileState {
     __device__ __forceinline__ void load(int s, int i, char *slot) const
     {
         const int at = stage_of(s);
-        if (i < A::kLoads) a.load(at, i, slot, wave, lane);
-        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, lane);
+        if (i < A::kLoads) a.load(at, i, slot, wave);
+        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave);
     }
     // waits until at most the loads of `behind` stages and `more` stores are on their way and nothing is being read from LDS
     template <int behind, int more = 0>
@@ -147,43 +152,53 @@ struct TileState {
     }
 };
 
-// One stage has two parts.  First all of `cur`'s fragments but those of the last group (four fragments along a) are multiplied, while the last
-// group's are read; then comes the barrier behind which `cur` is free and `nxt` is whole, and the last group is multiplied while nxt's
-// first fragments are read and the stage that will take cur's place is asked for.  PAR: parity of the stage, for registers that change places.
-template <int PAR, bool ACTIVE, int AMODE, int BMODE, int BB, int FA, int FB>
-__device__ __forceinline__ void tile_first(const TileState<AMODE, BMODE, BB, FA, FB> &t, const char *cur, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+// A stage has two parts, one per slice of the sum.  The first slice is multiplied while the second one's fragments are read; then comes the
+// barrier behind which `cur` is free and `nxt` is whole, and the second slice is multiplied while nxt's first fragments are read and the
+// stage that will take cur's place is asked for.  Every matrix instruction is followed by what can be issued while it runs.
+template <int FA, int FB>
+struct Slice {
+    bf16x8 a[FA], b[FB];
+};
+
+// what comes after matrix instruction m of FA * FB: fragment reads, those of b first, spread evenly
+template <int FA, int FB, typename S>
+__device__ __forceinline__ void read_after(const S &t, const char *slot, uint32_t a_at, uint32_t b_at, int ks, int m, Slice<FA, FB> &to)
 {
-    if (!ACTIVE || FA == 4) return;
-    uint32_t at = t.a_lane;
-    asm volatile("" : "+v"(at));         // fragments' places are worked out where they are used, not kept in registers over the loop
+    constexpr int kReads = FA + FB, kEach = (kReads + FA * FB - 1) / (FA * FB);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        a[1][i] = t.a.fragment(cur, at, 4 + i);
-#pragma unroll
-        for (int j = 0; j < FB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[0][i], b[PAR][j], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int i = m * kEach; i < (m + 1) * kEach && i < kReads; ++i) {
+        if (i < FB) to.b[i] = t.b.fragment(slot + S::A::kBytes, b_at, i, ks);
+        else to.a[i - FB] = t.a.fragment(slot, a_at, i - FB, ks);
     }
 }
 
-template <int PAR, bool ACTIVE, int STORES, int AMODE, int BMODE, int BB, int FA, int FB>
-__device__ __forceinline__ void tile_last(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *cur, const char *nxt, int s, bf16x8 (&a)[2][4], bf16x8 (&b)[2][FB], f32x4 (&acc)[FA][FB])
+template <bool ACTIVE, int STORES, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nxt, int s, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
 {
-    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
-    constexpr int kLast = FA == 8 ? 1 : PAR, kNext = FA == 8 ? 0 : 1 - PAR, kRow = FA - 4;   // which a[], which rows of acc
+    uint32_t a_at = t.a_lane, b_at = t.b_lane;
+    asm volatile("" : "+v"(a_at), "+v"(b_at));   // fragments' places are worked out where they are used, not kept in registers over the loop
+    if (ACTIVE) {
+#pragma unroll
+        for (int m = 0; m < FA * FB; ++m) {
+            acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0].a[m / FB], x[0].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
+            read_after(t, cur, a_at, b_at, 1, m, x[1]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
     t.template wait<kSlots - 2, STORES>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    uint32_t a_at = t.a_lane, b_at = t.b_lane;
-    asm volatile("" : "+v"(a_at), "+v"(b_at));
+    if (ACTIVE) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        t.load(s + kSlots, i, cur);
-        if (ACTIVE) {
-            if (i < FB) b[1 - PAR][i] = t.b.fragment(nxt + kABytes, b_at, i);
-            a[kNext][i] = t.a.fragment(nxt, a_at, i);
-#pragma unroll
-            for (int j = 0; j < FB; ++j) acc[kRow + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[kLast][i], b[PAR][j], acc[kRow + i][j], 0, 0, 0);
+        for (int m = 0; m < FA * FB; ++m) {
+            acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1].a[m / FB], x[1].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
+            read_after(t, nxt, a_at, b_at, 0, m, x[0]);
+            if (m >= FA * FB - 2) t.load(s + kSlots, m - (FA * FB - 2), cur);
+            __builtin_amdgcn_sched_barrier(0);
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) t.load(s + kSlots, i, cur);
         __builtin_amdgcn_sched_barrier(0);
     }
 }
@@ -205,24 +220,19 @@ __device__ __forceinline__ void tile_begin(const TileState<AMODE, BMODE, BB, FA,
 // The sums of a tile whose first stages are under way; after them STORES stores at least were issued (the outputs of the tile before), which
 // the first three stages do not wait for.  The slots are arrays of their own: the compiler then knows that a fragment's read waits for
 // its own slot's loads only.
-template <bool ACTIVE, int STORES, int AMODE, int BMODE, int BB, int FA, int FB>
-__device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x4 (&acc)[FA][FB])
+template <bool ACTIVE, int STORES, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_sum(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x16 (&acc)[FA][FB])
 {
-    constexpr int kABytes = TileState<AMODE, BMODE, BB, FA, FB>::A::kBytes;
     if (t.stages == 0) return;
     t.template wait<kSlots - 1, STORES>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    bf16x8 a[2][4], b[2][FB];
+    Slice<FA, FB> x[2];
     if (ACTIVE) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[0][i] = t.a.fragment(slot0, t.a_lane, i);
-#pragma unroll
-        for (int j = 0; j < FB; ++j) b[0][j] = t.b.fragment(slot0 + kABytes, t.b_lane, j);
+        for (int m = 0; m < FA * FB; ++m) read_after(t, slot0, t.a_lane, t.b_lane, 0, m, x[0]);
     }
-#define FUSCO_STAGE(n, cur, nxt, stores)                                     \
-    tile_first<(n) % 2, ACTIVE>(t, cur, a, b, acc);                          \
-    tile_last<(n) % 2, ACTIVE, stores>(t, cur, nxt, s + (n), a, b, acc)
+#define FUSCO_STAGE(n, cur, nxt, stores) tile_stage<ACTIVE, stores>(t, cur, nxt, s + (n), x, acc)
     // Whole turns through the slots, then what is left.  The loop has one way out: at the head of one with several the compiler would
     // take loads of the present turn to be still under way.
     int s = 0;
@@ -253,10 +263,8 @@ __device__ __forceinline__ void tile_sum(const TileState<AMODE, BMODE, BB, FA, F
 }
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
-typedef uint32_t words2 __attribute__((ext_vector_type(2)));
 
-// Outputs of a wave: lane l has FA / 2 pairs of fragments along a and FB along b.  Stores go through a bounds-checked view, so that their
-// number is the same for every tile: what lies outside is dropped.
+// Outputs of a wave.  Stores go through a bounds-checked view, so that their number is the same for every tile: what lies outside is dropped.
 struct Target {
     __amdgpu_buffer_rsrc_t to;
     uint32_t ld;           // bytes from row to row
@@ -265,24 +273,18 @@ struct Target {
         ld = (uint32_t)row_bytes;
         to = view(p + row0 * row_bytes + column_bytes, rows > 0 ? rows * row_bytes - column_bytes : 0);
     }
-    __device__ __forceinline__ void put8(f32x4 lo, f32x4 hi, uint32_t offset) const
+    __device__ __forceinline__ void put8(const float *v, uint32_t offset) const
     {
         bf16x8 o;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            o[q] = (__bf16)lo[q];
-            o[q + 4] = (__bf16)hi[q];
-        }
+        for (int q = 0; q < 8; ++q) o[q] = (__bf16)v[q];
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, o), to, (int)offset, 0, 0);
     }
-    __device__ __forceinline__ void put4(f32x4 v, uint32_t offset) const
+    __device__ __forceinline__ void put4(const float *v, uint32_t offset) const
     {
-        bf16x4 o;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = (__bf16)v[q];
-        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(words2, o), to, (int)offset, 0, 0);
+        const f32x4 o = {v[0], v[1], v[2], v[3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, o), to, (int)offset, 0, 0);
     }
-    __device__ __forceinline__ void put_f32(f32x4 v, uint32_t offset) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, v), to, (int)offset, 0, 0); }
 };
 
 __device__ __forceinline__ void store4(char *out, int64_t element, f32x4 v)
@@ -328,17 +330,17 @@ __device__ __forceinline__ int tile_in_list(int i)
     return ((i * (int)(gridDim.x / kCus) + round) * kXcds + in % kXcds) * per_xcd + in / kXcds;
 }
 
-// FA x FB fragments of 16 x 16 outputs per wave, kTileA / (16 * FA) waves along a
+// FA x FB fragments of 32 x 32 outputs per wave, kTileA / (32 * FA) waves along a
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
 __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel(ProductArgs p)
 {
     typedef TileState<AMODE, BMODE, BB, FA, FB> State;
-    constexpr int kWavesA = kTileA / (16 * FA), kWavesB = BB / (16 * FB);
+    constexpr int kWavesA = kTileA / (32 * FA), kWavesB = BB / (32 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
     constexpr bool kGated = STORE == kStoreGated;
     constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
-    static_assert(FA % 4 == 0 && FB <= 4, "groups of four fragments along a");
+    static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[State::kStageBytes], slot3[State::kStageBytes];
     __shared__ int prefix[FUSCO_MAX_E + 1];
     __shared__ int part[kTileThreads / kWave];
@@ -362,9 +364,8 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
 
     State s;
     s.wave = wave;
-    s.lane = lane;
-    s.a_lane = State::A::lane_at(lane, wa * FA);
-    s.b_lane = State::B::lane_at(lane, wb * FB);
+    s.a_lane = State::A::lane_at(lane, wa * FA * 32);
+    s.b_lane = State::B::lane_at(lane, wb * FB * 32);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
 
     // the tile at hand
@@ -412,15 +413,16 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             s.a.base = p.other + ((int64_t)e * rows_e + a0) * s.a.ld;
             s.a.limit = (rows_e - a0) * s.a.ld;
             s.a.c_size = p.C;
+            s.a.chunk = State::A::chunk_of(tid);
 #pragma unroll
             for (int j = 0; j < State::A::kLoads; ++j) {
-                const int r = j * (kTileThreads / 4) + tid / 4;
+                const int r = State::A::row_of(j, tid);
                 int unit = r, up = 0;
-                if (kGated) {   // a wave's rows: FA * 8 gate rows, then the up rows of the same units
-                    unit = r / (16 * FA) * (8 * FA) + r % (8 * FA);
-                    up = r / (8 * FA) % 2;
+                if (kGated) {   // a wave's rows: FA * 16 gate rows, then the up rows of the same units
+                    unit = r / (32 * FA) * (16 * FA) + r % (16 * FA);
+                    up = r / (16 * FA) % 2;
                 }
-                s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (State::A::chunk_of(lane) << 4) : kNowhere;
+                s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (s.a.chunk << 4) : kNowhere;
             }
         } else {
             s.a.ld = (int64_t)p.NA * 2;
@@ -429,9 +431,8 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             s.a.base = (kByRows ? p.other + (int64_t)e * p.C * s.a.ld : p.rows + first * s.a.ld) + s.a.limit;
 #pragma unroll
             for (int j = 0; j < State::A::kLoads; ++j) {
-                const int c = j * (kTileThreads / 32) + tid / 32, swz = (c & 3) | ((c >> 3 & 1) << 2);
-                const int col = ((tid & 31) ^ (swz << 1)) * 8;
-                s.a.at[j] = col < a_left ? (uint32_t)(c * s.a.ld) + col * 2 : kNowhere;
+                const int output = State::A::output_of(j, tid);
+                s.a.at[j] = output < a_left ? (uint32_t)(State::A::row_of(j, tid) * s.a.ld) + output * 2 : kNowhere;
             }
         }
         // operand B
@@ -440,21 +441,19 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             s.b.base = p.rows + ((int64_t)first + b0) * s.b.ld;
             s.b.limit = (b_left < BB ? b_left : BB) * s.b.ld;
             s.b.c_size = p.C;
+            s.b.chunk = State::B::chunk_of(tid);
 #pragma unroll
-            for (int j = 0; j < State::B::kLoads; ++j)
-                s.b.at[j] = (uint32_t)((j * (kTileThreads / 4) + tid / 4) * s.b.ld) + (State::B::chunk_of(lane) << 4);
+            for (int j = 0; j < State::B::kLoads; ++j) s.b.at[j] = (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + (s.b.chunk << 4);
             s.stages = (p.C + kTileC - 1) / kTileC;
         } else {
-            constexpr int kChunks = BB / 8;
             s.b.ld = (int64_t)p.NB * 2;
             s.b.limit = (int64_t)b0 * 2;
             s.b.base = p.other + first * s.b.ld + s.b.limit;
             s.b.c_size = rows;
 #pragma unroll
             for (int j = 0; j < State::B::kLoads; ++j) {
-                const int c = j * (kTileThreads / kChunks) + tid / kChunks, swz = (c & 3) | ((c >> 3 & 1) << 2);
-                const int col = ((tid & (kChunks - 1)) ^ (swz << 1)) * 8;
-                s.b.at[j] = col < b_left ? (uint32_t)(c * s.b.ld) + col * 2 : kNowhere;
+                const int output = State::B::output_of(j, tid);
+                s.b.at[j] = output < b_left ? (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + output * 2 : kNowhere;
             }
             s.stages = (rows + kTileC - 1) / kTileC;
         }
@@ -463,9 +462,9 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
         tile_begin(s, slot0, slot1, slot2, slot3);
     };
 
-    // Lane l holds, of fragment (f, j), four neighbouring outputs along a of b = 16 * j + l % 16.
+    // Lane l holds, of fragment (f, j), the outputs a = 32 * f + l / 32 * 16 + 0 .. 15 of b = 32 * j + l % 32.
     constexpr int kOutA = kGated ? FA / 2 : FA;
-    f32x4 acc[FA][FB];
+    f32x16 acc[FA][FB];
     auto store = [&](int a0, int a_left, int b_left, int64_t row0) {
         constexpr int kSize = STORE == kStoreF32 ? 4 : 2;
         const int rows = b_left < BB ? b_left : BB;
@@ -477,54 +476,49 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
         asm volatile("" : "+v"(lane));   // places are worked out here, not kept in registers over the sums
 #pragma unroll
         for (int j = 0; j < FB; ++j) {
-            const int b = wb * FB * 16 + j * 16 + (lane & 15);
-            if constexpr (State::kPaired) {
+            const int b = (wb * FB + j) * 32 + (lane & 31);
 #pragma unroll
-                for (int f = 0; f < kOutA; f += 2) {
-                    const int a = wa * kOutA * 16 + f * 16 + (lane >> 4) * 8;
-                    const uint32_t at = a < a_left && b < b_left ? b * out.ld + a * kSize : kNowhere;
-                    f32x4 lo = acc[f][j], hi = acc[f + 1][j];
-                    if (kGated) {
-                        const f32x4 up_lo = acc[f + FA / 2][j], up_hi = acc[f + 1 + FA / 2][j];
-                        if (p.pre) {
-                            const uint32_t to = a < a_left && b < b_left ? b * pre.ld + a * kSize : kNowhere;
-                            pre.put8(lo, hi, to);
-                            pre.put8(up_lo, up_hi, to + second);
-                        }
+            for (int f = 0; f < kOutA; ++f) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            lo[q] = silu(lo[q]) * up_lo[q];
-                            hi[q] = silu(hi[q]) * up_hi[q];
-                        }
-                    }
-                    out.put8(lo, hi, at);
-                }
-            } else {
-#pragma unroll
-                for (int f = 0; f < kOutA; ++f) {
-                    const int a = wa * kOutA * 16 + f * 16 + (lane >> 4) * 4;
+                for (int h = 0; h < 2; ++h) {
+                    const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16 + h * 8;
                     const bool in = a < a_left && b < b_left;
                     const uint32_t at = in ? b * out.ld + a * kSize : kNowhere;
-                    const f32x4 v = acc[f][j];
-                    if (STORE == kStoreF32) {
-                        out.put_f32(v, at);
-                    } else if (STORE == kStoreBf16) {
-                        out.put4(v, at);
-                    } else {
-                        bf16x4 gate, up;
-                        if (in) {
-                            gate = *(const bf16x4 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
-                            up = *(const bf16x4 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
-                        }
-                        f32x4 dgate, dup;
+                    float v[8];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < 8; ++q) v[q] = acc[f][j][h * 8 + q];
+                    if (STORE == kStoreF32) {
+                        out.put4(v, at);
+                        out.put4(v + 4, at + 16);
+                    } else if (STORE == kStoreBf16) {
+                        out.put8(v, at);
+                    } else if (STORE == kStoreGated) {
+                        float up[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) up[q] = acc[f + FA / 2][j][h * 8 + q];
+                        if (p.pre) {
+                            const uint32_t to = in ? b * pre.ld + a * kSize : kNowhere;
+                            pre.put8(v, to);
+                            pre.put8(up, to + second);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) v[q] = silu(v[q]) * up[q];
+                        out.put8(v, at);
+                    } else {
+                        bf16x8 gate, up;
+                        if (in) {
+                            gate = *(const bf16x8 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
+                            up = *(const bf16x8 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
+                        }
+                        float dup[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) {
                             const float g = (float)gate[q], sig = 1.0f / (1.0f + __expf(-g));
                             dup[q] = v[q] * g * sig;
-                            dgate[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
+                            v[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
                         }
-                        out.put4(dgate, at);
-                        out.put4(dup, at + second);
+                        out.put8(v, at);
+                        out.put8(dup, at + second);
                     }
                 }
             }
@@ -535,10 +529,12 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
 #pragma unroll
         for (int f = 0; f < FA; ++f)
 #pragma unroll
-            for (int j = 0; j < FB; ++j) acc[f][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int j = 0; j < FB; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[f][j][q] = 0.0f;
     };
     // stores of one tile and wave; the activation's gradient waits for loads in between and counts as none
-    constexpr int kStores = STORE == kStoreGatedGrad ? 0 : State::kPaired ? FB * kOutA / 2 : FB * kOutA;
+    constexpr int kStores = STORE == kStoreGatedGrad ? 0 : FB * kOutA * (STORE == kStoreF32 ? 4 : 2);
 
     int t = tile_in_list(0);
     if (t >= total) return;
@@ -546,7 +542,7 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     begin(t);
     store(0, 0, 0, 0);   // nothing, but the stores are counted
     for (int i = 1;; ++i) {
-        if (wb * FB * 16 < b_left) tile_sum<true, kStores>(s, slot0, slot1, slot2, slot3, acc);
+        if (wb * FB * 32 < b_left) tile_sum<true, kStores>(s, slot0, slot1, slot2, slot3, acc);
         else tile_sum<false, kStores>(s, slot0, slot1, slot2, slot3, acc);   // rows past the segment: loads and barriers only
         const int done_a0 = a0, done_a = a_left, done_b = b_left;
         const int64_t done_row = row0;
