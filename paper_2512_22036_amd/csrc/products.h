@@ -20,7 +20,6 @@ typedef __attribute__((address_space(3))) char lds_byte;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int kCus = 256;              // compute units of an MI355X
-constexpr int kTileC = 32;             // elements of the summed dimension per stage
 constexpr int kTileThreads = 512;
 constexpr int kTileA = 256;
 constexpr uint32_t kNowhere = 0x7f000000u;   // byte offset past every buffer: such a load gives zeros
@@ -52,17 +51,18 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, ui
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 16, (int)offset, uniform, 0, 0);
 }
 
-// One operand of a tile: where a stage of it comes from and how it lies in LDS.  A fragment is 32 outputs by 16 elements of the sum, slice `ks`
-// (0 or 1) of the stage; lane l has output l % 32 and elements l / 32 * 8 + 0 .. 7.
+// One operand of a tile: where a stage of it (KC elements of the summed dimension) comes from and how it lies in LDS.  A fragment is 32 outputs
+// by 16 elements of the sum, slice `ks` of the stage; lane l has output l % 32 and elements l / 32 * 8 + 0 .. 7.
 //   OUT (operand A): the outputs of a fragment are dealt out so that the 16 results of a lane are neighbours: output i of the matrix
 //   instruction is the fragment's row (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3).  Operand B keeps its order.
-//   kAlongC: LDS rows of 32 elements (64 bytes), the 16-byte chunk q of row r at place q ^ (r >> 2 & 3): the 16 lanes that are
+//   kAlongC: LDS rows of KC elements, the 16-byte chunk q of row r at place q ^ swizzle(r): the 16 lanes that are
 //            served together (0-3, 12-15, 20-27 and so on) hit all banks in either order of the rows.
 //   kAcross: LDS rows of W elements, one per c; windows of 32 outputs (64 bytes) of row c at place window ^ (c & 3): the transposing read of 32
 //            lanes takes one window of each of four rows.
-template <int MODE, int W, bool OUT>
+template <int MODE, int W, int KC, bool OUT>
 struct Operand {
-    static constexpr int kBytes = W * kTileC * 2;
+    static constexpr int kBytes = W * KC * 2;
+    static constexpr int kRowLanes = KC / 8;   // kAlongC: lanes that load one row
     static constexpr int kChunks = kBytes / 16, kLoads = (kChunks + kTileThreads - 1) / kTileThreads;   // loads per thread and stage
     static constexpr int kLoadWaves = kChunks < kTileThreads ? kChunks / kWave : kTileThreads / kWave;  // waves that take part in a load
     const char *base;
@@ -76,20 +76,20 @@ struct Operand {
     {
         if (kLoadWaves < kTileThreads / kWave && wave >= kLoadWaves) return;
         if (MODE == kAlongC) {
-            const bool in = stage * kTileC + chunk * 8 < c_size;
-            to_lds(view(base, limit), lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, stage * kTileC * 2);
+            const bool in = stage * KC + chunk * 8 < c_size;
+            to_lds(view(base, limit), lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, stage * KC * 2);
         } else {
-            const int left = min(max(c_size - stage * kTileC, 0), kTileC);
+            const int left = min(max(c_size - stage * KC, 0), KC);
             const int bytes = __builtin_amdgcn_readfirstlane(max(left * (int)ld - (int)limit, 0));
-            to_lds(__builtin_amdgcn_make_buffer_rsrc((void *)(base + (int64_t)stage * (int64_t)(kTileC * (int)ld)), 0, bytes, 0x00020000),
+            to_lds(__builtin_amdgcn_make_buffer_rsrc((void *)(base + (int64_t)stage * (int64_t)(KC * (int)ld)), 0, bytes, 0x00020000),
                    lds + (i * kTileThreads + wave * kWave) * 16, at[i], 0);
         }
     }
 
     // Load i of thread tid: which row of the stage's LDS (an output for kAlongC, a c for kAcross), and the first output (kAcross)
-    static __device__ __forceinline__ int row_of(int i, int tid) { return MODE == kAlongC ? i * (kTileThreads / 4) + tid / 4 : (i * kTileThreads + tid) / (W / 8); }
-    static __device__ __forceinline__ int swizzle(int row) { return row >> 2 & 3; }
-    static __device__ __forceinline__ int chunk_of(int tid) { return (tid & 3) ^ swizzle(tid / 4); }
+    static __device__ __forceinline__ int row_of(int i, int tid) { return MODE == kAlongC ? (i * kTileThreads + tid) / kRowLanes : (i * kTileThreads + tid) / (W / 8); }
+    static __device__ __forceinline__ int swizzle(int row) { return KC == 64 ? row >> 1 & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int chunk_of(int tid) { return (tid & (kRowLanes - 1)) ^ swizzle(tid / kRowLanes); }
     static __device__ __forceinline__ int output_of(int i, int tid) { return ((tid & (W / 8 - 1)) ^ ((row_of(i, tid) & 3) << 2)) * 8; }
 
     // byte offset of this lane's part of the wave's first fragment, which begins at output `first`, a multiple of all its outputs
@@ -97,7 +97,7 @@ struct Operand {
     {
         if (MODE == kAlongC) {
             const int i = lane & 31, row = OUT ? (i >> 2 & 1) * 16 + (i >> 3) * 4 + (i & 3) : i;
-            return (first + row) * (kTileC * 2) + (((lane >> 5) ^ swizzle(row)) << 4);
+            return (first + row) * (KC * 2) + (((lane >> 5) ^ swizzle(row)) << 4);
         }
         // a group of 16 lanes reads 4 outputs of 4 rows each, which the transposition gives to 16 outputs of one lane each
         const int c = (lane >> 5) * 8 + (lane >> 2 & 3), m = lane & 3, half = lane >> 4 & 1;
@@ -107,7 +107,7 @@ struct Operand {
 
     static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t at, int f, int ks)
     {
-        if (MODE == kAlongC) return *(const bf16x8 *)(lds + (at ^ (ks << 5)) + f * 32 * kTileC * 2);
+        if (MODE == kAlongC) return *(const bf16x8 *)(lds + (at ^ (ks << 5)) + f * 32 * KC * 2);
         const char *p = lds + (at ^ (f << 6)) + ks * 16 * W * 2;
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)p);
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(p + 4 * W * 2));
@@ -115,13 +115,17 @@ struct Operand {
     }
 };
 
-// Everything a wave keeps over a tile
-constexpr int kSlots = 4;              // stages in LDS: one is multiplied while three are on their way
+// Everything a wave keeps over a tile.  Of the stages in LDS one is multiplied while the others are on their way.  Operands along c come in
+// rows of 128 bytes, whole lines of the L2, which leaves room for two stages; rows of operands across c are long anyway, and four stages of
+// half the length keep more in flight (8 experts of 16384 rows, 4096 x 2560, TF/s: two of 64 / four of 32: forward 1225 / 1190, input
+// gradient 1103 / 1150, weight gradient 1206 / 1345).
 template <int AMODE, int BMODE, int BB, int FA, int FB>
 struct TileState {
-    typedef Operand<AMODE, kTileA, true> A;
-    typedef Operand<BMODE, BB, false> B;
-    static constexpr int kStageBytes = A::kBytes + B::kBytes;
+    static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
+    typedef Operand<AMODE, kTileA, kStageC, true> A;
+    typedef Operand<BMODE, BB, kStageC, false> B;
+    static constexpr int kStageBytes = A::kBytes + B::kBytes, kLoads = A::kLoads;
+    static_assert(A::kLoads >= B::kLoads, "the wider operand");
     A a;
     B b;
     uint32_t a_lane, b_lane;
@@ -152,9 +156,9 @@ struct TileState {
     }
 };
 
-// A stage has two parts, one per slice of the sum.  The first slice is multiplied while the second one's fragments are read; then comes the
-// barrier behind which `cur` is free and `nxt` is whole, and the second slice is multiplied while nxt's first fragments are read and the
-// stage that will take cur's place is asked for.  Every matrix instruction is followed by what can be issued while it runs.
+// One stage, slice by slice: a slice is multiplied while the next one's fragments are read.  Before the last one comes the barrier behind which
+// `cur` is free and `nxt` is whole: nxt's first fragments are read then, and the stage that will take cur's place is asked for.  Every
+// matrix instruction is followed by what can be issued while it runs.
 template <int FA, int FB>
 struct Slice {
     bf16x8 a[FA], b[FB];
@@ -177,54 +181,60 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
 {
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
     asm volatile("" : "+v"(a_at), "+v"(b_at));   // fragments' places are worked out where they are used, not kept in registers over the loop
-    if (ACTIVE) {
 #pragma unroll
-        for (int m = 0; m < FA * FB; ++m) {
-            acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[0].a[m / FB], x[0].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
-            read_after(t, cur, a_at, b_at, 1, m, x[1]);
+    for (int ks = 0; ks < S::kSlices; ++ks) {
+        const bool last = ks == S::kSlices - 1;
+        if (last) {
+            t.template wait<S::kSlots - 2, STORES>();
+            __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    t.template wait<kSlots - 2, STORES>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    if (ACTIVE) {
+        const int next = (ks + 1) % S::kSlices;
+        if (ACTIVE) {
 #pragma unroll
-        for (int m = 0; m < FA * FB; ++m) {
-            acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[1].a[m / FB], x[1].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
-            read_after(t, nxt, a_at, b_at, 0, m, x[0]);
-            if (m >= FA * FB - 2) t.load(s + kSlots, m - (FA * FB - 2), cur);
+            for (int m = 0; m < FA * FB; ++m) {
+                acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % 2].a[m / FB], x[ks % 2].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
+                read_after(t, last ? nxt : cur, a_at, b_at, next, m, x[next % 2]);
+                if (last) {              // loads behind the last matrix instructions
+                    constexpr int kEach = (S::kLoads + FA * FB - 1) / (FA * FB), kBegin = FA * FB - S::kLoads / kEach;
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i)
+                        if (m >= kBegin) t.load(s + S::kSlots, (m - kBegin) * kEach + i, cur);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else if (last) {
+#pragma unroll
+            for (int i = 0; i < S::kLoads; ++i) t.load(s + S::kSlots, i, cur);
             __builtin_amdgcn_sched_barrier(0);
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) t.load(s + kSlots, i, cur);
-        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-template <int AMODE, int BMODE, int BB, int FA, int FB>
-__device__ __forceinline__ void tile_begin(const TileState<AMODE, BMODE, BB, FA, FB> &t, char *slot0, char *slot1, char *slot2, char *slot3)
+template <typename S>
+__device__ __forceinline__ void tile_begin(const S &t, char *slot0, char *slot1, char *slot2, char *slot3)
 {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) t.load(0, i, slot0);
+    for (int i = 0; i < S::kLoads; ++i) t.load(0, i, slot0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) t.load(1, i, slot1);
+    for (int i = 0; i < S::kLoads; ++i) t.load(1, i, slot1);
+    if constexpr (S::kSlots == 4) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) t.load(2, i, slot2);
+        for (int i = 0; i < S::kLoads; ++i) t.load(2, i, slot2);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) t.load(3, i, slot3);
+        for (int i = 0; i < S::kLoads; ++i) t.load(3, i, slot3);
+    }
     __builtin_amdgcn_sched_barrier(0);
 }
 
 // The sums of a tile whose first stages are under way; after them STORES stores at least were issued (the outputs of the tile before), which
-// the first three stages do not wait for.  The slots are arrays of their own: the compiler then knows that a fragment's read waits for
+// the first stages do not wait for.  The slots are arrays of their own: the compiler then knows that a fragment's read waits for
 // its own slot's loads only.
 template <bool ACTIVE, int STORES, int FA, int FB, typename S>
 __device__ __forceinline__ void tile_sum(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x16 (&acc)[FA][FB])
 {
     if (t.stages == 0) return;
-    t.template wait<kSlots - 1, STORES>();
+    t.template wait<S::kSlots - 1, STORES>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     Slice<FA, FB> x[2];
@@ -236,26 +246,41 @@ __device__ __forceinline__ void tile_sum(const S &t, char *slot0, char *slot1, c
     // Whole turns through the slots, then what is left.  The loop has one way out: at the head of one with several the compiler would
     // take loads of the present turn to be still under way.
     int s = 0;
-    const int whole = t.stages & ~(kSlots - 1);
-    if (whole > 0) {
-        FUSCO_STAGE(0, slot0, slot1, STORES);
-        FUSCO_STAGE(1, slot1, slot2, STORES);
-        FUSCO_STAGE(2, slot2, slot3, STORES);
-        FUSCO_STAGE(3, slot3, slot0, 0);
-        s = kSlots;
-    }
-    for (; s < whole; s += kSlots) {
-        FUSCO_STAGE(0, slot0, slot1, 0);
-        FUSCO_STAGE(1, slot1, slot2, 0);
-        FUSCO_STAGE(2, slot2, slot3, 0);
-        FUSCO_STAGE(3, slot3, slot0, 0);
-    }
-    if (s < t.stages) {
-        FUSCO_STAGE(0, slot0, slot1, 0);
-        if (s + 1 < t.stages) {
+    const int whole = t.stages & ~(S::kSlots - 1);
+    if constexpr (S::kSlots == 2) {
+        if (whole > 0) {
+            FUSCO_STAGE(0, slot0, slot1, STORES);
+            FUSCO_STAGE(1, slot1, slot0, 0);
+            s = 2;
+        }
+        for (; s < whole; s += 2) {
+            FUSCO_STAGE(0, slot0, slot1, 0);
+            FUSCO_STAGE(1, slot1, slot0, 0);
+        }
+        if (s < t.stages) {
+            FUSCO_STAGE(0, slot0, slot1, 0);
+        }
+    } else {
+        if (whole > 0) {
+            FUSCO_STAGE(0, slot0, slot1, STORES);
+            FUSCO_STAGE(1, slot1, slot2, STORES);
+            FUSCO_STAGE(2, slot2, slot3, STORES);
+            FUSCO_STAGE(3, slot3, slot0, 0);
+            s = 4;
+        }
+        for (; s < whole; s += 4) {
+            FUSCO_STAGE(0, slot0, slot1, 0);
             FUSCO_STAGE(1, slot1, slot2, 0);
-            if (s + 2 < t.stages) {
-                FUSCO_STAGE(2, slot2, slot3, 0);
+            FUSCO_STAGE(2, slot2, slot3, 0);
+            FUSCO_STAGE(3, slot3, slot0, 0);
+        }
+        if (s < t.stages) {
+            FUSCO_STAGE(0, slot0, slot1, 0);
+            if (s + 1 < t.stages) {
+                FUSCO_STAGE(1, slot1, slot2, 0);
+                if (s + 2 < t.stages) {
+                    FUSCO_STAGE(2, slot2, slot3, 0);
+                }
             }
         }
     }
@@ -341,7 +366,8 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
-    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[State::kStageBytes], slot3[State::kStageBytes];
+    constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
+    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[kMore], slot3[kMore];
     __shared__ int prefix[FUSCO_MAX_E + 1];
     __shared__ int part[kTileThreads / kWave];
 
@@ -444,7 +470,7 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             s.b.chunk = State::B::chunk_of(tid);
 #pragma unroll
             for (int j = 0; j < State::B::kLoads; ++j) s.b.at[j] = (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + (s.b.chunk << 4);
-            s.stages = (p.C + kTileC - 1) / kTileC;
+            s.stages = (p.C + State::kStageC - 1) / State::kStageC;
         } else {
             s.b.ld = (int64_t)p.NB * 2;
             s.b.limit = (int64_t)b0 * 2;
@@ -455,7 +481,7 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
                 const int output = State::B::output_of(j, tid);
                 s.b.at[j] = output < b_left ? (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + output * 2 : kNowhere;
             }
-            s.stages = (rows + kTileC - 1) / kTileC;
+            s.stages = (rows + State::kStageC - 1) / State::kStageC;
         }
         // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
         s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
