@@ -155,6 +155,7 @@ RouteArgs route_args(const fusco_router *R, const void *d_logits)
     a.stride = R->logits_stride;
     a.N = R->N; a.E = R->E; a.k = R->k;
     a.groups = R->groups; a.keep_groups = R->keep_groups; a.group_best = R->group_best; a.group_size = R->E / R->groups;
+    a.group_magic = ((1 << 20) + a.group_size - 1) / a.group_size;
     a.bf16 = R->logits_dtype == FUSCO_BF16;
     a.sigmoid = R->score == FUSCO_SCORE_SIGMOID;
     a.renorm = R->renorm;
@@ -162,16 +163,27 @@ RouteArgs route_args(const fusco_router *R, const void *d_logits)
     return a;
 }
 
-// calls f(lanes per row, values per lane)
+// calls f(lanes per row, values per lane, threads per workgroup).  16 lanes per row where every lane then has at most 32 values and k of the
+// lanes' largest values say enough; single waves per workgroup for few rows, which spreads them over the compute units.
 template <typename F>
 void with_route_shape(const fusco_router *R, F f)
 {
-    const int per_lane = (R->E + 63) / 64;
-    if (per_lane <= 1) f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-    else if (per_lane <= 2) f(std::integral_constant<int, 64>(), std::integral_constant<int, 2>());
-    else if (per_lane <= 4) f(std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
-    else if (per_lane <= 8) f(std::integral_constant<int, 64>(), std::integral_constant<int, 8>());
-    else f(std::integral_constant<int, 64>(), std::integral_constant<int, 16>());
+    const int by16 = (R->E + 15) / 16, by64 = (R->E + 63) / 64;
+    auto go = [&](auto lanes, auto values) {
+        if (R->N <= 4096) f(lanes, values, std::integral_constant<int, 64>());
+        else f(lanes, values, std::integral_constant<int, 256>());
+    };
+    const std::integral_constant<int, 16> some;
+    const std::integral_constant<int, 64> all;
+    if (R->k <= 10 && by16 <= 4) go(some, std::integral_constant<int, 4>());
+    else if (R->k <= 10 && by16 <= 8) go(some, std::integral_constant<int, 8>());
+    else if (R->k <= 10 && by16 <= 16) go(some, std::integral_constant<int, 16>());
+    else if (R->k <= 10 && by16 <= 32) go(some, std::integral_constant<int, 32>());
+    else if (by64 <= 1) go(all, std::integral_constant<int, 1>());
+    else if (by64 <= 2) go(all, std::integral_constant<int, 2>());
+    else if (by64 <= 4) go(all, std::integral_constant<int, 4>());
+    else if (by64 <= 8) go(all, std::integral_constant<int, 8>());
+    else go(all, std::integral_constant<int, 16>());
 }
 
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
@@ -192,9 +204,9 @@ int fusco_route(const fusco_router *R, const void *d_logits, const float *d_bias
     a.bias = d_bias;
     a.chosen = d_topk_idx;
     a.w = d_w;
-    with_route_shape(R, [&](auto lanes, auto vpl) {
-        constexpr int kRows = kRouteThreads / decltype(lanes)::value;
-        hipLaunchKernelGGL((route_kernel<decltype(lanes)::value, decltype(vpl)::value>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kRouteThreads), 0, (hipStream_t)stream, a);
+    with_route_shape(R, [&](auto lanes, auto values, auto threads) {
+        constexpr int kLanes = decltype(lanes)::value, kThreads = decltype(threads)::value, kRows = kThreads / kLanes;
+        hipLaunchKernelGGL((route_kernel<kLanes, decltype(values)::value, kThreads>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kThreads), 0, (hipStream_t)stream, a);
     });
     return launch_status();
 }
@@ -212,9 +224,9 @@ int fusco_route_backward(const fusco_router *R, const void *d_logits, const int3
     a.chosen = const_cast<int32_t *>(d_topk_idx);
     a.dw = d_dw;
     a.dlogits = (char *)d_dlogits;
-    with_route_shape(R, [&](auto lanes, auto vpl) {
-        constexpr int kRows = kRouteThreads / decltype(lanes)::value;
-        hipLaunchKernelGGL((route_grad_kernel<decltype(lanes)::value, decltype(vpl)::value>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kRouteThreads), 0, (hipStream_t)stream, a);
+    with_route_shape(R, [&](auto lanes, auto values, auto threads) {
+        constexpr int kLanes = decltype(lanes)::value, kThreads = decltype(threads)::value, kRows = kThreads / kLanes;
+        hipLaunchKernelGGL((route_grad_kernel<kLanes, decltype(values)::value, kThreads>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kThreads), 0, (hipStream_t)stream, a);
     });
     return launch_status();
 }

@@ -5,15 +5,13 @@
 //   as much as its group_best largest b together, and only experts of the keep_groups best groups compete
 //   chosen: the k largest b, descending, ties to the lower index;  w = scale * s / (sum of the chosen s)  or  scale * s
 //
-// LANES lanes of a wave hold one row, VPL values each: expert e is value e / LANES of lane e % LANES.
+// LANES lanes of a wave (16 or all 64) hold one row, VPL values each: expert e is value e / LANES of lane e % LANES.
 #ifndef FUSCO_CSRC_ROUTING_H
 #define FUSCO_CSRC_ROUTING_H
 
 #include "common.h"
 
 namespace {
-
-constexpr int kRouteThreads = 256;
 
 struct RouteArgs {
     const char *logits;
@@ -23,47 +21,48 @@ struct RouteArgs {
     const float *dw;       // backward: [N, k]
     char *dlogits;         // backward: [N, E] of the logits' type
     int64_t stride;        // elements from row to row of the logits
-    int32_t N, E, k, groups, keep_groups, group_best, group_size;
+    int32_t N, E, k, groups, keep_groups, group_best, group_size, group_magic;   // e / group_size == e * group_magic >> 20 for every e < 1024
     int32_t bf16, sigmoid, renorm;
     float scale;
 };
 
-template <int LANES>
-__device__ __forceinline__ float lanes_max(float v)
+// Values of the lanes `by` places on in the row of 16 lanes, round and round: no LDS, one instruction
+template <int by>
+__device__ __forceinline__ uint32_t turned(uint32_t v)
 {
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d /= 2) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + by, 0xf, 0xf, true);
 }
 
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v)
+// Reductions over the LANES lanes of a row, in all of them
+template <int LANES, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F f)
 {
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d /= 2) v += __shfl_xor(v, d);
-    return v;
-}
-
-template <int LANES>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v)
-{
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d /= 2) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
-        v = o > v ? o : v;
+    static_assert(sizeof(T) == 4 && (LANES == 16 || LANES == 64), "");
+    auto with = [&](uint32_t o) { v = f(v, __builtin_bit_cast(T, o)); };
+    with(turned<8>(__builtin_bit_cast(uint32_t, v)));
+    with(turned<4>(__builtin_bit_cast(uint32_t, v)));
+    with(turned<2>(__builtin_bit_cast(uint32_t, v)));
+    with(turned<1>(__builtin_bit_cast(uint32_t, v)));
+    if (LANES == 64) {
+        with((uint32_t)__shfl_xor((int)__builtin_bit_cast(uint32_t, v), 16));
+        with((uint32_t)__shfl_xor((int)__builtin_bit_cast(uint32_t, v), 32));
     }
     return v;
 }
-
 template <int LANES>
-__device__ __forceinline__ uint32_t lanes_min(uint32_t v)
+__device__ __forceinline__ float lanes_max(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) { return over_lanes<LANES>(v, [](float a, float b) { return a + b; }); }
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return over_lanes<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_min(uint32_t v) { return over_lanes<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
+
+// Orders the LDS accesses of a wave's lanes: a row belongs to one wave
+__device__ __forceinline__ void wave_sync()
 {
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d /= 2) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
-        v = o < v ? o : v;
-    }
-    return v;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 // Order of the scores as whole numbers.  Below every score: NaN (2), an expert of a group that was not kept (1), an expert that was
@@ -80,31 +79,65 @@ __device__ __forceinline__ float load_logit(const RouteArgs &p, int64_t at)
     return p.bf16 ? (float)((const __bf16 *)p.logits)[at] : ((const float *)p.logits)[at];
 }
 
-// 1 / (1 + e) with every operation rounded on its own: equal logits then score the same wherever they are computed
-__device__ __forceinline__ float sigmoid_exact(float l)
+// Sigmoids, 1 / (1 + exp(-l)) with every operation rounded correctly on its own: equal logits score the same wherever they are computed.
+// The reciprocal of 1 <= d < 2^126 comes from the hardware's (one unit in the last place) by one step of Newton's with fused
+// multiply-adds, which rounds it correctly for every such d; a wave with a d beyond divides.
+template <int n>
+__device__ __forceinline__ void sigmoids(float (&l)[n])
 {
 #pragma clang fp contract(off)
-    const float e = expf(-l);
-    const float d = 1.0f + e;
-    return 1.0f / d;
+    float largest = 0.0f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const float e = expf(-l[i]);
+        l[i] = 1.0f + e;
+        largest = fmaxf(largest, l[i]);
+    }
+    if (__any(!(largest < 0x1p126f))) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) l[i] = 1.0f / l[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const float r = __builtin_amdgcn_rcpf(l[i]);
+        l[i] = __builtin_fmaf(__builtin_fmaf(-l[i], r, 1.0f), r, r);
+    }
+}
+
+// What an expert of logit l scores in a row whose largest logit is m
+__device__ __forceinline__ float score_of(const RouteArgs &p, float l, float m)
+{
+    if (!p.sigmoid) return expf(l - m);
+    float s[1] = {l};
+    sigmoids(s);
+    return s[0];
 }
 
 // The row's scores: sigmoids, or exponentials with their sum in `total` (NaN where the row has a NaN or +infinity)
 template <int LANES, int VPL>
-__device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, float (&s)[VPL], float &total)
+__device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, float (&s)[VPL], float &total, float &m)
 {
+    // loads past the row's end are loads of its last logit
+    const int64_t row = (int64_t)n * p.stride;
+    if (p.bf16) {
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-        const int e = v * LANES + sub;
-        s[v] = e < p.E ? load_logit(p, (int64_t)n * p.stride + e) : -INFINITY;
+        for (int v = 0; v < VPL; ++v) s[v] = (float)((const __bf16 *)p.logits)[row + min(v * LANES + sub, p.E - 1)];
+    } else {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) s[v] = ((const float *)p.logits)[row + min(v * LANES + sub, p.E - 1)];
     }
     total = 1.0f;
-    if (p.sigmoid) {
-#pragma unroll
-        for (int v = 0; v < VPL; ++v) s[v] = sigmoid_exact(s[v]);
+    m = 0.0f;
+    if (p.sigmoid) {   // an expert that does not exist scores what the last one does, and its key says that it does not exist
+        sigmoids(s);
         return;
     }
-    float m = s[0];
+    if (p.E < LANES * VPL) {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) s[v] = v * LANES + sub < p.E ? s[v] : -INFINITY;
+    }
+    m = s[0];
 #pragma unroll
     for (int v = 1; v < VPL; ++v) m = fmaxf(m, s[v]);
     m = lanes_max<LANES>(m);
@@ -112,71 +145,79 @@ __device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, f
     total = 0.0f;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-        s[v] = expf(s[v] - m);
+        s[v] = score_of(p, s[v], m);
         total += s[v];
     }
     total = lanes_sum<LANES>(total);
 }
 
+// Groups: each one's score, which are kept, and what of that holds for this lane's experts.  `by` holds the row's b, group_score is the
+// row's LDS of FUSCO_MAX_GROUPS entries.
 template <int LANES, int VPL>
-__global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p)
+__device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const float *by, float *group_score, uint32_t (&key)[VPL])
 {
-    constexpr int kRows = kRouteThreads / LANES;
-    __shared__ float scores[kRows][LANES * VPL];          // s
-    __shared__ float by[kRows][LANES * VPL];              // b, where there are groups
-    __shared__ float group_score[kRows][FUSCO_MAX_GROUPS];
-    __shared__ uint8_t group_kept[kRows][FUSCO_MAX_GROUPS];
-    const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
-    const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;   // rows past the end repeat the last one and store nothing
-
-    float s[VPL], total;
-    row_scores<LANES, VPL>(p, n, sub, s, total);
-    uint32_t key[VPL];
-#pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-        const int e = v * LANES + sub;
-        scores[slot][e] = s[v];
-        float b = s[v];
-        if (p.bias && e < p.E) b = (p.sigmoid ? s[v] : s[v] / total) + p.bias[e];
-        key[v] = e < p.E ? score_key(b) : kKeyGone;
-        if (p.groups > 1) by[slot][e] = b;
+    wave_sync();
+    // as many lanes per group as there are, a power of two; each takes every `share`-th expert, begun at another place per group so that
+    // groups of 32 do not meet in one bank
+    int share = 1;
+    while (share * 2 * p.groups <= LANES) share *= 2;
+    const int each = (p.group_size + share - 1) / share;
+    for (int base = 0; base < p.groups; base += LANES / share) {
+        const int g = base + sub / share, h = sub % share;
+        float best = -INFINITY, second = -INFINITY;
+        if (g < p.groups) {
+            int i = g % each;
+#pragma unroll 8
+            for (int n = 0; n < each; ++n) {
+                const int at = i * share + h;
+                const float b = at < p.group_size ? by[g * p.group_size + at] : -INFINITY;
+                second = __builtin_amdgcn_fmed3f(best, second, b);   // a NaN is passed over, here and below
+                best = fmaxf(best, b);
+                i = i + 1 == each ? 0 : i + 1;
+            }
+        }
+        for (int d = 1; d < share; d *= 2) {
+            const float b = __shfl_xor(best, d), s = __shfl_xor(second, d);
+            second = fmaxf(fmaxf(second, s), fminf(best, b));
+            best = fmaxf(best, b);
+        }
+        if (g < p.groups && h == 0) group_score[g] = p.group_best == 2 ? best + second : best;
     }
-    __syncthreads();
-    if (p.groups > 1) {
-        for (int g = sub; g < p.groups; g += LANES) {
-            // the group's largest and second largest b
-            float best = -INFINITY, second = -INFINITY;
-            for (int i = 0; i < p.group_size; ++i) {
-                const float b = by[slot][g * p.group_size + i];
-                if (b > best) {
-                    second = best;
-                    best = b;
-                } else if (b > second) {
-                    second = b;
-                }
-            }
-            group_score[slot][g] = p.group_best == 2 ? best + second : best;
+    wave_sync();
+    uint64_t kept = 0;   // bit g: group g of this lane's row is kept
+    for (int base = 0; base < p.groups; base += LANES) {
+        const int g = base + sub;
+        const uint32_t mine = score_key(g < p.groups ? group_score[g] : 0.0f);
+        int ahead = 0;
+#pragma unroll 8
+        for (int o = 0; o < p.groups; ++o) {
+            const uint32_t other = score_key(group_score[o]);
+            ahead += other > mine || (other == mine && o < g);
         }
-        __syncthreads();
-        for (int g = sub; g < p.groups; g += LANES) {
-            const uint32_t mine = score_key(group_score[slot][g]);
-            int ahead = 0;
-            for (int o = 0; o < p.groups; ++o) {
-                const uint32_t other = score_key(group_score[slot][o]);
-                ahead += other > mine || (other == mine && o < g);
-            }
-            group_kept[slot][g] = ahead < p.keep_groups;
-        }
-        __syncthreads();
+        const uint64_t said = __ballot(g < p.groups && ahead < p.keep_groups);
+        kept |= LANES == 64 ? said : (said >> (threadIdx.x & 48) & 0xffff) << base;
+    }
+    if (p.groups <= 32) {
+        const uint32_t some = (uint32_t)kept;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const int e = v * LANES + sub;
-            if (e < p.E && !group_kept[slot][e / p.group_size]) key[v] = kKeyDropped;
+            const uint32_t e = v * LANES + sub;
+            if (!(some >> (e * p.group_magic >> 20) & 1) && e < (uint32_t)p.E) key[v] = kKeyDropped;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) {
+            const uint32_t e = v * LANES + sub;
+            if (!(kept >> (e * p.group_magic >> 20) & 1) && e < (uint32_t)p.E) key[v] = kKeyDropped;
         }
     }
+}
 
-    // k times the largest key of the row, the lowest expert among equal ones; lane j % LANES keeps the j-th
-    float picked_sum = 0.0f;
+// The j-th chosen expert of the row in lane j (of 64 lanes' j % LANES), one after the other: k times the largest key, the lowest expert among
+// equal ones
+template <int LANES, int VPL>
+__device__ __forceinline__ int choose_in_turn(const RouteArgs &p, int sub, uint32_t (&key)[VPL])
+{
     int mine = 0;
     for (int j = 0; j < p.k; ++j) {
         uint32_t best = key[0];
@@ -193,35 +234,137 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(RouteArgs p)
 #pragma unroll
         for (int v = 0; v < VPL; ++v)
             if ((uint32_t)(v * LANES + sub) == e) key[v] = kKeyGone;
-        picked_sum += scores[slot][e];
-        if (sub == j % LANES) mine = (int)e;
-        if ((j % LANES == LANES - 1 || j == p.k - 1) && sub <= j % LANES && n_real < p.N) p.chosen[(int64_t)n * p.k + j - j % LANES + sub] = mine;
+        if (sub == j) mine = (int)e;
     }
+    return mine;
+}
+
+constexpr int kListed = 32;   // candidates that choose_at_once ranks
+
+template <int by>
+struct RankTurn {
+    // how many of the entries (key, expert) that lie 1 .. by lanes on come before this lane's
+    static __device__ __forceinline__ void count(uint64_t entry, uint64_t others, int &ahead)
+    {
+        const uint64_t o = (uint64_t)turned<by>((uint32_t)(others >> 32)) << 32 | turned<by>((uint32_t)others);
+        ahead += o > entry;
+        if constexpr (by > 1) RankTurn<by - 1>::count(entry, others, ahead);
+    }
+};
+template <int by>
+__device__ __forceinline__ void count_larger(uint32_t m, int &larger)
+{
+    larger += turned<by>(m) > m;
+    if constexpr (by > 1) count_larger<by - 1>(m, larger);
+}
+
+// The same for 16 lanes without k dependent rounds.  The k-th largest of the lanes' largest keys bounds the k-th largest of all from below;
+// what reaches it (about 11 keys of 256 for k = 8) is listed in LDS and ranked, every entry against every other.  False in the whole wave
+// if some row has more than kListed candidates (many equal scores): nothing is chosen then.
+template <int VPL>
+__device__ __forceinline__ bool choose_at_once(const RouteArgs &p, int sub, const uint32_t (&key)[VPL], uint64_t *list, int *order, int &mine)
+{
+    uint32_t m = key[0];
+#pragma unroll
+    for (int v = 1; v < VPL; ++v) m = key[v] > m ? key[v] : m;
+    int larger = 0;
+    count_larger<15>(m, larger);
+    uint32_t bound = lanes_min<16>(larger < p.k ? m : 0xffffffffu);
+    bound = bound < kKeyDropped ? kKeyDropped : bound;
+    int count = 0;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) count += key[v] >= bound;
+    int before = count;   // inclusive sums over the lanes
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+        const int o = __shfl_up(before, d, 16);
+        if (sub >= d) before += o;
+    }
+    const int total = __shfl(before, 15, 16);
+    if (__any(total > kListed)) return false;
+    before -= count;
+    list[sub] = 0;
+    list[sub + 16] = 0;
+    wave_sync();
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+        if (key[v] >= bound) list[before++] = (uint64_t)key[v] << 32 | (uint32_t)~(v * 16 + sub);
+    }
+    wave_sync();
+    const uint64_t first = list[sub];
+    int rank = 0;
+    RankTurn<15>::count(first, first, rank);
+    if (__any(total > 16)) {
+        const uint64_t second = list[sub + 16];
+        int rank2 = 0;
+        RankTurn<15>::count(second, second, rank2);
+        RankTurn<15>::count(second, first, rank2);
+        rank2 += first > second;
+        RankTurn<15>::count(first, second, rank);
+        rank += second > first;
+        if (second != 0 && rank2 < p.k) order[rank2] = (int)~(uint32_t)second;
+    }
+    if (first != 0 && rank < p.k) order[rank] = (int)~(uint32_t)first;
+    wave_sync();
+    mine = order[sub];
+    return true;
+}
+
+template <int LANES, int VPL, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
+{
+    constexpr int kRows = THREADS / LANES, kPitch = LANES * VPL + (LANES == 16 ? 16 : 0);   // rows of a wave begin in different banks
+    __shared__ float by[kRows][kPitch];              // b, where there are groups
+    __shared__ float group_score[kRows][FUSCO_MAX_GROUPS];
+    __shared__ uint64_t list[LANES == 16 ? kRows : 1][kListed];
+    __shared__ int order[LANES == 16 ? kRows : 1][16];
+    const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;   // rows past the end repeat the last one and store nothing
+
+    float s[VPL], total, m;
+    row_scores<LANES, VPL>(p, n, sub, s, total, m);
+    uint32_t key[VPL];
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+        const int e = v * LANES + sub;
+        float b = s[v];
+        if (p.bias) b = (p.sigmoid ? s[v] : s[v] / total) + p.bias[min(e, p.E - 1)];
+        key[v] = e < p.E ? score_key(b) : kKeyGone;
+        if (p.groups > 1) by[slot][e] = b;
+    }
+    if (p.groups > 1) drop_groups<LANES, VPL>(p, sub, by[slot], group_score[slot], key);
+
+    int mine = 0;                                        // lane j has the j-th chosen expert
+    if constexpr (LANES == 16) {
+        if (!choose_at_once<VPL>(p, sub, key, list[slot], order[slot], mine)) mine = choose_in_turn<LANES, VPL>(p, sub, key);
+    } else {
+        mine = choose_in_turn<LANES, VPL>(p, sub, key);
+    }
+
     // weights; a row whose scores are all zero (no expert allowed) has weights 0
-    const float of = p.renorm ? picked_sum : total;
-    for (int j = sub; j < p.k; j += LANES) {
-        if (n_real >= p.N) break;
-        const int e = p.k <= LANES ? mine : p.chosen[(int64_t)n * p.k + j];
-        const float v = p.scale * scores[slot][e];
-        float w = of == 0.0f ? 0.0f : v / of;
-        if (total != total) w = total;
-        p.w[(int64_t)n * p.k + j] = w;
+    const float score = sub < p.k ? score_of(p, load_logit(p, (int64_t)n * p.stride + mine), m) : 0.0f;   // once more, for the chosen alone
+    const float of = p.renorm ? lanes_sum<LANES>(score) : total;
+    float w = of == 0.0f ? 0.0f : p.scale * score / of;
+    if (total != total) w = total;
+    if (n_real < p.N && sub < p.k) {
+        p.chosen[(int64_t)n * p.k + sub] = mine;
+        p.w[(int64_t)n * p.k + sub] = w;
     }
 }
 
 // dlogits of w = scale * s[chosen] / of (of: sum of the chosen s, or 1):
 //   renormalised: ds_j = scale / of * (dw_j - sum_i dw_i s_i / of), otherwise ds_j = scale * dw_j
 //   sigmoid: dl = ds s (1 - s);  softmax: dl = s (ds - sum_i ds_i s_i), where the sum vanishes if the weights are renormalised
-template <int LANES, int VPL>
-__global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(RouteArgs p)
+template <int LANES, int VPL, int THREADS>
+__global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteArgs p)
 {
-    constexpr int kRows = kRouteThreads / LANES;
+    constexpr int kRows = THREADS / LANES;
     __shared__ float scores[kRows][LANES * VPL];
     __shared__ float dscore[kRows][LANES * VPL];
     const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;
-    float s[VPL], total;
-    row_scores<LANES, VPL>(p, n, sub, s, total);
+    float s[VPL], total, m;
+    row_scores<LANES, VPL>(p, n, sub, s, total, m);
     const float inv_total = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
@@ -229,7 +372,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(RouteArgs p)
         scores[slot][v * LANES + sub] = s[v];
         dscore[slot][v * LANES + sub] = 0.0f;
     }
-    __syncthreads();
+    wave_sync();
     float sum_s = 0.0f, sum_ds = 0.0f;   // of the chosen: s, dw * s
     for (int j = sub; j < p.k; j += LANES) {
         const int e = p.chosen[(int64_t)n * p.k + j];
@@ -246,7 +389,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_grad_kernel(RouteArgs p)
         if ((uint32_t)e >= (uint32_t)p.E) continue;
         atomicAdd(&dscore[slot][e], factor * (p.dw[(int64_t)n * p.k + j] - mean));   // chosen experts of a row are distinct: one addition each
     }
-    __syncthreads();
+    wave_sync();
     if (n_real >= p.N) return;
     const float common = p.sigmoid || p.renorm ? 0.0f : factor * sum_ds;
 #pragma unroll
