@@ -71,7 +71,7 @@ constexpr uint32_t kKeyGone = 0, kKeyDropped = 1, kKeyNan = 2;
 __device__ __forceinline__ uint32_t score_key(float b)
 {
     const uint32_t u = __float_as_uint(b);
-    return b != b ? kKeyNan : (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    return b != b ? kKeyNan : u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 __device__ __forceinline__ float load_logit(const RouteArgs &p, int64_t at)
@@ -94,6 +94,7 @@ __device__ __forceinline__ void sigmoids(float (&l)[n])
         largest = fmaxf(largest, l[i]);
     }
     if (__any(!(largest < 0x1p126f))) {
+        asm volatile("");   // rare: not to be worked out beside the other way
 #pragma unroll
         for (int i = 0; i < n; ++i) l[i] = 1.0f / l[i];
         return;
@@ -201,14 +202,14 @@ __device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const f
         const uint32_t some = (uint32_t)kept;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const uint32_t e = v * LANES + sub;
-            if (!(some >> (e * p.group_magic >> 20) & 1) && e < (uint32_t)p.E) key[v] = kKeyDropped;
+            const uint32_t g = (uint32_t)(v * LANES + sub) * p.group_magic >> 20;
+            key[v] = some >> g & 1 ? key[v] : min(key[v], kKeyDropped);
         }
     } else {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const uint32_t e = v * LANES + sub;
-            if (!(kept >> (e * p.group_magic >> 20) & 1) && e < (uint32_t)p.E) key[v] = kKeyDropped;
+            const uint32_t g = (uint32_t)(v * LANES + sub) * p.group_magic >> 20;
+            key[v] = kept >> g & 1 ? key[v] : min(key[v], kKeyDropped);
         }
     }
 }
@@ -295,6 +296,7 @@ __device__ __forceinline__ bool choose_at_once(const RouteArgs &p, int sub, cons
     int rank = 0;
     RankTurn<15>::count(first, first, rank);
     if (__any(total > 16)) {
+        asm volatile("");   // one wave in several
         const uint64_t second = list[sub + 16];
         int rank2 = 0;
         RankTurn<15>::count(second, second, rank2);
@@ -323,14 +325,22 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
 
     float s[VPL], total, m;
     row_scores<LANES, VPL>(p, n, sub, s, total, m);
+    if (p.bias) {
+        float by_total = 1.0f;
+        if (!p.sigmoid) by_total = 1.0f / total;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) s[v] = s[v] * by_total + p.bias[min(v * LANES + sub, p.E - 1)];
+    }
     uint32_t key[VPL];
 #pragma unroll
-    for (int v = 0; v < VPL; ++v) {
-        const int e = v * LANES + sub;
-        float b = s[v];
-        if (p.bias) b = (p.sigmoid ? s[v] : s[v] / total) + p.bias[min(e, p.E - 1)];
-        key[v] = e < p.E ? score_key(b) : kKeyGone;
-        if (p.groups > 1) by[slot][e] = b;
+    for (int v = 0; v < VPL; ++v) key[v] = score_key(s[v]);
+    if (p.E < LANES * VPL) {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) key[v] = v * LANES + sub < p.E ? key[v] : kKeyGone;
+    }
+    if (p.groups > 1) {
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) by[slot][v * LANES + sub] = s[v];
     }
     if (p.groups > 1) drop_groups<LANES, VPL>(p, sub, by[slot], group_score[slot], key);
 
