@@ -128,22 +128,33 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(NormGradArgs p)
             if (AFTER) dgain[c].v[i] = 0.0f;
             if (GATE_CHANNEL) dgate[c].v[i] = 0.0f;
         }
-    for (int n = blockIdx.x; n < p.N; n += gridDim.x) {
-        const size_t row = (size_t)n * p.chunks;
-        RawEight<STREAM_BF16> rd[CPT], ro[CPT];
-        RawEight<BLOCK_BF16> rn[CPT], ry[CPT];
+    RawEight<STREAM_BF16> rd[CPT], ro[CPT], rd_next[CPT], ro_next[CPT];
+    RawEight<BLOCK_BF16> rn[CPT], ry[CPT], rn_next[CPT], ry_next[CPT];
+    auto ask = [&](int n) {   // a row's loads, a row ahead of their use: the waits of the sums then cost no bandwidth
 #pragma unroll
         for (int c = 0; c < CPT; ++c) {
             const int at = c * blockDim.x + threadIdx.x;
             if (at >= p.chunks) continue;
-            const size_t el = (row + at) * kEight;
+            const size_t el = ((size_t)n * p.chunks + at) * kEight;
             if (NEXT) {
-                rn[c] = load_raw<BLOCK_BF16>(p.dnext, el);
-                ro[c] = load_raw<STREAM_BF16>(p.out, el);
+                rn_next[c] = load_raw<BLOCK_BF16>(p.dnext, el);
+                ro_next[c] = load_raw<STREAM_BF16>(p.out, el);
             }
-            if (AFTER) ry[c] = load_raw<BLOCK_BF16>(p.y, el);
-            if (p.dout) rd[c] = load_raw<STREAM_BF16>(p.dout, el);
+            if (AFTER) ry_next[c] = load_raw<BLOCK_BF16>(p.y, el);
+            if (p.dout) rd_next[c] = load_raw<STREAM_BF16>(p.dout, el);
         }
+    };
+    if ((int)blockIdx.x < p.N) ask(blockIdx.x);
+    for (int n = blockIdx.x; n < p.N; n += gridDim.x) {
+        const size_t row = (size_t)n * p.chunks;
+#pragma unroll
+        for (int c = 0; c < CPT; ++c) {
+            rd[c] = rd_next[c];
+            ro[c] = ro_next[c];
+            rn[c] = rn_next[c];
+            ry[c] = ry_next[c];
+        }
+        if (n + (int)gridDim.x < p.N) ask(n + gridDim.x);
         float s[3] = {0.0f, 0.0f, 0.0f};   // out^2, g2 * out, y^2
 #pragma unroll
         for (int c = 0; c < CPT; ++c) {
@@ -243,20 +254,23 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(NormGradArgs p)
 
 constexpr int kJoinThreads = 256, kJoinCols = 64;
 
-// total[s][h] = sum over the groups of partial[g][s][h]: four waves take every fourth group each, in ascending order
+// total[s][h] = sum over the groups of partial[g][s][h]: 16 threads share a column and take every 16th group each, in ascending order
 __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(const float *partial, int groups, int sums, int H, float *a, float *b, float *c)
 {
-    __shared__ float part[kJoinThreads];
-    const int col = blockIdx.x * kJoinCols + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+    constexpr int kShare = kJoinThreads / (kJoinCols / 4);
+    __shared__ rows_f32x4 part[kShare][kJoinCols / 4];
+    const int quad = threadIdx.x % (kJoinCols / 4), share = threadIdx.x / (kJoinCols / 4), col = blockIdx.x * kJoinCols + quad * 4;
     const int s = blockIdx.y;
-    float v = 0.0f;
-    if (col < H)
-        for (int g = wave; g < groups; g += kJoinThreads / kJoinCols) v += partial[((size_t)g * sums + s) * H + col];
-    part[threadIdx.x] = v;
+    rows_f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < H) {
+#pragma unroll 8
+        for (int g = share; g < groups; g += kShare) v += *(const rows_f32x4 *)(partial + ((size_t)g * sums + s) * H + col);
+    }
+    part[share][quad] = v;
     __syncthreads();
-    if (wave != 0 || col >= H) return;
-    for (int w = 1; w < kJoinThreads / kJoinCols; ++w) v += part[w * kJoinCols + threadIdx.x];
-    (s == 0 ? a : s == 1 ? b : c)[col] = v;
+    if (share != 0 || col >= H) return;
+    for (int w = 1; w < kShare; ++w) v += part[w][quad];
+    *(rows_f32x4 *)((s == 0 ? a : s == 1 ? b : c) + col) = v;
 }
 
 }   // namespace

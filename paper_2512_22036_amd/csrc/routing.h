@@ -9,7 +9,7 @@
 #ifndef FUSCO_CSRC_ROUTING_H
 #define FUSCO_CSRC_ROUTING_H
 
-#include "common.h"
+#include "rows.h"
 
 namespace {
 
@@ -25,13 +25,6 @@ struct RouteArgs {
     int32_t bf16, sigmoid, renorm;
     float scale;
 };
-
-// Values of the lanes `by` places on in the row of 16 lanes, round and round: no LDS, one instruction
-template <int by>
-__device__ __forceinline__ uint32_t turned(uint32_t v)
-{
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + by, 0xf, 0xf, true);
-}
 
 // Reductions over the LANES lanes of a row, in all of them
 template <int LANES, typename T, typename F>

@@ -87,11 +87,28 @@ __device__ __forceinline__ void store_eight(char *p, size_t element, const Eight
     }
 }
 
+// Values of the lanes `by` places on in the row of 16 lanes, round and round: no LDS, one instruction
+template <int by>
+__device__ __forceinline__ uint32_t turned(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + by, 0xf, 0xf, true);
+}
+
+// Sums over 16 neighbouring lanes and over the wave, in all of their lanes
+__device__ __forceinline__ float sixteen_sum(float v)
+{
+    v += __uint_as_float(turned<8>(__float_as_uint(v)));
+    v += __uint_as_float(turned<4>(__float_as_uint(v)));
+    v += __uint_as_float(turned<2>(__float_as_uint(v)));
+    v += __uint_as_float(turned<1>(__float_as_uint(v)));
+    return v;
+}
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int d = 32; d >= 1; d /= 2) v += __shfl_xor(v, d);
-    return v;
+    const int s = (int)__float_as_uint(sixteen_sum(v));
+    const float a = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(s, 0)), b = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(s, 16));
+    const float c = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(s, 32)), d = __uint_as_float((uint32_t)__builtin_amdgcn_readlane(s, 48));
+    return (a + b) + (c + d);
 }
 
 constexpr int kMaxWaves = 16;   // of a workgroup
@@ -111,11 +128,7 @@ __device__ __forceinline__ void group_sums(float (&v)[n], float *part, int waves
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-        float s = 0.0f;
-        for (int w = 0; w < waves; ++w) s += part[i * kMaxWaves + w];
-        v[i] = s;
-    }
+    for (int i = 0; i < n; ++i) v[i] = sixteen_sum((lane & 15) < waves ? part[i * kMaxWaves + (lane & 15)] : 0.0f);
 }
 
 }   // namespace
