@@ -189,6 +189,8 @@ def _bind_fastcall(lib):
         return None
     _fastcall.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
                      for name in ("fusco_plan", "fusco_dispatch", "fusco_plan_dispatch", "fusco_combine", "fusco_combine_two_hop")))
+    _fastcall.bind_block(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
+                           for name in ("fusco_route", "fusco_norm_before", "fusco_norm_after", "fusco_experts_gated", "fusco_experts_linear")))
     return _fastcall
 
 
@@ -422,6 +424,10 @@ def fusco_route(logits: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, b
                 scale: float = 1.0, stream=None) -> None:
     """Routing: logits [N, E] (bfloat16 or float32, rows may lie apart) to topk_idx [N, k] int32 and w [N, k] float32, as
     fusco_plan and fusco_combine take them.  bias: float32 [E], added to the scores for the choice alone."""
+    if stream is None and _fast is not None:
+        rc = _fast.route(logits, topk_idx, w, bias, score, groups, keep_groups, group_best, renorm, scale)
+        if rc is not None:
+            return _check(rc, "fusco_route")
     R = _router(logits, topk_idx, score, groups, keep_groups, group_best, renorm, scale)
     _fp32(w, "w", topk_idx.shape)
     if bias is not None:
@@ -475,6 +481,10 @@ def _like(n: _CNorm, dtype: torch.dtype, **tensors) -> None:
 
 def fusco_norm_before(x: torch.Tensor, gain: torch.Tensor, out: torch.Tensor, eps: float = 1e-6, stream=None) -> None:
     """out = x / sqrt(mean(x^2) + eps) * gain, row by row: the norm before a block; x is the residual stream."""
+    if stream is None and _fast is not None:
+        rc = _fast.norm_before(x, gain, out, eps)
+        if rc is not None:
+            return _check(rc, "fusco_norm_before")
     n = _norm(x, out.dtype, [("gain", gain)], None, None, 1.0, eps)
     _like(n, out.dtype, out=out)
     _check(load_library().fusco_norm_before(ctypes.byref(n), x.data_ptr(), gain.data_ptr(), out.data_ptr(), _stream(stream)),
@@ -487,6 +497,10 @@ def fusco_norm_after(r: torch.Tensor, y: torch.Tensor, gain: torch.Tensor, out: 
     """out = r + scale * gate * norm(y) * gain: the norm after a block, its gate and the sum with the residual stream r; with
     next_out also the norm before the next block, norm(out) * next_gain.  gate: [H] (per channel) or [N] (per token);
     gate_kind says which where N == H."""
+    if stream is None and _fast is not None:
+        rc = _fast.norm_after(r, y, gain, out, gate, scale, next_gain, next_out, eps, gate_kind)
+        if rc is not None:
+            return _check(rc, "fusco_norm_after")
     if (next_gain is None) != (next_out is None):
         raise FuscoError("next_gain and next_out go together")
     n = _norm(r, y.dtype, [("gain", gain), ("next_gain", next_gain)], gate, gate_kind, scale, eps)
@@ -569,6 +583,10 @@ def fusco_experts_gated(layout: Layout, x: torch.Tensor, w: torch.Tensor, h: tor
                         stream=None) -> None:
     """h = silu(x Wg^T) * (x Wu^T), expert by expert: x [P, H] as fusco_dispatch wrote it, w [E, 2 I, H] with the gate rows
     first, h [P, I], all bfloat16.  pre [P, 2 I]: also keep both factors before the activation, for the gradient."""
+    if stream is None and _fast is not None:
+        rc = _fast.experts_gated(layout, x, w, h, pre)
+        if rc is not None:
+            return _check(rc, "fusco_experts_gated")
     _weights(layout, w, "w")
     I, H = w.shape[1] // 2, w.shape[2]
     if w.shape[1] % 2:
@@ -583,6 +601,10 @@ def fusco_experts_gated(layout: Layout, x: torch.Tensor, w: torch.Tensor, h: tor
 
 def fusco_experts_linear(layout: Layout, x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, stream=None) -> None:
     """y = x W^T, expert by expert: x [P, C], w [E, M, C], y [P, M], all bfloat16."""
+    if stream is None and _fast is not None:
+        rc = _fast.experts_linear(layout, x, w, y)
+        if rc is not None:
+            return _check(rc, "fusco_experts_linear")
     _weights(layout, w, "w")
     M, C = w.shape[1], w.shape[2]
     _bf16(x, "x", (layout.P, C))
