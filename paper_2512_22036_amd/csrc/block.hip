@@ -36,14 +36,14 @@ int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
     constexpr int kF = 2, kUnits = STORE == kStoreGated ? 8 * kF : 16 * kF;
     const int64_t blocks = (a.NA + kUnits - 1) / kUnits, spread = L->P / 16 + L->E, tiles = spread < L->P ? spread : L->P;
-    if (tiles * blocks > (int64_t)1 << 30) return FUSCO_ERR_INVALID_ARG;
     hipLaunchKernelGGL((few_rows_kernel<kF, WAVES, STORE>), dim3((unsigned)(tiles * blocks)), dim3(WAVES * kWave), 0, s, a);
     return launch_status();
 }
 
 // Products whose tiles are rows of one expert: the tile's height goes by the mean number of rows of an expert.  Measured, 128 experts of
-// 4096 x (2 x 1280) gated and 1280 x 4096, us, few / 64 / 128 / 256:  mean 4: 442 / 441 / - / -, 8: 482 / 453 / 531 / 591, 32: - / 488 / 535 / 601,
-// 64: - / 671 / 574 / 619, 128: - / 996 / 826 / 703.
+// 4096 x (2 x 1280) gated, us, few / 64 / 128 / 256:  mean 4: 437 / 441 / - / -, 8: 482 / 455 / 531 / 591, 32: - / 476 / 535 / 601,
+// 64: - / 671 / 511 / 619, 128: - / 996 / 826 / 601.  Input gradient of 64 experts with 512 uneven rows, 2816 x 2048: 656 / 477 / 450 with 64 / 128 /
+// 256.
 template <int AMODE, int STORE>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {

@@ -37,7 +37,9 @@ struct ProductArgs {
     int32_t E, NA, NB, C;              // NA: outputs along a (gated forward: units); NB, C: weight gradient has NB outputs along b, others sum over C
 };
 
-__device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+// 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal, a few units in the last place of fp32: results are rounded to bf16
+__device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
+__device__ __forceinline__ float silu(float g) { return g * sigmoid(g); }
 
 // The bounds-checked view of `bytes` bytes from p: loads outside give zeros
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t view(const char *p, int64_t bytes)
@@ -320,8 +322,14 @@ __device__ __forceinline__ void store4(char *out, int64_t element, f32x4 v)
     *(bf16x4 *)(out + element * 2) = o;
 }
 
+__device__ __forceinline__ bf16x8 load_fragment(__amdgpu_buffer_rsrc_t from, uint32_t offset)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(bf16x8, (words)__builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0));
+}
+
 // Exclusive prefix sums of the experts' tile counts, [E + 1] ints in LDS
-__device__ __forceinline__ void tile_prefix(const int32_t *__restrict__ exp_off, int E, int BB, int *__restrict__ prefix, int *__restrict__ part)
+__device__ __forceinline__ void tile_prefix(const int *__restrict__ exp_off, int E, int BB, int *__restrict__ prefix, int *__restrict__ part)
 {
     static_assert(FUSCO_MAX_E <= 2 * kTileThreads, "two experts per thread");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = 2 * tid;
@@ -368,10 +376,12 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
     __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[kMore], slot3[kMore];
-    __shared__ int prefix[FUSCO_MAX_E + 1];
+    __shared__ int offsets[FUSCO_MAX_E + 1], prefix[kByRows ? FUSCO_MAX_E + 1 : 1];
     __shared__ int part[kTileThreads / kWave];
 
     const int tid = threadIdx.x, lane = tid & 63;
+    for (int e = tid; e <= p.E; e += kTileThreads) offsets[e] = p.exp_off[e];
+    __syncthreads();
     // Where a slot is written and read from is hidden from the compiler: as long as it cannot tell one place in a slot from another, it lets
     // reads wait for the loads to their slot; where it could, it would let them wait for all loads.
     int hidden = tid >> 6;
@@ -382,7 +392,7 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     const int tiles_b = kByRows ? 0 : (p.NB + BB - 1) / BB;
     int total;
     if (kByRows) {
-        tile_prefix(p.exp_off, p.E, BB, prefix, part);
+        tile_prefix(offsets, p.E, BB, prefix, part);
         total = prefix[p.E] * tiles_a;
     } else {
         total = p.E * tiles_a * tiles_b;
@@ -424,8 +434,8 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
             at -= g * kGroupB * tiles_a;
             ta = at / wide;
             tb = g * kGroupB + at % wide;
-            first = __builtin_amdgcn_readfirstlane(p.exp_off[e]);
-            rows = __builtin_amdgcn_readfirstlane(p.exp_off[e + 1]) - first;
+            first = __builtin_amdgcn_readfirstlane(offsets[e]);
+            rows = __builtin_amdgcn_readfirstlane(offsets[e + 1]) - first;
         }
         a0 = ta * kUnitsA;
         const int b0 = tb * BB;
@@ -496,13 +506,25 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
         const int rows = b_left < BB ? b_left : BB;
         Target out, pre;
         out.open(p.out, row0, (int64_t)p.NA * (STORE == kStoreGatedGrad ? 2 : 1) * kSize, (int64_t)a0 * kSize, rows);
-        if (kGated && p.pre) pre.open(p.pre, row0, (int64_t)p.NA * 2 * kSize, (int64_t)a0 * kSize, rows);
+        if ((kGated && p.pre) || STORE == kStoreGatedGrad) pre.open(p.pre, row0, (int64_t)p.NA * 2 * kSize, (int64_t)a0 * kSize, rows);
         const uint32_t second = (uint32_t)p.NA * kSize;
         int lane = tid & 63;
         asm volatile("" : "+v"(lane));   // places are worked out here, not kept in registers over the sums
 #pragma unroll
         for (int j = 0; j < FB; ++j) {
             const int b = (wb * FB + j) * 32 + (lane & 31);
+            bf16x8 gates[STORE == kStoreGatedGrad ? kOutA : 1][2], ups[STORE == kStoreGatedGrad ? kOutA : 1][2];
+            if constexpr (STORE == kStoreGatedGrad) {   // all pre-activations at once, not one after the other
+#pragma unroll
+                for (int f = 0; f < kOutA; ++f)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16 + h * 8;
+                        const uint32_t at = a < a_left && b < b_left ? b * out.ld + a * kSize : kNowhere;
+                        gates[f][h] = load_fragment(pre.to, at);
+                        ups[f][h] = load_fragment(pre.to, at + second);
+                    }
+            }
 #pragma unroll
             for (int f = 0; f < kOutA; ++f) {
 #pragma unroll
@@ -531,17 +553,12 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
                         for (int q = 0; q < 8; ++q) v[q] = silu(v[q]) * up[q];
                         out.put8(v, at);
                     } else {
-                        bf16x8 gate, up;
-                        if (in) {
-                            gate = *(const bf16x8 *)(p.pre + ((row0 + b) * 2 * p.NA + a0 + a) * 2);
-                            up = *(const bf16x8 *)(p.pre + (((row0 + b) * 2 + 1) * p.NA + a0 + a) * 2);
-                        }
                         float dup[8];
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            const float g = (float)gate[q], sig = 1.0f / (1.0f + __expf(-g));
+                            const float g = (float)gates[f][h][q], sig = sigmoid(g);
                             dup[q] = v[q] * g * sig;
-                            v[q] = v[q] * (float)up[q] * sig * (1.0f + g * (1.0f - sig));
+                            v[q] = v[q] * (float)ups[f][h][q] * sig * (1.0f + g * (1.0f - sig));
                         }
                         out.put8(v, at);
                         out.put8(dup, at + second);
@@ -642,12 +659,6 @@ struct FewTile {
         return e >= 0;
     }
 };
-
-__device__ __forceinline__ bf16x8 load_fragment(__amdgpu_buffer_rsrc_t from, uint32_t offset)
-{
-    typedef uint32_t words __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(bf16x8, (words)__builtin_amdgcn_raw_buffer_load_b128(from, (int)offset, 0, 0));
-}
 
 template <int F, int WAVES, int STORE>
 __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
