@@ -81,13 +81,17 @@ void with_cpt(int cpt, F f)
     else f(std::integral_constant<int, 4>());
 }
 
-// calls f(stream is bf16, block is bf16) for the pairs of types that are offered
+// calls f(stream is bf16, block is bf16, loads go past the caches) for the pairs of types that are offered.  Rows of bf16 go past the caches if
+// the call's tensors exceed the memory-side cache, rows of fp32, whose two halves a thread loads one after the other, never.  Norm after a
+// block, past / through, us: 16384 x 4096 bf16 102.6 / 105.8, 512 x 7168 6.7 / 5.8; with an fp32 stream 8192 x 7168 148 / 139, 1537 x 2880
+// 13.8 / 10.1; gradients 8192 x 7168 with an fp32 stream 252 / 234.
 template <typename F>
-void with_types(const fusco_norm *n, F f)
+void with_types(const fusco_norm *n, int64_t bytes_per_element, F f)
 {
-    if (n->stream_dtype == FUSCO_BF16) f(std::true_type(), std::true_type());
-    else if (n->block_dtype == FUSCO_BF16) f(std::false_type(), std::true_type());
-    else f(std::false_type(), std::false_type());
+    if (n->stream_dtype == FUSCO_BF16 && bytes_per_element * n->N * n->H > kCacheBytes) f(std::true_type(), std::true_type(), std::true_type());
+    else if (n->stream_dtype == FUSCO_BF16) f(std::true_type(), std::true_type(), std::false_type());
+    else if (n->block_dtype == FUSCO_BF16) f(std::false_type(), std::true_type(), std::false_type());
+    else f(std::false_type(), std::false_type(), std::false_type());
 }
 
 int norm_check(const fusco_norm *n)
@@ -121,8 +125,8 @@ int launch_norm(const fusco_norm *n, const NormArgs &a, hipStream_t s)
 {
     const int cpt = row_cpt(a.chunks, n->N < 1024);
     const dim3 grid((unsigned)n->N), block(row_threads(a.chunks, cpt));
-    with_types(n, [&](auto st, auto bl) {
-        with_cpt(cpt, [&](auto c) { hipLaunchKernelGGL((norm_kernel<decltype(st)::value, decltype(bl)::value, decltype(c)::value, AFTER>), grid, block, 0, s, a); });
+    with_types(n, AFTER ? 8 : 4, [&](auto st, auto bl, auto past) {
+        with_cpt(cpt, [&](auto c) { hipLaunchKernelGGL((norm_kernel<decltype(st)::value, decltype(bl)::value, decltype(c)::value, decltype(past)::value, AFTER>), grid, block, 0, s, a); });
     });
     return launch_status();
 }
@@ -131,10 +135,10 @@ template <bool AFTER, bool NEXT, bool CHANNEL>
 void launch_norm_grad(const fusco_norm *n, const NormGradArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)norm_groups(n->N, n->H)), block(row_threads(a.chunks, grad_cpt(a.chunks)));
-    with_types(n, [&](auto st, auto bl) {
-        constexpr bool kS = decltype(st)::value, kB = decltype(bl)::value;
-        if (grad_cpt(a.chunks) == 1) hipLaunchKernelGGL((norm_grad_kernel<kS, kB, 1, AFTER, NEXT, CHANNEL>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((norm_grad_kernel<kS, kB, 4, AFTER, NEXT, CHANNEL>), grid, block, 0, s, a);
+    with_types(n, (NEXT ? 4 : 0) + (AFTER ? 4 : 0) + 4, [&](auto st, auto bl, auto past) {
+        constexpr bool kS = decltype(st)::value, kB = decltype(bl)::value, kPast = decltype(past)::value;
+        if (grad_cpt(a.chunks) == 1) hipLaunchKernelGGL((norm_grad_kernel<kS, kB, 1, kPast, AFTER, NEXT, CHANNEL>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((norm_grad_kernel<kS, kB, 4, kPast, AFTER, NEXT, CHANNEL>), grid, block, 0, s, a);
     });
 }
 
@@ -340,12 +344,19 @@ int fusco_combine_backward(const fusco_layout *L, const void *d_y, int y_dtype, 
     const CombineGradArgs a = {L->pair_slot, (const char *)d_y, (const char *)d_dout, d_w, (char *)d_dy, d_dw, L->N, L->k, H / kEight};
     const int cpt = row_cpt(a.chunks, L->N < 1024);
     const dim3 grid((unsigned)L->N), block(row_threads(a.chunks, cpt));
+    // tensors that the memory-side cache cannot hold are read past it: 16384 x 8 x 8 KiB 448 us / 455 through it, 1537 x 6 x 5760 B 25.9 / 20.9
+    const int64_t y_bytes = y_dtype == FUSCO_BF16 ? 2 : 4, bytes = ((int64_t)2 * L->P * y_bytes + (int64_t)L->N * (dout_dtype == FUSCO_BF16 ? 2 : 4)) * H;
     with_cpt(cpt, [&](auto c) {
         constexpr int kCpt = decltype(c)::value, kJu = kCpt == 4 ? 2 : 4;
-        if (y_dtype == FUSCO_BF16 && dout_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<true, true, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
-        else if (y_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<true, false, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
-        else if (dout_dtype == FUSCO_BF16) hipLaunchKernelGGL((combine_grad_kernel<false, true, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
-        else hipLaunchKernelGGL((combine_grad_kernel<false, false, kCpt, kJu>), grid, block, 0, (hipStream_t)stream, a);
+        auto go = [&](auto y, auto dout) {
+            constexpr bool kY = decltype(y)::value, kD = decltype(dout)::value;
+            if (bytes > kCacheBytes) hipLaunchKernelGGL((combine_grad_kernel<kY, kD, kCpt, kJu, true>), grid, block, 0, (hipStream_t)stream, a);
+            else hipLaunchKernelGGL((combine_grad_kernel<kY, kD, kCpt, kJu, false>), grid, block, 0, (hipStream_t)stream, a);
+        };
+        if (y_dtype == FUSCO_BF16 && dout_dtype == FUSCO_BF16) go(std::true_type(), std::true_type());
+        else if (y_dtype == FUSCO_BF16) go(std::true_type(), std::false_type());
+        else if (dout_dtype == FUSCO_BF16) go(std::false_type(), std::true_type());
+        else go(std::false_type(), std::false_type());
     });
     return launch_status();
 }

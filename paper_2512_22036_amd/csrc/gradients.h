@@ -18,7 +18,7 @@ struct CombineGradArgs {
 };
 
 // CPT chunks of eight elements per thread, rows of y taken JU at a time
-template <bool Y_BF16, bool DOUT_BF16, int CPT, int JU>
+template <bool Y_BF16, bool DOUT_BF16, int CPT, int JU, bool PAST>
 __global__ __launch_bounds__(1024) void combine_grad_kernel(CombineGradArgs p)
 {
     __shared__ float part[FUSCO_MAX_K][kMaxWaves];
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(1024) void combine_grad_kernel(CombineGradArgs p)
 #pragma unroll
     for (int c = 0; c < CPT; ++c) {
         const int at = c * blockDim.x + threadIdx.x;
-        if (at < p.chunks) d[c] = wide(load_raw<DOUT_BF16>(p.dout, ((size_t)t * p.chunks + at) * kEight));
+        if (at < p.chunks) d[c] = wide(load_raw<DOUT_BF16, PAST>(p.dout, ((size_t)t * p.chunks + at) * kEight));
     }
     for (int j0 = 0; j0 < p.k; j0 += JU) {
         RawEight<Y_BF16> y[JU][CPT];
@@ -42,7 +42,7 @@ __global__ __launch_bounds__(1024) void combine_grad_kernel(CombineGradArgs p)
 #pragma unroll
             for (int c = 0; c < CPT; ++c) {
                 const int at = c * blockDim.x + threadIdx.x;
-                if (at < p.chunks) y[u][c] = load_raw<Y_BF16>(p.y, ((size_t)slot[u] * p.chunks + at) * kEight);
+                if (at < p.chunks) y[u][c] = load_raw<Y_BF16, PAST>(p.y, ((size_t)slot[u] * p.chunks + at) * kEight);
             }
         }
 #pragma unroll

@@ -22,7 +22,7 @@ struct NormArgs {
 };
 
 // CPT chunks per thread: thread i has the chunks i, i + blockDim, ...
-template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool AFTER>
+template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool PAST, bool AFTER>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs p)
 {
     __shared__ float part[2][kMaxWaves];
@@ -37,8 +37,8 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs p)
         for (int c = 0; c < CPT; ++c) {
             const int at = c * blockDim.x + threadIdx.x;
             if (at >= p.chunks) continue;
-            ry[c] = load_raw<BLOCK_BF16>(p.y, (row + at) * kEight);
-            rr[c] = load_raw<STREAM_BF16>(p.r, (row + at) * kEight);
+            ry[c] = load_raw<BLOCK_BF16, PAST>(p.y, (row + at) * kEight);
+            rr[c] = load_raw<STREAM_BF16, PAST>(p.r, (row + at) * kEight);
         }
         sums[0] = 0.0f;
 #pragma unroll
@@ -76,7 +76,7 @@ __global__ __launch_bounds__(1024) void norm_kernel(NormArgs p)
         for (int c = 0; c < CPT; ++c) {
             const int at = c * blockDim.x + threadIdx.x;
             if (at >= p.chunks) continue;
-            r[c] = wide(load_raw<STREAM_BF16>(p.r, (row + at) * kEight));
+            r[c] = wide(load_raw<STREAM_BF16, PAST>(p.r, (row + at) * kEight));
         }
 #pragma unroll
         for (int c = 0; c < CPT; ++c) {
@@ -114,7 +114,7 @@ struct NormGradArgs {
     float scale, eps, inv_h;
 };
 
-template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool AFTER, bool NEXT, bool GATE_CHANNEL>
+template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool PAST, bool AFTER, bool NEXT, bool GATE_CHANNEL>
 __global__ __launch_bounds__(1024) void norm_grad_kernel(NormGradArgs p)
 {
     __shared__ float part[2][3 * kMaxWaves];
@@ -137,11 +137,11 @@ __global__ __launch_bounds__(1024) void norm_grad_kernel(NormGradArgs p)
             if (at >= p.chunks) continue;
             const size_t el = ((size_t)n * p.chunks + at) * kEight;
             if (NEXT) {
-                rn_next[c] = load_raw<BLOCK_BF16>(p.dnext, el);
-                ro_next[c] = load_raw<STREAM_BF16>(p.out, el);
+                rn_next[c] = load_raw<BLOCK_BF16, PAST>(p.dnext, el);
+                ro_next[c] = load_raw<STREAM_BF16, PAST>(p.out, el);
             }
-            if (AFTER) ry_next[c] = load_raw<BLOCK_BF16>(p.y, el);
-            if (p.dout) rd_next[c] = load_raw<STREAM_BF16>(p.dout, el);
+            if (AFTER) ry_next[c] = load_raw<BLOCK_BF16, PAST>(p.y, el);
+            if (p.dout) rd_next[c] = load_raw<STREAM_BF16, PAST>(p.dout, el);
         }
     };
     if ((int)blockIdx.x < p.N) ask(blockIdx.x);

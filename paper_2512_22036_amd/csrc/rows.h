@@ -6,6 +6,7 @@
 
 namespace {
 
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;   // the memory-side cache
 constexpr int kEight = 8;   // elements per thread and access: 16 bytes of bf16, two times 16 bytes of fp32
 
 typedef __bf16 rows_bf16x8 __attribute__((ext_vector_type(8)));
@@ -26,15 +27,18 @@ struct RawEight<false> {
     rows_f32x4 a, b;
 };
 
-template <bool BF16>
+// PAST: past the caches, for tensors that they cannot hold (kCacheBytes); otherwise rows that were just written are read from there
+template <bool BF16, bool PAST>
 __device__ __forceinline__ RawEight<BF16> load_raw(const char *p, size_t element)
 {
     RawEight<BF16> r;
     if constexpr (BF16) {
-        r.a = __builtin_nontemporal_load((const rows_bf16x8 *)(p + element * 2));
+        const rows_bf16x8 *at = (const rows_bf16x8 *)(p + element * 2);
+        r.a = PAST ? __builtin_nontemporal_load(at) : *at;
     } else {
-        r.a = __builtin_nontemporal_load((const rows_f32x4 *)(p + element * 4));
-        r.b = __builtin_nontemporal_load((const rows_f32x4 *)(p + element * 4 + 16));
+        const rows_f32x4 *at = (const rows_f32x4 *)(p + element * 4);
+        r.a = PAST ? __builtin_nontemporal_load(at) : at[0];
+        r.b = PAST ? __builtin_nontemporal_load(at + 1) : at[1];
     }
     return r;
 }
