@@ -134,6 +134,9 @@ struct TileState {
     int wave;
     int stages, turn;
 
+    // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
+    __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots - 1) / kSlots : 1; }
+
     // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one loads fetch nothing, but they are made, so that
     // the number of loads behind a stage is always the same
     __device__ __forceinline__ int stage_of(int s) const
@@ -179,7 +182,7 @@ __device__ __forceinline__ void read_after(const S &t, const char *slot, uint32_
 }
 
 template <bool ACTIVE, int STORES, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nxt, int s, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nxt, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
 {
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
     asm volatile("" : "+v"(a_at), "+v"(b_at));   // fragments' places are worked out where they are used, not kept in registers over the loop
@@ -191,102 +194,38 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (!ACTIVE && !last) continue;
         const int next = (ks + 1) % S::kSlices;
-        if (ACTIVE) {
 #pragma unroll
-            for (int m = 0; m < FA * FB; ++m) {
-                acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % 2].a[m / FB], x[ks % 2].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
-                read_after(t, last ? nxt : cur, a_at, b_at, next, m, x[next % 2]);
-                if (last) {              // loads behind the last matrix instructions
-                    constexpr int kEach = (S::kLoads + FA * FB - 1) / (FA * FB), kBegin = FA * FB - S::kLoads / kEach;
+        for (int m = 0; m < FA * FB; ++m) {
+            if (ACTIVE) acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % 2].a[m / FB], x[ks % 2].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
+            read_after(t, last ? nxt : cur, a_at, b_at, next, m, x[next % 2]);
+            if (last) {                  // loads behind the last matrix instructions
+                constexpr int kEach = (S::kLoads + FA * FB - 1) / (FA * FB), kBegin = FA * FB - S::kLoads / kEach;
 #pragma unroll
-                    for (int i = 0; i < kEach; ++i)
-                        if (m >= kBegin) t.load(s + S::kSlots, (m - kBegin) * kEach + i, cur);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < kEach; ++i)
+                    if (m >= kBegin) t.load(ask, (m - kBegin) * kEach + i, cur);
             }
-        } else if (last) {
-#pragma unroll
-            for (int i = 0; i < S::kLoads; ++i) t.load(s + S::kSlots, i, cur);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
 }
 
-template <typename S>
-__device__ __forceinline__ void tile_begin(const S &t, char *slot0, char *slot1, char *slot2, char *slot3)
-{
-#pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) t.load(0, i, slot0);
-#pragma unroll
-    for (int i = 0; i < S::kLoads; ++i) t.load(1, i, slot1);
-    if constexpr (S::kSlots == 4) {
-#pragma unroll
-        for (int i = 0; i < S::kLoads; ++i) t.load(2, i, slot2);
-#pragma unroll
-        for (int i = 0; i < S::kLoads; ++i) t.load(3, i, slot3);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// The sums of a tile whose first stages are under way; after them STORES stores at least were issued (the outputs of the tile before), which
-// the first stages do not wait for.  The slots are arrays of their own: the compiler then knows that a fragment's read waits for
-// its own slot's loads only.
+// One turn through the slots, while stage ask, ask + 1, ... of this tile or the next are asked for.  STORES: stores that were issued after
+// the loads of the stages that are under way, which the turn need not wait for.  The slots are arrays of their own: the compiler then
+// knows that a fragment's read waits for its own slot's loads only.
 template <bool ACTIVE, int STORES, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_sum(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, f32x16 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_turn(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
 {
-    if (t.stages == 0) return;
-    t.template wait<S::kSlots - 1, STORES>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    Slice<FA, FB> x[2];
-    if (ACTIVE) {
-#pragma unroll
-        for (int m = 0; m < FA * FB; ++m) read_after(t, slot0, t.a_lane, t.b_lane, 0, m, x[0]);
-    }
-#define FUSCO_STAGE(n, cur, nxt, stores) tile_stage<ACTIVE, stores>(t, cur, nxt, s + (n), x, acc)
-    // Whole turns through the slots, then what is left.  The loop has one way out: at the head of one with several the compiler would
-    // take loads of the present turn to be still under way.
-    int s = 0;
-    const int whole = t.stages & ~(S::kSlots - 1);
     if constexpr (S::kSlots == 2) {
-        if (whole > 0) {
-            FUSCO_STAGE(0, slot0, slot1, STORES);
-            FUSCO_STAGE(1, slot1, slot0, 0);
-            s = 2;
-        }
-        for (; s < whole; s += 2) {
-            FUSCO_STAGE(0, slot0, slot1, 0);
-            FUSCO_STAGE(1, slot1, slot0, 0);
-        }
-        if (s < t.stages) {
-            FUSCO_STAGE(0, slot0, slot1, 0);
-        }
+        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc);
+        tile_stage<ACTIVE, 0>(t, slot1, slot0, ask + 1, x, acc);
     } else {
-        if (whole > 0) {
-            FUSCO_STAGE(0, slot0, slot1, STORES);
-            FUSCO_STAGE(1, slot1, slot2, STORES);
-            FUSCO_STAGE(2, slot2, slot3, STORES);
-            FUSCO_STAGE(3, slot3, slot0, 0);
-            s = 4;
-        }
-        for (; s < whole; s += 4) {
-            FUSCO_STAGE(0, slot0, slot1, 0);
-            FUSCO_STAGE(1, slot1, slot2, 0);
-            FUSCO_STAGE(2, slot2, slot3, 0);
-            FUSCO_STAGE(3, slot3, slot0, 0);
-        }
-        if (s < t.stages) {
-            FUSCO_STAGE(0, slot0, slot1, 0);
-            if (s + 1 < t.stages) {
-                FUSCO_STAGE(1, slot1, slot2, 0);
-                if (s + 2 < t.stages) {
-                    FUSCO_STAGE(2, slot2, slot3, 0);
-                }
-            }
-        }
+        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc);
+        tile_stage<ACTIVE, STORES>(t, slot1, slot2, ask + 1, x, acc);
+        tile_stage<ACTIVE, STORES>(t, slot2, slot3, ask + 2, x, acc);
+        tile_stage<ACTIVE, 0>(t, slot3, slot0, ask + 3, x, acc);
     }
-#undef FUSCO_STAGE
 }
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
@@ -495,7 +434,6 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
         }
         // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
         s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
-        tile_begin(s, slot0, slot1, slot2, slot3);
     };
 
     // Lane l holds, of fragment (f, j), the outputs a = 32 * f + l / 32 * 16 + 0 .. 15 of b = 32 * j + l % 32.
@@ -579,20 +517,54 @@ __global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel
     // stores of one tile and wave; the activation's gradient waits for loads in between and counts as none
     constexpr int kStores = STORE == kStoreGatedGrad ? 0 : FB * kOutA * (STORE == kStoreF32 ? 4 : 2);
 
+    // Tiles follow one another without a pause: the last turn of one asks for the first stages of the next, whose first fragments it reads.
     int t = tile_in_list(0);
     if (t >= total) return;
     clear();
     begin(t);
+#pragma unroll
+    for (int i = 0; i < State::kLoads; ++i) s.load(0, i, slot0);
+#pragma unroll
+    for (int i = 0; i < State::kLoads; ++i) s.load(1, i, slot1);
+    if constexpr (State::kSlots == 4) {
+#pragma unroll
+        for (int i = 0; i < State::kLoads; ++i) s.load(2, i, slot2);
+#pragma unroll
+        for (int i = 0; i < State::kLoads; ++i) s.load(3, i, slot3);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     store(0, 0, 0, 0);   // nothing, but the stores are counted
+    s.template wait<State::kSlots - 1, kStores>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    Slice<FA, FB> x[2];
+#pragma unroll
+    for (int m = 0; m < FA * FB; ++m) read_after(s, slot0, s.a_lane, s.b_lane, 0, m, x[0]);
     for (int i = 1;; ++i) {
-        if (wb * FB * 32 < b_left) tile_sum<true, kStores>(s, slot0, slot1, slot2, slot3, acc);
-        else tile_sum<false, kStores>(s, slot0, slot1, slot2, slot3, acc);   // rows past the segment: loads and barriers only
-        const int done_a0 = a0, done_a = a_left, done_b = b_left;
-        const int64_t done_row = row0;
+        const int now_a0 = a0, now_a = a_left, now_b = b_left;
+        const int64_t now_row = row0;
+        const bool active = wb * FB * 32 < b_left;   // or all of this wave's rows lie past the segment: loads and barriers only
+        const int turns = s.turns();
+        int ask = State::kSlots;
+        if (turns > 1) {
+            if (active) {
+                tile_turn<true, kStores>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) tile_turn<true, 0>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+            } else {
+                tile_turn<false, kStores>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) tile_turn<false, 0>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+            }
+        }
         t = tile_in_list(i);
         const bool more = t < total;   // later tiles of this workgroup lie behind it
-        if (more) begin(t);            // under way while this tile's outputs are stored
-        store(done_a0, done_a, done_b, done_row);
+        if (more) {
+            begin(t);
+        } else {
+            s.stages = s.a.c_size = s.b.c_size = 0;
+        }
+        if (active) tile_turn<true, 0>(s, slot0, slot1, slot2, slot3, 0, x, acc);
+        else tile_turn<false, 0>(s, slot0, slot1, slot2, slot3, 0, x, acc);
+        store(now_a0, now_a, now_b, now_row);
         if (!more) break;
         clear();
     }
