@@ -23,11 +23,10 @@ int check_pointers(bool empty, const void *const *p, int n)
 }
 
 template <typename K>
-void launch_product(K kernel, int64_t tiles, int per_cu, const ProductArgs &a, hipStream_t s)
+void launch_product(K kernel, const ProductArgs &a, hipStream_t s)
 {
-    // whole sets of compute units, so that the tile list is dealt to the XCDs in runs
-    const int sets = tiles > (int64_t)kCus && per_cu > 1 ? per_cu : 1;
-    hipLaunchKernelGGL(kernel, dim3(kCus * sets), dim3(kTileThreads), 0, s, a);
+    // a workgroup per compute unit, also where there are fewer tiles: the list is dealt to the XCDs in runs
+    hipLaunchKernelGGL(kernel, dim3(kCus), dim3(kTileThreads), 0, s, a);
 }
 
 // Few rows per expert: a workgroup per tile of 16 token rows and block of weight rows; tiles that do not exist leave at once
@@ -47,14 +46,14 @@ int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 template <int AMODE, int STORE>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
-    const int64_t mean = L->P / L->E, tiles_a = (a.NA + kTileA - 1) / kTileA;
+    const int64_t mean = L->P / L->E;
     if constexpr (AMODE == kAlongC) {
         // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
         if (mean < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
     }
-    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, (L->P / 256 + L->E) * tiles_a, 1, a, s);
-    else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, (L->P / 128 + L->E) * tiles_a, 1, a, s);
-    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, (L->P / 64 + L->E) * tiles_a, 2, a, s);
+    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
+    else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);
+    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
     return launch_status();
 }
 
@@ -400,9 +399,8 @@ int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const voi
     if (check_pointers(L->N == 0, rows, 2) != FUSCO_OK || check_pointers(false, weights, 1) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
     if (((int64_t)L->E * ((M + 255) / 256)) * ((C + 255) / 256) >= (int64_t)1 << 30) return FUSCO_ERR_INVALID_ARG;
     ProductArgs a = {L->exp_off, (const char *)d_x, (const char *)d_dy, (char *)d_dw, nullptr, L->E, C, M, 0};
-    const int64_t tiles = (int64_t)L->E * ((M + 255) / 256) * ((C + 255) / 256);
-    if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32>, tiles, 1, a, (hipStream_t)stream);
-    else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16>, tiles, 1, a, (hipStream_t)stream);
+    if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32>, a, (hipStream_t)stream);
+    else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16>, a, (hipStream_t)stream);
     return launch_status();
 }
 

@@ -294,17 +294,15 @@ __device__ __forceinline__ void tile_prefix(const int *__restrict__ exp_off, int
 // work on at a time) then share 4 tiles of rows and 8 tiles of weights in their L2.
 constexpr int kGroupB = 4;
 
-// Workgroup g of `groups` takes tiles of the list in runs of 32 per XCD: workgroups are dealt to the XCDs in turn.
+// The i-th tile of a workgroup: in each round an XCD has 32 tiles that follow one another, and workgroups are dealt to the XCDs in turn.
 __device__ __forceinline__ int tile_in_list(int i)
 {
-    const int per_xcd = kCus / kXcds, g = blockIdx.x;
-    const int round = g / kCus, in = g % kCus;
-    return ((i * (int)(gridDim.x / kCus) + round) * kXcds + in % kXcds) * per_xcd + in / kXcds;
+    return (i * kXcds + blockIdx.x % kXcds) * (kCus / kXcds) + blockIdx.x / kXcds;
 }
 
 // FA x FB fragments of 32 x 32 outputs per wave, kTileA / (32 * FA) waves along a
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
-__global__ __launch_bounds__(kTileThreads, BB == 64 ? 4 : 2) void product_kernel(ProductArgs p)
+__global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
     typedef TileState<AMODE, BMODE, BB, FA, FB> State;
     constexpr int kWavesA = kTileA / (32 * FA), kWavesB = BB / (32 * FB);
