@@ -174,8 +174,10 @@ RouteArgs route_args(const fusco_router *R, const void *d_logits)
     return a;
 }
 
-// calls f(lanes per row, values per lane, threads per workgroup).  16 lanes per row where every lane then has at most 32 values and k of the
-// lanes' largest values say enough; single waves per workgroup for few rows, which spreads them over the compute units.
+// calls f(lanes per row, values per lane, threads per workgroup).  A wave per row where rows are few and long, for its latency (8 of E, sigmoids, 8 groups, us,
+// 16 lanes / 64: 128 x 256 5.1 / 4.5, 128 x 512 7.1 / 5.2, 2048 x 256 5.7 / 5.3, 4096 x 256 5.8 / 7.0, 1024 x 128 4.3 / 5.1).  Else 16 lanes
+// where every lane then has at most 32 values and k of the lanes' largest values say enough; single waves per workgroup for few rows, which
+// spreads them over the compute units.
 template <typename F>
 void with_route_shape(const fusco_router *R, F f)
 {
@@ -186,7 +188,9 @@ void with_route_shape(const fusco_router *R, F f)
     };
     const std::integral_constant<int, 16> some;
     const std::integral_constant<int, 64> all;
-    if (R->k <= 10 && by16 <= 4) go(some, std::integral_constant<int, 4>());
+    if (R->N <= 2048 && R->E > 128 && by64 <= 4) go(all, std::integral_constant<int, 4>());
+    else if (R->N <= 2048 && R->E > 128 && by64 <= 8) go(all, std::integral_constant<int, 8>());
+    else if (R->k <= 10 && by16 <= 4) go(some, std::integral_constant<int, 4>());
     else if (R->k <= 10 && by16 <= 8) go(some, std::integral_constant<int, 8>());
     else if (R->k <= 10 && by16 <= 16) go(some, std::integral_constant<int, 16>());
     else if (R->k <= 10 && by16 <= 32) go(some, std::integral_constant<int, 32>());
@@ -216,8 +220,19 @@ int fusco_route(const fusco_router *R, const void *d_logits, const float *d_bias
     a.chosen = d_topk_idx;
     a.w = d_w;
     with_route_shape(R, [&](auto lanes, auto values, auto threads) {
-        constexpr int kLanes = decltype(lanes)::value, kThreads = decltype(threads)::value, kRows = kThreads / kLanes;
-        hipLaunchKernelGGL((route_kernel<kLanes, decltype(values)::value, kThreads>), dim3((unsigned)((R->N + kRows - 1) / kRows)), dim3(kThreads), 0, (hipStream_t)stream, a);
+        constexpr int kLanes = decltype(lanes)::value, kValues = decltype(values)::value, kThreads = decltype(threads)::value, kRows = kThreads / kLanes;
+        const dim3 grid((unsigned)((R->N + kRows - 1) / kRows));
+        // Rows held in whole lanes spare the groups their way through LDS (8 groups, us, without / with: 32768 x 256 19.2 / 15.7, 32768 x 512 33.6 / 28.8);
+        // 16 lanes without groups gain nothing worth an instance.
+        if constexpr (kValues >= 4) {
+            a.group_lanes = a.group_size % kValues == 0 && ((a.group_size / kValues) & (a.group_size / kValues - 1)) == 0 ? a.group_size / kValues : 0;
+            const bool boundaries = aligned16(d_logits) && R->logits_stride * (a.bf16 ? 2 : 4) % 16 == 0 && aligned16(d_bias);
+            if (boundaries && R->E == kLanes * kValues && (kLanes == 64 || (R->groups > 1 && a.group_lanes > 0))) {
+                hipLaunchKernelGGL((route_kernel<kLanes, kValues, kThreads, true>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((route_kernel<kLanes, kValues, kThreads, false>), grid, dim3(kThreads), 0, (hipStream_t)stream, a);
     });
     return launch_status();
 }

@@ -5,7 +5,9 @@
 //   as much as its group_best largest b together, and only experts of the keep_groups best groups compete
 //   chosen: the k largest b, descending, ties to the lower index;  w = scale * s / (sum of the chosen s)  or  scale * s
 //
-// LANES lanes of a wave (16 or all 64) hold one row, VPL values each: expert e is value e / LANES of lane e % LANES.
+// LANES lanes of a wave (16 or all 64) hold one row, VPL values each.  WHOLE: a row has LANES * VPL experts and lies on 16-byte boundaries;
+// a lane then has neighbours, expert e is value e % VPL of lane e / VPL, which are loaded 16 bytes at a time and often lie in one
+// group.  Otherwise expert e is value e / LANES of lane e % LANES, so that no lane is left without.
 #ifndef FUSCO_CSRC_ROUTING_H
 #define FUSCO_CSRC_ROUTING_H
 
@@ -21,10 +23,13 @@ struct RouteArgs {
     const float *dw;       // backward: [N, k]
     char *dlogits;         // backward: [N, E] of the logits' type
     int64_t stride;        // elements from row to row of the logits
-    int32_t N, E, k, groups, keep_groups, group_best, group_size, group_magic;   // e / group_size == e * group_magic >> 20 for every e < 1024
+    int32_t N, E, k, groups, keep_groups, group_best, group_size, group_magic, group_lanes;   // e / group_size == e * group_magic >> 20 for every e < 1024
     int32_t bf16, sigmoid, renorm;
     float scale;
 };
+
+template <int LANES, int VPL, bool WHOLE>
+__device__ __forceinline__ int expert_at(int v, int sub) { return WHOLE ? sub * VPL + v : v * LANES + sub; }
 
 // Reductions over the LANES lanes of a row, in all of them
 template <int LANES, typename T, typename F>
@@ -50,6 +55,15 @@ template <int LANES>
 __device__ __forceinline__ uint32_t lanes_max(uint32_t v) { return over_lanes<LANES>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
 template <int LANES>
 __device__ __forceinline__ uint32_t lanes_min(uint32_t v) { return over_lanes<LANES>(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; }); }
+
+// Largest value of the wave, as a scalar
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    const uint32_t m = lanes_max<16>(v);
+    const uint32_t a = __builtin_amdgcn_readlane(m, 0), b = __builtin_amdgcn_readlane(m, 16), c = __builtin_amdgcn_readlane(m, 32), d = __builtin_amdgcn_readlane(m, 48);
+    const uint32_t ab = a > b ? a : b, cd = c > d ? c : d;
+    return ab > cd ? ab : cd;
+}
 
 // Orders the LDS accesses of a wave's lanes: a row belongs to one wave
 __device__ __forceinline__ void wave_sync()
@@ -109,12 +123,30 @@ __device__ __forceinline__ float score_of(const RouteArgs &p, float l, float m)
 }
 
 // The row's scores: sigmoids, or exponentials with their sum in `total` (NaN where the row has a NaN or +infinity)
-template <int LANES, int VPL>
+template <int LANES, int VPL, bool WHOLE>
 __device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, float (&s)[VPL], float &total, float &m)
 {
     // loads past the row's end are loads of its last logit
     const int64_t row = (int64_t)n * p.stride;
-    if (p.bf16) {
+    if constexpr (WHOLE) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        const int64_t at = row + sub * VPL;
+        if (p.bf16) {
+#pragma unroll
+            for (int v = 0; v < VPL; v += 4) {
+                const bf16x4 l = *(const bf16x4 *)(p.logits + (at + v) * 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[v + i] = (float)l[i];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < VPL; v += 4) {
+                const rows_f32x4 l = *(const rows_f32x4 *)(p.logits + (at + v) * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[v + i] = l[i];
+            }
+        }
+    } else if (p.bf16) {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) s[v] = (float)((const __bf16 *)p.logits)[row + min(v * LANES + sub, p.E - 1)];
     } else {
@@ -127,7 +159,7 @@ __device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, f
         sigmoids(s);
         return;
     }
-    if (p.E < LANES * VPL) {
+    if (!WHOLE && p.E < LANES * VPL) {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) s[v] = v * LANES + sub < p.E ? s[v] : -INFINITY;
     }
@@ -145,10 +177,42 @@ __device__ __forceinline__ void row_scores(const RouteArgs &p, int n, int sub, f
     total = lanes_sum<LANES>(total);
 }
 
-// Groups: each one's score, which are kept, and what of that holds for this lane's experts.  `by` holds the row's b, group_score is the
-// row's LDS of FUSCO_MAX_GROUPS entries.
+// The two largest of both lanes' two largest
+__device__ __forceinline__ void join_best(float &best, float &second, float b, float s)
+{
+    second = fmaxf(fmaxf(second, s), fminf(best, b));
+    best = fmaxf(best, b);
+}
+template <int control>
+__device__ __forceinline__ float moved(float v)
+{
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), control, 0xf, 0xf, true));
+}
+
+// Scores of groups that are `lanes` whole lanes each, a power of two: the lane's own two largest b, then those of its group's lanes
 template <int LANES, int VPL>
-__device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const float *by, float *group_score, uint32_t (&key)[VPL])
+__device__ __forceinline__ void score_own_group(const RouteArgs &p, int sub, const float (&b)[VPL], int lanes, float *group_score)
+{
+    float best = -INFINITY, second = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < VPL; ++v) {
+        const float some = fmaxf(b[v], -INFINITY);   // a NaN is passed over
+        second = __builtin_amdgcn_fmed3f(best, second, some);
+        best = fmaxf(best, some);
+    }
+    if (lanes >= 2) join_best(best, second, moved<0xb1>(best), moved<0xb1>(second));      // lane ^ 1
+    if (lanes >= 4) join_best(best, second, moved<0x4e>(best), moved<0x4e>(second));      // lane ^ 2
+    if (lanes >= 8) join_best(best, second, moved<0x141>(best), moved<0x141>(second));    // the other four of eight, mirrored
+    if (lanes >= 16) join_best(best, second, moved<0x140>(best), moved<0x140>(second));   // the other eight of sixteen
+    if (LANES == 64) {
+        for (int d = 16; d < lanes; d *= 2) join_best(best, second, __shfl_xor(best, d), __shfl_xor(second, d));
+    }
+    if (sub % lanes == 0) group_score[sub / lanes] = p.group_best == 2 ? best + second : best;
+}
+
+// The same from the row's b in LDS, for groups of any size
+template <int LANES>
+__device__ __forceinline__ void score_groups(const RouteArgs &p, int sub, const float *by, float *group_score)
 {
     wave_sync();
     // as many lanes per group as there are, a power of two; each takes every `share`-th expert, begun at another place per group so that
@@ -164,19 +228,21 @@ __device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const f
 #pragma unroll 8
             for (int n = 0; n < each; ++n) {
                 const int at = i * share + h;
-                const float b = at < p.group_size ? by[g * p.group_size + at] : -INFINITY;
-                second = __builtin_amdgcn_fmed3f(best, second, b);   // a NaN is passed over, here and below
+                const float b = fmaxf(at < p.group_size ? by[g * p.group_size + at] : -INFINITY, -INFINITY);   // a NaN is passed over
+                second = __builtin_amdgcn_fmed3f(best, second, b);
                 best = fmaxf(best, b);
                 i = i + 1 == each ? 0 : i + 1;
             }
         }
-        for (int d = 1; d < share; d *= 2) {
-            const float b = __shfl_xor(best, d), s = __shfl_xor(second, d);
-            second = fmaxf(fmaxf(second, s), fminf(best, b));
-            best = fmaxf(best, b);
-        }
+        for (int d = 1; d < share; d *= 2) join_best(best, second, __shfl_xor(best, d), __shfl_xor(second, d));
         if (g < p.groups && h == 0) group_score[g] = p.group_best == 2 ? best + second : best;
     }
+}
+
+// Which groups are kept, and what of that holds for this lane's experts.  own: all of them are of group `own`, or -1.
+template <int LANES, int VPL, bool WHOLE>
+__device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const float *group_score, int own, uint32_t (&key)[VPL])
+{
     wave_sync();
     uint64_t kept = 0;   // bit g: group g of this lane's row is kept
     for (int base = 0; base < p.groups; base += LANES) {
@@ -191,17 +257,21 @@ __device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const f
         const uint64_t said = __ballot(g < p.groups && ahead < p.keep_groups);
         kept |= LANES == 64 ? said : (said >> (threadIdx.x & 48) & 0xffff) << base;
     }
-    if (p.groups <= 32) {
+    if (WHOLE && own >= 0) {
+        const uint32_t most = kept >> own & 1 ? 0xffffffffu : kKeyDropped;
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) key[v] = min(key[v], most);
+    } else if (p.groups <= 32) {
         const uint32_t some = (uint32_t)kept;
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const uint32_t g = (uint32_t)(v * LANES + sub) * p.group_magic >> 20;
+            const uint32_t g = (uint32_t)expert_at<LANES, VPL, WHOLE>(v, sub) * p.group_magic >> 20;
             key[v] = some >> g & 1 ? key[v] : min(key[v], kKeyDropped);
         }
     } else {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) {
-            const uint32_t g = (uint32_t)(v * LANES + sub) * p.group_magic >> 20;
+            const uint32_t g = (uint32_t)expert_at<LANES, VPL, WHOLE>(v, sub) * p.group_magic >> 20;
             key[v] = kept >> g & 1 ? key[v] : min(key[v], kKeyDropped);
         }
     }
@@ -209,7 +279,7 @@ __device__ __forceinline__ void drop_groups(const RouteArgs &p, int sub, const f
 
 // The j-th chosen expert of the row in lane j (of 64 lanes' j % LANES), one after the other: k times the largest key, the lowest expert among
 // equal ones
-template <int LANES, int VPL>
+template <int LANES, int VPL, bool WHOLE>
 __device__ __forceinline__ int choose_in_turn(const RouteArgs &p, int sub, uint32_t (&key)[VPL])
 {
     int mine = 0;
@@ -223,11 +293,23 @@ __device__ __forceinline__ int choose_in_turn(const RouteArgs &p, int sub, uint3
                 at = v;
             }
         }
-        const uint32_t top = lanes_max<LANES>(best);
-        const uint32_t e = lanes_min<LANES>(best == top ? (uint32_t)(at * LANES + sub) : 0xffffffffu);
+        uint32_t e;
+        if constexpr (LANES == 64) {
+            const uint32_t top = wave_max(best);
+            const uint64_t with = __ballot(best == top);
+            if (__popcll(with) == 1) {
+                const int lane = __ffsll((long long)with) - 1;
+                e = (uint32_t)expert_at<LANES, VPL, WHOLE>(__builtin_amdgcn_readlane(at, lane), lane);
+            } else {
+                e = lanes_min<LANES>(best == top ? (uint32_t)expert_at<LANES, VPL, WHOLE>(at, sub) : 0xffffffffu);
+            }
+        } else {
+            const uint32_t top = lanes_max<LANES>(best);
+            e = lanes_min<LANES>(best == top ? (uint32_t)expert_at<LANES, VPL, WHOLE>(at, sub) : 0xffffffffu);
+        }
 #pragma unroll
         for (int v = 0; v < VPL; ++v)
-            if ((uint32_t)(v * LANES + sub) == e) key[v] = kKeyGone;
+            if ((uint32_t)expert_at<LANES, VPL, WHOLE>(v, sub) == e) key[v] = kKeyGone;
         if (sub == j) mine = (int)e;
     }
     return mine;
@@ -305,11 +387,13 @@ __device__ __forceinline__ bool choose_at_once(const RouteArgs &p, int sub, cons
     return true;
 }
 
-template <int LANES, int VPL, int THREADS>
+// Bound by vector instructions where there are many rows (32768 x 256 with 8 groups, sigmoids, 8 chosen: 15.7 us, 2.3 TB/s read and written;
+// without groups 13.4), by a wave's chain of dependent steps where there are few (128 x 256: 4.4 us, an empty launch 2).
+template <int LANES, int VPL, int THREADS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
 {
-    constexpr int kRows = THREADS / LANES, kPitch = LANES * VPL + (LANES == 16 ? 16 : 0);   // rows of a wave begin in different banks
-    __shared__ float by[kRows][kPitch];              // b, where there are groups
+    constexpr int kRows = THREADS / LANES, kPitch = LANES * VPL + (LANES == 64 ? 0 : WHOLE ? 80 : 16);   // rows of a wave begin in different banks
+    __shared__ __align__(16) float by[kRows][kPitch];              // b, where there are groups
     __shared__ float group_score[kRows][FUSCO_MAX_GROUPS];
     __shared__ uint64_t list[LANES == 16 ? kRows : 1][kListed];
     __shared__ int order[LANES == 16 ? kRows : 1][16];
@@ -317,31 +401,50 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
     const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;   // rows past the end repeat the last one and store nothing
 
     float s[VPL], total, m;
-    row_scores<LANES, VPL>(p, n, sub, s, total, m);
+    row_scores<LANES, VPL, WHOLE>(p, n, sub, s, total, m);
     if (p.bias) {
         float by_total = 1.0f;
         if (!p.sigmoid) by_total = 1.0f / total;
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) s[v] = s[v] * by_total + p.bias[min(v * LANES + sub, p.E - 1)];
+        for (int v = 0; v < VPL; ++v) s[v] = s[v] * by_total + p.bias[WHOLE ? sub * VPL + v : min(v * LANES + sub, p.E - 1)];
     }
     uint32_t key[VPL];
 #pragma unroll
     for (int v = 0; v < VPL; ++v) key[v] = score_key(s[v]);
-    if (p.E < LANES * VPL) {
+    if (!WHOLE && p.E < LANES * VPL) {
 #pragma unroll
         for (int v = 0; v < VPL; ++v) key[v] = v * LANES + sub < p.E ? key[v] : kKeyGone;
     }
     if (p.groups > 1) {
+        const bool own = WHOLE && (LANES == 16 || p.group_lanes > 0);   // a group is some whole lanes of the row
+        if (own) {
+            score_own_group<LANES, VPL>(p, sub, s, p.group_lanes, group_score[slot]);
+        } else {
 #pragma unroll
-        for (int v = 0; v < VPL; ++v) by[slot][v * LANES + sub] = s[v];
+            for (int v = 0; v < VPL; ++v) by[slot][expert_at<LANES, VPL, WHOLE>(v, sub)] = s[v];
+            score_groups<LANES>(p, sub, by[slot], group_score[slot]);
+        }
+        drop_groups<LANES, VPL, WHOLE>(p, sub, group_score[slot], own ? sub / p.group_lanes : -1, key);
     }
-    if (p.groups > 1) drop_groups<LANES, VPL>(p, sub, by[slot], group_score[slot], key);
+    // choose_at_once wants the candidates spread over the lanes, which those of kept groups are not
+    constexpr bool kSpread = WHOLE && LANES == 16;
+    if constexpr (kSpread) {
+        uint32_t *keys = (uint32_t *)by[slot];
+#pragma unroll
+        for (int v = 0; v < VPL; v += 4) {
+            typedef uint32_t words __attribute__((ext_vector_type(4)));
+            *(words *)(keys + sub * (VPL + 4) + v) = words{key[v], key[v + 1], key[v + 2], key[v + 3]};
+        }
+        wave_sync();
+#pragma unroll
+        for (int v = 0; v < VPL; ++v) key[v] = keys[v * LANES + sub + (v * LANES + sub) / VPL * 4];
+    }
 
     int mine = 0;                                        // lane j has the j-th chosen expert
     if constexpr (LANES == 16) {
-        if (!choose_at_once<VPL>(p, sub, key, list[slot], order[slot], mine)) mine = choose_in_turn<LANES, VPL>(p, sub, key);
+        if (!choose_at_once<VPL>(p, sub, key, list[slot], order[slot], mine)) mine = choose_in_turn<LANES, VPL, false>(p, sub, key);
     } else {
-        mine = choose_in_turn<LANES, VPL>(p, sub, key);
+        mine = choose_in_turn<LANES, VPL, WHOLE>(p, sub, key);
     }
 
     // weights; a row whose scores are all zero (no expert allowed) has weights 0
@@ -367,7 +470,7 @@ __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteArgs p)
     const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;
     float s[VPL], total, m;
-    row_scores<LANES, VPL>(p, n, sub, s, total, m);
+    row_scores<LANES, VPL, false>(p, n, sub, s, total, m);
     const float inv_total = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
