@@ -39,20 +39,41 @@ int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
     return launch_status();
 }
 
-// Products whose tiles are rows of one expert: the tile's height goes by the mean number of rows of an expert.  Measured, 128 experts of
-// 4096 x (2 x 1280) gated, us, few / 64 / 128 / 256:  mean 4: 437 / 441 / - / -, 8: 482 / 455 / 531 / 591, 32: - / 476 / 535 / 601,
-// 64: - / 671 / 511 / 619, 128: - / 996 / 826 / 601.  Input gradient of 64 experts with 512 uneven rows, 2816 x 2048: 656 / 477 / 450 with 64 / 128 /
-// 256.
+// Products whose tiles are rows of one expert.  From eight rows per expert on, the tile's height is the one whose rounds of tiles over the compute units
+// take least: an expert's rows end inside a tile, two fifths of one on average, and a tile of 64, 128 or 256 rows takes 1 : 1.2 : 1.4 (fitted to
+// 130 products of 8 to 128 experts with 8 to 1000 rows, where the choice is 3 % slower than the best one; by the mean number of rows alone, from 48 and from
+// 96 on, it was 20 %).  Measured with 64 / 128 / 256, us: 128 experts of 4096 x (2 x 1280) gated, 8 rows 455 / 531 / 591, 64 rows 671 / 511 / 619, 128 rows 996 / 826 /
+// 601; 16 of 2048 x 1408 with 128 rows, gradient of the pre-activations 32 / 48 / 61; 16 of 4096 x (2 x 1280) with 230 rows 224 / 185 / 127, its
+// gradient of the pre-activations 120 / 90 / 136.
+template <int STORE>
+int tile_rows(const fusco_layout *L, const ProductArgs &a)
+{
+    const int units = STORE == kStoreGated ? kTileA / 2 : kTileA;
+    const double across = (a.NA + units - 1) / units, takes[] = {1.0, 1.2, 1.4};
+    int best = 256;
+    double least = INFINITY;
+    for (int i = 2; i >= 0; --i) {
+        const int rows = 64 << i;
+        const double tiles = fmax((double)L->E, (double)L->P / rows + 0.4 * L->E) * across;
+        const double time = ceil(tiles / kCus) * takes[i];
+        if (time < least) {
+            least = time;
+            best = rows;
+        }
+    }
+    return best;
+}
+
 template <int AMODE, int STORE>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
-    const int64_t mean = L->P / L->E;
     if constexpr (AMODE == kAlongC) {
         // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
-        if (mean < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
+        if (L->P / L->E < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);   // 4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455
     }
-    if (mean >= 96) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
-    else if (mean >= 48) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);
+    const int rows = tile_rows<STORE>(L, a);
+    if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
+    else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);
     else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
     return launch_status();
 }
