@@ -246,12 +246,36 @@ struct Target {
         for (int q = 0; q < 8; ++q) o[q] = (__bf16)v[q];
         __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, o), to, (int)offset, 0, 0);
     }
-    __device__ __forceinline__ void put4(const float *v, uint32_t offset) const
-    {
-        const f32x4 o = {v[0], v[1], v[2], v[3]};
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(words4, o), to, (int)offset, 0, 0);
-    }
 };
+
+// Part k of a lane's sixteen results as it is stored: four of fp32 or eight of bf16
+template <bool F32>
+__device__ __forceinline__ words4 packed(const f32x16 &v, int k)
+{
+    if constexpr (F32) {
+        const f32x4 o = {v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]};
+        return __builtin_bit_cast(words4, o);
+    } else {
+        bf16x8 o;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) o[q] = (__bf16)v[8 * k + q];
+        return __builtin_bit_cast(words4, o);
+    }
+}
+
+// Transposes two values over two lanes of four neighbours: the lower keeps its first and gets the other's first as its second, the upper (upper != 0)
+// gets the other's second as its first
+template <int control>
+__device__ __forceinline__ void exchange(int upper, words4 &first, words4 &second)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t of_first = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)first[i], control, 0xf, 0xf, true);
+        const uint32_t of_second = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)second[i], control, 0xf, 0xf, true);
+        first[i] = upper ? of_second : first[i];
+        second[i] = upper ? second[i] : of_first;
+    }
+}
 
 __device__ __forceinline__ void store4(char *out, int64_t element, f32x4 v)
 {
@@ -463,6 +487,26 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             }
 #pragma unroll
             for (int f = 0; f < kOutA; ++f) {
+                if constexpr (STORE == kStoreF32 || STORE == kStoreBf16) {
+                    // 64 (fp32) or 32 bytes of a lane's row are dealt out to as many neighbours, so that a store meets whole pieces of a row
+                    constexpr int kParts = STORE == kStoreF32 ? 4 : 2;
+                    words4 v[kParts];
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) v[k] = packed<STORE == kStoreF32>(acc[f][j], k);
+#pragma unroll
+                    for (int k = 0; k < kParts; k += 2) exchange<0xb1>(lane & 1, v[k], v[k + 1]);
+                    if constexpr (kParts == 4) {
+                        exchange<0x4e>(lane & 2, v[0], v[2]);
+                        exchange<0x4e>(lane & 2, v[1], v[3]);
+                    }
+                    const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16 + (lane & (kParts - 1)) * (16 / kParts);
+#pragma unroll
+                    for (int k = 0; k < kParts; ++k) {
+                        const int row = (wb * FB + j) * 32 + (lane & 32 - kParts) + k;
+                        __builtin_amdgcn_raw_buffer_store_b128(v[k], out.to, (int)(a < a_left && row < b_left ? row * out.ld + a * kSize : kNowhere), 0, 0);
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16 + h * 8;
@@ -471,12 +515,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                     float v[8];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] = acc[f][j][h * 8 + q];
-                    if (STORE == kStoreF32) {
-                        out.put4(v, at);
-                        out.put4(v + 4, at + 16);
-                    } else if (STORE == kStoreBf16) {
-                        out.put8(v, at);
-                    } else if (STORE == kStoreGated) {
+                    if (STORE == kStoreGated) {
                         float up[8];
 #pragma unroll
                         for (int q = 0; q < 8; ++q) up[q] = acc[f + FA / 2][j][h * 8 + q];
