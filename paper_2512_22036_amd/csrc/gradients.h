@@ -18,6 +18,7 @@ struct CombineGradArgs {
 };
 
 // CPT chunks of eight elements per thread, rows of y taken JU at a time
+// Bound by memory, rows read and written all over the tensors at once: 8192 x 8 x 14336 B 401 us, 5.0 TB/s; 1537 x 6 x 5760 B 20 us.
 template <bool Y_BF16, bool DOUT_BF16, int CPT, int JU, bool PAST>
 __global__ __launch_bounds__(1024) void combine_grad_kernel(CombineGradArgs p)
 {

@@ -325,6 +325,11 @@ __device__ __forceinline__ int tile_in_list(int i)
 }
 
 // FA x FB fragments of 32 x 32 outputs per wave, kTileA / (32 * FA) waves along a
+//
+// Bound by the matrix instructions under the card's power limit where experts have many rows (8 experts of 16384 rows, 4096 x 2560: 1.21 to 1.29 PFLOP/s
+// forward, 1.15 to 1.20 input gradient, 1.20 to 1.38 weight gradient; 128 uneven ones of 1024 rows gated 1.13), by the weights where they have few (128 experts
+// with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
+// of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {

