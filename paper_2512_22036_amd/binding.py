@@ -8,6 +8,7 @@ fallback path: a missing library is an error.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from types import SimpleNamespace
@@ -514,9 +515,15 @@ def fusco_norm_scratch_bytes(N: int, H: int) -> int:
     return load_library().fusco_norm_scratch_bytes(N, H)
 
 
-def _norm_scratch(n: _CNorm, scratch: Optional[torch.Tensor], device) -> torch.Tensor:
+def _norm_scratch(n: _CNorm, scratch: Optional[torch.Tensor], device, stream) -> torch.Tensor:
+    """The caller's scratch, or one for this call alone.  That one is given up when the call returns, with its kernels still to
+    run: it is made on their stream, whose later work is all that may get the block again."""
     if scratch is None:
-        return torch.empty(fusco_norm_scratch_bytes(n.N, n.H), dtype=torch.uint8, device=device)
+        own = contextlib.nullcontext()
+        if stream is not None:
+            own = torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=device))
+        with own:
+            return torch.empty(fusco_norm_scratch_bytes(n.N, n.H), dtype=torch.uint8, device=device)
     if not scratch.is_cuda or not scratch.is_contiguous():
         raise FuscoError("scratch must be a contiguous device tensor")
     return scratch
@@ -526,12 +533,12 @@ def fusco_norm_before_backward(dout: torch.Tensor, x: torch.Tensor, gain: torch.
                                dres: Optional[torch.Tensor] = None, eps: float = 1e-6, scratch: Optional[torch.Tensor] = None,
                                stream=None) -> None:
     """Gradients of fusco_norm_before: dx = dres + what comes through the norm, dgain float32 [H].  dres: the gradient that
-    reaches x past the block.  scratch: fusco_norm_scratch_bytes(N, H) bytes, made here if not given."""
+    reaches x past the block.  scratch: fusco_norm_scratch_bytes(N, H) bytes, made here on the call's stream if not given."""
     n = _norm(x, dout.dtype, [("gain", gain)], None, None, 1.0, eps)
     _like(n, dout.dtype, dout=dout)
     _like(n, x.dtype, dx=dx, dres=dres)
     _fp32(dgain, "dgain", (n.H,))
-    scratch = _norm_scratch(n, scratch, x.device)
+    scratch = _norm_scratch(n, scratch, x.device, stream)
     _check(load_library().fusco_norm_before_backward(ctypes.byref(n), dout.data_ptr(), x.data_ptr(), gain.data_ptr(), _ptr(dres),
                                                      dx.data_ptr(), dgain.data_ptr(), scratch.data_ptr(),
                                                      scratch.numel() * scratch.element_size(), _stream(stream)),
@@ -559,7 +566,7 @@ def fusco_norm_after_backward(dout: Optional[torch.Tensor], y: torch.Tensor, gai
         _fp32(dnext_gain, "dnext_gain", (n.H,))
     if gate is not None:
         _fp32(dgate, "dgate", gate.shape)
-    scratch = _norm_scratch(n, scratch, dr.device)
+    scratch = _norm_scratch(n, scratch, dr.device, stream)
     _check(load_library().fusco_norm_after_backward(ctypes.byref(n), _ptr(dout), _ptr(dnext), y.data_ptr(), _ptr(out), gain.data_ptr(),
                                                     _ptr(gate), _ptr(next_gain), dr.data_ptr(), dy.data_ptr(), dgain.data_ptr(),
                                                     _ptr(dgate), _ptr(dnext_gain), scratch.data_ptr(),
