@@ -404,7 +404,7 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
     row_scores<LANES, VPL, WHOLE>(p, n, sub, s, total, m);
     if (p.bias) {
         float by_total = 1.0f;
-        if (!p.sigmoid) by_total = 1.0f / total;
+        if (!p.sigmoid) by_total = total == 0.0f ? 0.0f : 1.0f / total;   // no expert allowed: scores stay 0, the bias decides
 #pragma unroll
         for (int v = 0; v < VPL; ++v) s[v] = s[v] * by_total + p.bias[WHOLE ? sub * VPL + v : min(v * LANES + sub, p.E - 1)];
     }
