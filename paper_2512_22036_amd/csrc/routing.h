@@ -458,55 +458,55 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
     }
 }
 
-// dlogits of w = scale * s[chosen] / of (of: sum of the chosen s, or 1):
-//   renormalised: ds_j = scale / of * (dw_j - sum_i dw_i s_i / of), otherwise ds_j = scale * dw_j
-//   sigmoid: dl = ds s (1 - s);  softmax: dl = s (ds - sum_i ds_i s_i), where the sum vanishes if the weights are renormalised
+// dlogits of w = scale * q, with q = s[chosen], or s[chosen] / (sum of the chosen s) if renormalised; d_j is what dw_j gives to the logarithm of s_j:
+//   renormalised: d_j = scale * q_j * (dw_j - sum_i dw_i q_i), otherwise d_j = scale * q_j * dw_j
+//   sigmoid: dl = d (1 - s);  softmax: dl = d - s * sum_i d_i, where the sum vanishes if the weights are renormalised
+// No factor grows as the scores shrink: with ds = scale * (dw - ...) / (sum of the chosen s) and dl = ds * s (...) it would overflow.
 // Bound by latency and vector instructions: 16384 x 128 bf16, softmax, 8 chosen: 6.2 us.
 template <int LANES, int VPL, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteArgs p)
 {
     constexpr int kRows = THREADS / LANES;
-    __shared__ float scores[kRows][LANES * VPL];
-    __shared__ float dscore[kRows][LANES * VPL];
+    static_assert(LANES == FUSCO_MAX_K || LANES == 16, "a lane per chosen expert: 16 lanes are taken for at most 10");
+    __shared__ float grad[kRows][LANES * VPL];
     const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     const int n_real = blockIdx.x * kRows + slot, n = n_real < p.N ? n_real : p.N - 1;
+    // lane j has the j-th chosen expert, or none
+    const int64_t at = (int64_t)n * p.k + sub;
+    const int e = sub < p.k ? p.chosen[at] : -1;
+    const bool some = (uint32_t)e < (uint32_t)p.E;
+    const float dw = some ? p.dw[at] : 0.0f, l = some ? load_logit(p, (int64_t)n * p.stride + e) : 0.0f;
     float s[VPL], total, m;
     row_scores<LANES, VPL, false>(p, n, sub, s, total, m);
     const float inv_total = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
         s[v] *= inv_total;
-        scores[slot][v * LANES + sub] = s[v];
-        dscore[slot][v * LANES + sub] = 0.0f;
+        grad[slot][v * LANES + sub] = 0.0f;
     }
+    const float score = score_of(p, l, m);   // as in the row
+    float q = some ? score : 0.0f;
+    if (p.renorm) {
+        const float sum = lanes_sum<LANES>(q);
+        q = sum == 0.0f ? 0.0f : q / sum;
+    } else {
+        q *= inv_total;
+    }
+    const float mean = lanes_sum<LANES>(dw * q);
+    float d = p.scale * q * (p.renorm ? dw - mean : dw);
+    if (p.sigmoid) d *= 1.0f - score;
     wave_sync();
-    float sum_s = 0.0f, sum_ds = 0.0f;   // of the chosen: s, dw * s
-    for (int j = sub; j < p.k; j += LANES) {
-        const int e = p.chosen[(int64_t)n * p.k + j];
-        if ((uint32_t)e >= (uint32_t)p.E) continue;
-        sum_s += scores[slot][e];
-        sum_ds += p.dw[(int64_t)n * p.k + j] * scores[slot][e];
-    }
-    sum_s = lanes_sum<LANES>(sum_s);
-    sum_ds = lanes_sum<LANES>(sum_ds);
-    const float factor = p.renorm ? (sum_s == 0.0f ? 0.0f : p.scale / sum_s) : p.scale;
-    const float mean = p.renorm ? (sum_s == 0.0f ? 0.0f : sum_ds / sum_s) : 0.0f;
-    for (int j = sub; j < p.k; j += LANES) {
-        const int e = p.chosen[(int64_t)n * p.k + j];
-        if ((uint32_t)e >= (uint32_t)p.E) continue;
-        atomicAdd(&dscore[slot][e], factor * (p.dw[(int64_t)n * p.k + j] - mean));   // chosen experts of a row are distinct: one addition each
-    }
+    if (some) atomicAdd(&grad[slot][e], d);   // chosen experts of a row are distinct: one addition each
     wave_sync();
     if (n_real >= p.N) return;
-    const float common = p.sigmoid || p.renorm ? 0.0f : factor * sum_ds;
+    const float common = p.sigmoid || p.renorm ? 0.0f : p.scale * mean;
 #pragma unroll
     for (int v = 0; v < VPL; ++v) {
-        const int e = v * LANES + sub;
-        if (e >= p.E) continue;
-        const float d = dscore[slot][e];
-        const float dl = p.sigmoid ? d * s[v] * (1.0f - s[v]) : s[v] * (d - common);
-        if (p.bf16) ((__bf16 *)p.dlogits)[(int64_t)n * p.E + e] = (__bf16)dl;
-        else ((float *)p.dlogits)[(int64_t)n * p.E + e] = dl;
+        const int x = v * LANES + sub;
+        if (x >= p.E) continue;
+        const float dl = grad[slot][x] - s[v] * common;   // a NaN among the scores stays one
+        if (p.bf16) ((__bf16 *)p.dlogits)[(int64_t)n * p.E + x] = (__bf16)dl;
+        else ((float *)p.dlogits)[(int64_t)n * p.E + x] = dl;
     }
 }
 
