@@ -1,4 +1,4 @@
-"""The routing's gradient where every score is tiny and where logits are undefined, against the formula in 64 bits.
+"""The routing's gradient where a sigmoid saturates, where every score is tiny and where logits are undefined, against the formula in 64 bits.
 
 Tolerance.  Sigmoid scores: the gradient is sums of terms scale * s / S * dw * (1 - s), or without renormalisation scale * s * dw * (1 - s).  s and 1 - s =
 1 / (1 + exp(l)) are each an exponential (2 units in the last place, and |l| units for its rounded argument), an addition and a division; the sum over k
@@ -40,6 +40,28 @@ def exact(l, idx, dw, score, renorm, scale=2.5):
     if score == "softmax" and not renorm:
         want, bound = want - scale * s * mean, bound + scale * s * mean_size
     return want, bound
+
+
+def near(dl, l, idx, want, size, score):
+    k, E = idx.shape[1], l.shape[1]
+    l = l.double()
+    far = l.abs().amax(dim=1, keepdim=True) if score == "sigmoid" else (l.amax(dim=1, keepdim=True) - l.amin(dim=1, keepdim=True))
+    units = 4 * (far + 8) + k + 16 + (E / 64 + 16 if score == "softmax" else 0)
+    own = 2.0 ** -8 if dl.dtype == torch.bfloat16 else U
+    off = (dl.double() - want).abs() - (units * U * size + own * (want.abs() + units * U * size) + 1e-37)
+    assert bool((off <= 0).all()), "off by %g more than the bound" % float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("low,high", [(8, 16), (16, 40), (-40, -8), (-40, 40), (60, 80), (-84, -60)])
+@pytest.mark.parametrize("N,E,k", [(40, 64, 6), (37, 256, 8), (20, 100, 12), (2100, 256, 8)])
+def test_sigmoids_that_saturate(N, E, k, low, high, renorm, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(N + E + high)
+    l = (low + (high - low) * torch.rand((N, E), generator=gen, device="cuda")).to(dtype)
+    idx, dw = chosen(l, k), torch.randn((N, k), generator=gen, device="cuda")
+    want, size = exact(l, idx, dw, "sigmoid", renorm)
+    near(backward(l, idx, dw, "sigmoid", renorm), l, idx, want, size, "sigmoid")
 
 
 @pytest.mark.parametrize("score,low,bits", [("sigmoid", -88.7, 20), ("softmax", -89.0, 20), ("softmax", -96.0, 10)])
