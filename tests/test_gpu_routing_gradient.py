@@ -1,4 +1,5 @@
-"""The routing's gradient where a sigmoid saturates, where every score is tiny and where logits are undefined, against the formula in 64 bits.
+"""The routing's gradient where a sigmoid saturates, where every score is tiny, and at batch sizes of every instance of the kernel, against the
+formula in 64 bits.
 
 Tolerance.  Sigmoid scores: the gradient is sums of terms scale * s / S * dw * (1 - s), or without renormalisation scale * s * dw * (1 - s).  s and 1 - s =
 1 / (1 + exp(l)) are each an exponential (2 units in the last place, and |l| units for its rounded argument), an addition and a division; the sum over k
@@ -81,6 +82,19 @@ def test_tiny_scores(N, E, k, score, low, bits):
     want, size = exact(l, idx, dw, score, True)
     # what a score below the smallest normal number has left: half a unit of 2^-bits in a share, its sum, and the mean of both; and 4 (|l| + 8) + k + 16 of 2^-23
     assert bool(((dl.double() - want).abs() <= (4 * 2.0 ** -bits + 512 * U) * size + 1e-37).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("N,E,k", [(4097, 12, 2), (4097, 60, 4), (4098, 128, 8), (5001, 256, 8), (4099, 384, 8), (4100, 512, 10), (4097, 60, 16), (4098, 128, 12), (4099, 200, 11), (4101, 512, 24),
+                                   (4097, 1024, 16), (2047, 256, 8), (2049, 512, 8), (300, 512, 4)])
+def test_every_instance(N, E, k, renorm, score, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(N + E)
+    l = torch.randn((N, E), generator=gen, device="cuda").to(dtype)
+    idx, dw = chosen(l, k), torch.randn((N, k), generator=gen, device="cuda")
+    want, size = exact(l, idx, dw, score, renorm)
+    near(backward(l, idx, dw, score, renorm), l, idx, want, size, score)
 
 
 def test_undefined_logits():
