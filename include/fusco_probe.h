@@ -152,6 +152,18 @@ int fusco_probe_plan_dispatch_through(const fusco_layout *L, size_t row_bytes, s
 int fusco_probe_segments_wide(uint64_t stream_capacity, uint64_t slice_bytes);
 
 /*
+ * Study and test aid, host-only: how many of an expert's rows a tile of one of the experts' products holds, 16 (the weights straight to
+ * registers), 64, 128 or 256.  `which`: one of FUSCO_PROBE_PRODUCT_*; outputs: values per row that the product computes (I of
+ * fusco_experts_gated, M of fusco_experts_linear, C of fusco_experts_input_grad), sum: products that are added up for each.  Sizes
+ * as there.  Negative on invalid arguments.  (Tiles of fusco_experts_weight_grad always hold 256.)
+ */
+#define FUSCO_PROBE_PRODUCT_GATED 0
+#define FUSCO_PROBE_PRODUCT_LINEAR 1
+#define FUSCO_PROBE_PRODUCT_INPUT_GRAD 2
+#define FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION 3 /* with d_pre */
+int fusco_probe_experts_tile_rows(const fusco_layout *L, int which, int32_t outputs, int32_t sum);
+
+/*
  * Measurement aid: kernel time without stream events between the kernels.  The next fusco_plan,
  * fusco_dispatch (fused modes), fusco_plan_dispatch or fusco_combine call made by the calling thread attaches the two HIP
  * events (hipEvent_t passed as void*, created with timing enabled) to its own kernels: start_event

@@ -5,6 +5,7 @@
 #include "routing.h"
 #include "norms.h"
 #include "gradients.h"
+#include "fusco_probe.h"
 #include <math.h>
 
 namespace {
@@ -64,14 +65,22 @@ int tile_rows(const fusco_layout *L, const ProductArgs &a)
     return best;
 }
 
+// Rows per tile, 16 for few_rows_kernel: below eight rows per expert (4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455)
+template <int AMODE, int STORE>
+int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
+{
+    if (AMODE == kAlongC && L->P / L->E < 8) return 16;
+    return tile_rows<STORE>(L, a);
+}
+
 template <int AMODE, int STORE>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
+    const int rows = rows_per_tile<AMODE, STORE>(L, a);
     if constexpr (AMODE == kAlongC) {
         // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
-        if (L->P / L->E < 8) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);   // 4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455
+        if (rows == 16) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
     }
-    const int rows = tile_rows<STORE>(L, a);
     if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
     else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);
     else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
@@ -438,6 +447,18 @@ int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const voi
     if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32>, a, (hipStream_t)stream);
     else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16>, a, (hipStream_t)stream);
     return launch_status();
+}
+
+int fusco_probe_experts_tile_rows(const fusco_layout *L, int which, int32_t outputs, int32_t sum)
+{
+    const bool gated = which == FUSCO_PROBE_PRODUCT_GATED, activation = which == FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION;
+    if (!layout_ok(L) || which < 0 || which > FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION || !row_ok(outputs) || !row_ok(sum)) return FUSCO_ERR_INVALID_ARG;
+    if (((gated || activation) && !row_ok(2 * outputs)) || !weights_ok((gated ? 2 : 1) * (int64_t)outputs, sum)) return FUSCO_ERR_INVALID_ARG;
+    ProductArgs a = {};
+    a.E = L->E; a.NA = outputs; a.C = sum;
+    if (gated) return rows_per_tile<kAlongC, kStoreGated>(L, a);
+    if (which == FUSCO_PROBE_PRODUCT_LINEAR) return rows_per_tile<kAlongC, kStoreBf16>(L, a);
+    return activation ? rows_per_tile<kAcross, kStoreGatedGrad>(L, a) : rows_per_tile<kAcross, kStoreBf16>(L, a);
 }
 
 }   // extern "C"
