@@ -31,12 +31,21 @@ void launch_product(K kernel, const ProductArgs &a, hipStream_t s)
 }
 
 // Few rows per expert: a workgroup per tile of 16 token rows and block of weight rows; tiles that do not exist leave at once
+constexpr int kFewF = 2;
+template <int STORE>
+int64_t few_workgroups(const fusco_layout *L, const ProductArgs &a)
+{
+    constexpr int kUnits = STORE == kStoreGated ? 8 * kFewF : 16 * kFewF;
+    const int64_t blocks = (a.NA + kUnits - 1) / kUnits, spread = L->P / 16 + L->E, tiles = spread < L->P ? spread : L->P;
+    return tiles * blocks;
+}
+// eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
+int few_waves(const ProductArgs &a) { return a.C >= 2048 ? 8 : 4; }
+
 template <int WAVES, int STORE>
 int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
-    constexpr int kF = 2, kUnits = STORE == kStoreGated ? 8 * kF : 16 * kF;
-    const int64_t blocks = (a.NA + kUnits - 1) / kUnits, spread = L->P / 16 + L->E, tiles = spread < L->P ? spread : L->P;
-    hipLaunchKernelGGL((few_rows_kernel<kF, WAVES, STORE>), dim3((unsigned)(tiles * blocks)), dim3(WAVES * kWave), 0, s, a);
+    hipLaunchKernelGGL((few_rows_kernel<kFewF, WAVES, STORE>), dim3((unsigned)few_workgroups<STORE>(L, a)), dim3(WAVES * kWave), 0, s, a);
     return launch_status();
 }
 
@@ -65,11 +74,12 @@ int tile_rows(const fusco_layout *L, const ProductArgs &a)
     return best;
 }
 
-// Rows per tile, 16 for few_rows_kernel: below eight rows per expert (4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455)
+// Rows per tile, 16 for few_rows_kernel: below eight rows per expert (4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455), unless its
+// workgroups for very many outputs come to more threads than a launch may have
 template <int AMODE, int STORE>
 int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
 {
-    if (AMODE == kAlongC && L->P / L->E < 8) return 16;
+    if (AMODE == kAlongC && L->P / L->E < 8 && few_workgroups<STORE>(L, a) * few_waves(a) * kWave <= UINT32_MAX) return 16;
     return tile_rows<STORE>(L, a);
 }
 
@@ -78,8 +88,7 @@ int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
     const int rows = rows_per_tile<AMODE, STORE>(L, a);
     if constexpr (AMODE == kAlongC) {
-        // eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
-        if (rows == 16) return a.C >= 2048 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
+        if (rows == 16) return few_waves(a) == 8 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
     }
     if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
     else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);

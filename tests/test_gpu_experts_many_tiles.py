@@ -62,3 +62,20 @@ def test_an_experts_values_stay_its_own(N, rows):
     L = f.Layout(N, 2, 4, 1)
     assert f.fusco_probe_experts_tile_rows(L, f.PRODUCT_LINEAR, 136, 200) == f.fusco_probe_experts_tile_rows(L, f.PRODUCT_INPUT_GRAD, 200, 136) == rows
     small.test_an_experts_values_stay_its_own(N)
+
+
+def test_few_rows_of_very_many_outputs():
+    """7.8 rows per expert, 352512 outputs of 8 products each: more threads than one launch of the kernel for few rows may have."""
+    f = small.fusco()
+    torch = small.torch
+    N, k, E, C, M = 1000, 8, 1024, 8, 352512
+    L, gen, bounds = small.make(N, k, E, 12, "normal")
+    assert f.fusco_probe_experts_tile_rows(L, f.PRODUCT_LINEAR, M, C) == 64
+    x, w = small.bf16(gen, L.P, C), torch.empty((E, M, C), dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    y = torch.full((L.P, M), 7.0, dtype=torch.bfloat16, device="cuda")
+    f.fusco_experts_linear(L, x, w, y)
+    for e, rows in small.segments(bounds, x):
+        if e % 64 in (0, 63):
+            want, err = small.product(x[rows], w[e])
+            small.within(y[rows], want, err + small.BF16 * (want.abs() + err) + small.TINY)
+    assert not bool((y[:, ::4099] == 7.0).all(dim=1).any())

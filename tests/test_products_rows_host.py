@@ -36,6 +36,15 @@ def test_few_rows(rows):
     assert rows(1, 8, 128, INPUT_GRAD, 1280, 4096) == 64             # the gradients have no kernel of their own for few rows
 
 
+def test_few_rows_of_very_many_outputs(rows):
+    """A launch has fewer than 2^32 threads: what would exceed that with a workgroup per 16 rows and 32 outputs goes by tiles of more rows."""
+    assert rows(1000, 8, 1024, LINEAR, 32768, 8) == 16
+    assert rows(1000, 8, 1024, LINEAR, 352512, 8) == 64            # 1524 tiles of rows, 11016 blocks of outputs, 256 threads: 4.30e9
+    assert rows(1000, 8, 1024, LINEAR, 352000, 8) == 16            # 4.29e9
+    assert rows(1000, 8, 1024, GATED, 176256, 8) == 64 and rows(1000, 8, 1024, GATED, 176000, 8) == 16
+    assert rows(127, 8, 128, LINEAR, 1 << 18, 2048) == 16
+
+
 def test_rounds_of_tiles(rows):
     """The sizes that the rule's comment gives measured times for: the fastest height, or one within 15 us of it."""
     assert [rows(N, 8, 128, GATED, 1280, 4096) for N in (128, 1024, 2048, 16384)] == [64, 128, 256, 256]
