@@ -121,8 +121,8 @@ void with_cpt(int cpt, F f)
 
 // calls f(stream is bf16, block is bf16, loads go past the caches) for the pairs of types that are offered.  Rows of bf16 go past the caches if
 // the call's tensors exceed the memory-side cache, rows of fp32, whose two halves a thread loads one after the other, never.  Norm after a
-// block, past / through, us: 16384 x 4096 bf16 102.6 / 105.8, 512 x 7168 6.7 / 5.8; with an fp32 stream 8192 x 7168 148 / 139, 1537 x 2880
-// 13.8 / 10.1; gradients 8192 x 7168 with an fp32 stream 252 / 234.
+// block, past / through, us: 16384 x 4096 bf16 102.4 / 104.4, 512 x 7168 6.3 / 6.3; with an fp32 stream 8192 x 7168 146 / 137, 1537 x 2880
+// 13.0 / 9.5; gradients 8192 x 7168 with an fp32 stream 245 / 230.
 template <typename F>
 void with_types(const fusco_norm *n, int64_t bytes_per_element, F f)
 {
@@ -148,8 +148,8 @@ int gate_check(const fusco_norm *n, const void *d_gate)
 }
 
 // Norms' gradients: one chunk per thread where the row allows it (up to 1024 threads), and as many workgroups as the compute units hold at
-// 16 waves each, every one of which leaves a row of partial sums per parameter.  Measured with 256 / 512 / 1024 workgroups, us: 8192 x 7168
-// 292 / 301 / 320, 16384 x 4096 251 / 197 / 206, 32768 x 2048 428 / 239 / 201.
+// 16 waves each, every one of which leaves a row of partial sums per parameter.  Measured with 256 / 512 / 1024 workgroups, us: with an
+// fp32 stream 8192 x 7168 231 / 241 / 258, 16384 x 4096 271 / 236 / 243, 32768 x 2048 335 / 236 / 247; bf16 16384 x 4096 214 / 174 / 183, 32768 x 2048 298 / 193 / 178.
 int grad_cpt(int chunks) { return chunks <= 1024 ? 1 : 4; }
 int norm_groups(int N, int H)
 {
@@ -261,7 +261,7 @@ int fusco_route(const fusco_router *R, const void *d_logits, const float *d_bias
     with_route_shape(R, [&](auto lanes, auto values, auto threads) {
         constexpr int kLanes = decltype(lanes)::value, kValues = decltype(values)::value, kThreads = decltype(threads)::value, kRows = kThreads / kLanes;
         const dim3 grid((unsigned)((R->N + kRows - 1) / kRows));
-        // Rows held in whole lanes spare the groups their way through LDS (8 groups, us, without / with: 32768 x 256 19.2 / 15.7, 32768 x 512 33.6 / 28.8);
+        // Rows held in whole lanes spare the groups their way through LDS (8 groups, us, without / with: 32768 x 256 21.2 / 16.5, 32768 x 512 35.4 / 29.0);
         // 16 lanes without groups gain nothing worth an instance.
         if constexpr (kValues >= 4) {
             a.group_lanes = a.group_size % kValues == 0 && ((a.group_size / kValues) & (a.group_size / kValues - 1)) == 0 ? a.group_size / kValues : 0;

@@ -22,7 +22,8 @@ struct NormArgs {
 };
 
 // CPT chunks per thread: thread i has the chunks i, i + blockDim, ...
-// Bound by memory (norm after a block with the next one: 16384 x 4096 bf16 102 us, 5.2 TB/s; 8192 x 7168 with an fp32 stream 131 us, 5.4 TB/s), by
+// Bound by memory (norm after a block with the next one: 16384 x 4096 bf16 102 us, 5.3 TB/s; 8192 x 7168 with an fp32 stream 136 us with a gate per
+// channel, 130 with one per token, 5.2 and 5.4 TB/s; 4096 x 12288 bf16 74 us, 5.5 TB/s; norm before a block alone, 8192 x 7168 with an fp32 stream 61 us, 5.8 TB/s), by
 // latency for a few rows (4 x 7168: 3.6 us).
 template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool PAST, bool AFTER>
 __global__ __launch_bounds__(1024) void norm_kernel(NormArgs p)
@@ -116,7 +117,10 @@ struct NormGradArgs {
     float scale, eps, inv_h;
 };
 
-// Bound by memory: 8192 x 7168 with an fp32 stream, both norms, 232 us, 4.6 TB/s over six streams; the join 5 us.
+// Bound by memory up to 8192 columns: 8192 x 7168 with an fp32 stream, both norms, 231 us, 4.6 TB/s over six streams; the norm before a block alone
+// 160 us, 5.2 TB/s; the join 5 us.  Beyond, a thread has four chunks: with the row ahead, the row at hand and the sums they need more than the 128 registers of a workgroup
+// of 1024, and 340 to 1572 bytes per lane lie in memory, which bounds it: 4096 x 12288 bf16, both norms, 709 us, 0.85 TB/s; with an fp32 stream 1054, 0.86; the norm before
+// alone 225 us, 1.8 TB/s.
 template <bool STREAM_BF16, bool BLOCK_BF16, int CPT, bool PAST, bool AFTER, bool NEXT, bool GATE_CHANNEL>
 __global__ __launch_bounds__(1024) void norm_grad_kernel(NormGradArgs p)
 {

@@ -37,7 +37,8 @@ struct ProductArgs {
     int32_t E, NA, NB, C;              // NA: outputs along a (gated forward: units); NB, C: weight gradient has NB outputs along b, others sum over C
 };
 
-// 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal, a few units in the last place of fp32: results are rounded to bf16
+// 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal: off by some (|g| + 4) * 2^-23 of itself, below 2^-16 where it is not 0 (g > -87), and what comes
+// of it is rounded to bf16, 2^-8
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 __device__ __forceinline__ float silu(float g) { return g * sigmoid(g); }
 

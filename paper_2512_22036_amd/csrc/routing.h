@@ -387,8 +387,8 @@ __device__ __forceinline__ bool choose_at_once(const RouteArgs &p, int sub, cons
     return true;
 }
 
-// Bound by vector instructions where there are many rows (32768 x 256 with 8 groups, sigmoids, 8 chosen: 15.7 us, 2.3 TB/s read and written;
-// without groups 13.4), by a wave's chain of dependent steps where there are few (128 x 256: 4.4 us, an empty launch 2).
+// Bound by vector instructions where there are many rows (32768 x 256 with 8 groups, sigmoids, 8 chosen: 16.5 us, 2.2 TB/s read and written, vector units
+// busy for three quarters of it; without groups 13.7), by a wave's chain of dependent steps where there are few (128 x 256: 4.4 us, an empty launch 2).
 template <int LANES, int VPL, int THREADS, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
 {
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(THREADS) void route_kernel(RouteArgs p)
 //   renormalised: d_j = scale * q_j * (dw_j - sum_i dw_i q_i), otherwise d_j = scale * q_j * dw_j
 //   sigmoid: dl = d (1 - s), 1 - s = 1 / (1 + exp(l));  softmax: dl = d - s * sum_i d_i, where the sum vanishes if the weights are renormalised
 // No factor grows as the scores shrink: with ds = scale * (dw - ...) / (sum of the chosen s) and dl = ds * s (...) it would overflow.
-// Bound by latency and vector instructions: 16384 x 128 bf16, softmax, 8 chosen: 6.2 us.
+// Bound by latency and vector instructions, busy for two fifths of it: 16384 x 128 bf16, softmax, 8 chosen: 4.8 us; 32768 x 256 fp32, sigmoids: 13.4 us, 5.0 TB/s.
 template <int LANES, int VPL, int THREADS>
 __global__ __launch_bounds__(THREADS) void route_grad_kernel(RouteArgs p)
 {
