@@ -451,6 +451,42 @@ int fusco_experts_linear(const fusco_layout *L, const void *d_x, const void *d_w
                          void *stream);
 
 /*
+ * Rows and weights in 8-bit floating point (e4m3: four significant bits, largest 448, NaN but no infinities) with a scale per block:
+ *     s = 2^n, the smallest power of two with max |x| <= 448 s over the block (at least 2^-126; 1 for a block of zeros)
+ *     q = x / s rounded to e4m3 (nearest even)
+ * Infinities and NaN become NaN and take no part in the maximum.  A block is 128 columns of a row (matrix_rows 0: activations), or 128 rows by
+ * 128 columns of a matrix (weights); the last ones of a row or matrix end with it.  d_x [rows, columns] of dtype, d_q [rows, columns] e4m3, both
+ * contiguous; d_scale fp32: [rows, scale_stride] for rows (columns behind the last block's are left as they are: dispatch moves
+ * them as its second plane, whose rows are multiples of 16 bytes), [rows / matrix_rows, ceil(matrix_rows / 128), ceil(columns / 128)]
+ * for matrices.  fusco_from_fp8 writes x = q * s for any scales, rounded once; with the powers of two above bf16 holds it exactly.
+ * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, and less than 2^31 blocks of 128 columns.
+ */
+#define FUSCO_MAX_SCALE_STRIDE 65536
+typedef struct fusco_fp8 {
+    int64_t rows;
+    int32_t columns;
+    int32_t dtype;              /* of x: FUSCO_BF16 or FUSCO_F32                     */
+    int32_t matrix_rows;        /* 0: scales per row; else rows per matrix           */
+    int32_t scale_stride;       /* floats from one row of scales to the next; matrices: ceil(columns / 128) */
+} fusco_fp8;
+int fusco_to_fp8(const fusco_fp8 *f, const void *d_x, void *d_q, float *d_scale, void *stream);
+int fusco_from_fp8(const fusco_fp8 *f, const void *d_q, const float *d_scale, void *d_x, void *stream);
+
+/*
+ * fusco_experts_gated and fusco_experts_linear on rows and weights of e4m3 with scales per block, which may be any fp32 numbers:
+ *     sum over blocks b of 128 columns of   x_scale[r, b] * w_scale[e, m / 128, b] * sum over c in b of x[r, c] w[e, m, c]
+ * Sums and scales are fp32 and results are rounded once to bf16; the matrix instructions for e4m3 cut each product, before eight neighbours are added, to
+ * a multiple of 2^-13 of the largest one's power of two (2^-16 of a result on the average, where its rounding to bf16 is 2^-9.7).  d_x [P, H] or [P, C] and d_x_scale [P, x_scale_stride] as
+ * fusco_dispatch moves the two planes of such rows; weights [E, 2 I, H] or [E, M, C]; d_w_scale [E, 2 ceil(I / 128), ceil(H / 128)] (gate rows
+ * and up rows begin blocks of their own: the weights are 2 E matrices of I rows) or [E, ceil(M / 128), ceil(C / 128)].  d_h, d_pre
+ * and d_y are bf16 as there.  H (gated) and C (linear): multiples of 16.  I and M: multiples of 8.
+ */
+int fusco_experts_gated_fp8(const fusco_layout *L, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, const void *d_w,
+                            const float *d_w_scale, void *d_h, void *d_pre, int32_t H, int32_t I, void *stream);
+int fusco_experts_linear_fp8(const fusco_layout *L, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, const void *d_w,
+                             const float *d_w_scale, void *d_y, int32_t C, int32_t M, void *stream);
+
+/*
  * Gradients of these products (tensors, sizes and rounding as there).
  *
  * fusco_experts_input_grad: dx[r, c] = sum_m dy[r, m] w[e, m, c].  d_dy [P, M], d_w [E, M, C], d_dx [P, C].

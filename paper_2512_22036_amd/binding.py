@@ -30,7 +30,8 @@ EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_
            "fusco_disaggregated_plan", "fusco_disaggregated_dispatch", "fusco_disaggregated_combine",
            "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
            "fusco_norm_before_backward", "fusco_norm_after_backward",
-           "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad")
+           "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad",
+           "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8")
 
 
 class FuscoError(RuntimeError):
@@ -60,6 +61,11 @@ class _CNorm(ctypes.Structure):
     """Mirror of struct fusco_norm."""
     _fields_ = [(n, ctypes.c_int32) for n in ("N", "H", "stream_dtype", "block_dtype", "gain_dtype", "gate_kind")] + [
         ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _CFp8(ctypes.Structure):
+    """Mirror of struct fusco_fp8."""
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("columns", "dtype", "matrix_rows", "scale_stride")]
 
 
 _lib = None
@@ -176,6 +182,15 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_experts_input_grad.argtypes = [lp, vp, vp, vp, vp, i32, i32, vp]
     lib.fusco_experts_weight_grad.restype = ctypes.c_int
     lib.fusco_experts_weight_grad.argtypes = [lp, vp, vp, vp, ctypes.c_int, i32, i32, vp]
+    fp = ctypes.POINTER(_CFp8)
+    lib.fusco_to_fp8.restype = ctypes.c_int
+    lib.fusco_to_fp8.argtypes = [fp, vp, vp, vp, vp]
+    lib.fusco_from_fp8.restype = ctypes.c_int
+    lib.fusco_from_fp8.argtypes = [fp, vp, vp, vp, vp]
+    lib.fusco_experts_gated_fp8.restype = ctypes.c_int
+    lib.fusco_experts_gated_fp8.argtypes = [lp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp]
+    lib.fusco_experts_linear_fp8.restype = ctypes.c_int
+    lib.fusco_experts_linear_fp8.argtypes = [lp, vp, vp, i32, vp, vp, vp, i32, i32, vp]
     _lib = lib
     _fast = _bind_fastcall(lib)
     return lib
@@ -645,6 +660,89 @@ def fusco_experts_weight_grad(layout: Layout, dy: torch.Tensor, x: torch.Tensor,
     _bf16(x, "x", (layout.P, C))
     _check(load_library().fusco_experts_weight_grad(ctypes.byref(layout.c), dy.data_ptr(), x.data_ptr(), dw.data_ptr(),
                                                     _dtype_code(dw, "dw"), M, C, _stream(stream)), "fusco_experts_weight_grad")
+
+
+FP8 = torch.float8_e4m3fn
+_BLOCK = 128
+
+
+def _blocks(n: int) -> int:
+    return -(-n // _BLOCK)
+
+
+def _fp8(t: torch.Tensor, name: str, shape) -> torch.Tensor:
+    if not t.is_cuda or t.dtype != FP8 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise FuscoError("%s must be a contiguous float8_e4m3fn device tensor of shape %s" % (name, list(shape)))
+    return t
+
+
+def _row_scale(t: torch.Tensor, name: str, rows: int, columns: int) -> int:
+    """Scales of rows, a value per 128 columns; rows of scales may be longer than that.  Their length."""
+    if not t.is_cuda or t.dtype != torch.float32 or not t.is_contiguous() or t.dim() != 2 or t.shape[0] != rows or t.shape[1] < _blocks(columns):
+        raise FuscoError("%s must be a contiguous float32 device tensor of %d rows with at least %d columns" % (name, rows, _blocks(columns)))
+    return t.shape[1]
+
+
+def _scaled(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> _CFp8:
+    if not x.is_cuda or x.dim() not in (2, 3) or not x.is_contiguous():
+        raise FuscoError("x must be a contiguous device tensor of rows or of matrices")
+    _fp8(q, "q", x.shape)
+    if x.dim() == 2:
+        return _CFp8(x.shape[0], x.shape[1], _dtype_code(x, "x"), 0, _row_scale(scale, "scale", *x.shape))
+    E, M, C = x.shape
+    _fp32(scale, "scale", (E, _blocks(M), _blocks(C)))
+    return _CFp8(E * M, C, _dtype_code(x, "x"), M, _blocks(C))
+
+
+def fusco_to_fp8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=None) -> None:
+    """x, bfloat16 or float32, as q (float8_e4m3fn, of x's shape) with scales that are powers of two: per 128 columns of each
+    row for x [R, C] (scale float32 [R, S], S at least ceil(C / 128)), per 128 x 128 for matrices [E, M, C] (scale
+    [E, ceil(M / 128), ceil(C / 128)])."""
+    f = _scaled(x, q, scale)
+    _check(load_library().fusco_to_fp8(ctypes.byref(f), x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream)), "fusco_to_fp8")
+
+
+def fusco_from_fp8(q: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, stream=None) -> None:
+    """x = q * scale, tensors as in fusco_to_fp8, scales any numbers."""
+    f = _scaled(x, q, scale)
+    _check(load_library().fusco_from_fp8(ctypes.byref(f), q.data_ptr(), scale.data_ptr(), x.data_ptr(), _stream(stream)), "fusco_from_fp8")
+
+
+def _fp8_weights(layout: Layout, w: torch.Tensor, w_scale: torch.Tensor, matrices: int) -> None:
+    if w.dim() != 3 or w.shape[0] != layout.E:
+        raise FuscoError("w must have three dimensions, the first of them the %d experts" % layout.E)
+    _fp8(w, "w", w.shape)
+    _fp32(w_scale, "w_scale", (layout.E, matrices * _blocks(w.shape[1] // matrices), _blocks(w.shape[2])))
+
+
+def fusco_experts_gated_fp8(layout: Layout, x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                            h: torch.Tensor, pre: Optional[torch.Tensor] = None, stream=None) -> None:
+    """fusco_experts_gated on float8_e4m3fn: x [P, H] with x_scale float32 [P, S] as fusco_dispatch moves both, w [E, 2 I, H] with
+    w_scale [E, 2 ceil(I / 128), ceil(H / 128)] (gate and up rows are matrices of their own); h [P, I] and pre [P, 2 I] bfloat16."""
+    if w.dim() == 3 and w.shape[1] % 2:
+        raise FuscoError("w must have an even number of rows per expert")
+    _fp8_weights(layout, w, w_scale, 2)
+    I, H = w.shape[1] // 2, w.shape[2]
+    _fp8(x, "x", (layout.P, H))
+    stride = _row_scale(x_scale, "x_scale", layout.P, H)
+    _bf16(h, "h", (layout.P, I))
+    if pre is not None:
+        _bf16(pre, "pre", (layout.P, 2 * I))
+    _check(load_library().fusco_experts_gated_fp8(ctypes.byref(layout.c), x.data_ptr(), x_scale.data_ptr(), stride, w.data_ptr(), w_scale.data_ptr(), h.data_ptr(), _ptr(pre),
+                                                  H, I, _stream(stream)), "fusco_experts_gated_fp8")
+
+
+def fusco_experts_linear_fp8(layout: Layout, x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+                             y: torch.Tensor, stream=None) -> None:
+    """fusco_experts_linear on float8_e4m3fn: x [P, C] with x_scale float32 [P, S], w [E, M, C] with w_scale
+    [E, ceil(M / 128), ceil(C / 128)], y [P, M] bfloat16."""
+    _fp8_weights(layout, w, w_scale, 1)
+    M, C = w.shape[1], w.shape[2]
+    _fp8(x, "x", (layout.P, C))
+    stride = _row_scale(x_scale, "x_scale", layout.P, C)
+    _bf16(y, "y", (layout.P, M))
+    _check(load_library().fusco_experts_linear_fp8(ctypes.byref(layout.c), x.data_ptr(), x_scale.data_ptr(), stride, w.data_ptr(), w_scale.data_ptr(), y.data_ptr(), C, M,
+                                                   _stream(stream)), "fusco_experts_linear_fp8")
 
 
 def fusco_combine_two_hop(layout: Layout, y: torch.Tensor, w: torch.Tensor, partial: torch.Tensor,

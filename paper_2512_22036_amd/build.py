@@ -7,7 +7,7 @@ import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("fusco.hip", "block.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("fusco.hip", "block.hip", "eight.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libfusco.so")
 

@@ -1,104 +1,15 @@
 // The operators around the token shuffle of an MoE block for MI355X (gfx950): the experts' products on the dispatched rows
 // (products.h), routing (routing.h), the norms around the block (norms.h) and the gradient of the combine (gradients.h).  C entry
 // points, declared in fusco.h.
-#include "products.h"
+#include "block_host.h"
 #include "routing.h"
 #include "norms.h"
 #include "gradients.h"
 #include "fusco_probe.h"
-#include <math.h>
 
 namespace {
 
-// rows of `elements` bf16 that the kernels take
-bool row_ok(int32_t elements) { return elements > 0 && elements % 8 == 0 && (size_t)elements * 2 <= FUSCO_MAX_ROW_BYTES; }
-
-// one expert's weights: loads inside them are addressed with 31 bits
-bool weights_ok(int64_t rows, int64_t cols) { return rows * cols * 2 < (int64_t)kNowhere; }
-
-int check_pointers(bool empty, const void *const *p, int n)
-{
-    for (int i = 0; i < n; ++i)
-        if ((!empty && !p[i]) || !aligned16(p[i])) return FUSCO_ERR_INVALID_ARG;
-    return FUSCO_OK;
-}
-
-template <typename K>
-void launch_product(K kernel, const ProductArgs &a, hipStream_t s)
-{
-    // a workgroup per compute unit, also where there are fewer tiles: the list is dealt to the XCDs in runs
-    hipLaunchKernelGGL(kernel, dim3(kCus), dim3(kTileThreads), 0, s, a);
-}
-
-// Few rows per expert: a workgroup per tile of 16 token rows and block of weight rows; tiles that do not exist leave at once
-constexpr int kFewF = 2;
-template <int STORE>
-int64_t few_workgroups(const fusco_layout *L, const ProductArgs &a)
-{
-    constexpr int kUnits = STORE == kStoreGated ? 8 * kFewF : 16 * kFewF;
-    const int64_t blocks = (a.NA + kUnits - 1) / kUnits, spread = L->P / 16 + L->E, tiles = spread < L->P ? spread : L->P;
-    return tiles * blocks;
-}
-// eight waves share a long row, four a short one: 1280 x 4096, 32 tokens 217 us / 231 with eight; 4096 x (2 x 1280) 398 / 383
-int few_waves(const ProductArgs &a) { return a.C >= 2048 ? 8 : 4; }
-
-template <int WAVES, int STORE>
-int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
-{
-    hipLaunchKernelGGL((few_rows_kernel<kFewF, WAVES, STORE>), dim3((unsigned)few_workgroups<STORE>(L, a)), dim3(WAVES * kWave), 0, s, a);
-    return launch_status();
-}
-
-// Products whose tiles are rows of one expert.  From eight rows per expert on, the tile's height is the one whose rounds of tiles over the compute units
-// take least: an expert's rows end inside a tile, two fifths of one on average, and a tile of 64, 128 or 256 rows takes 1 : 1.2 : 1.4 (fitted to
-// 130 products of 8 to 128 experts with 8 to 1000 rows, where the choice is 3 % slower than the best one; by the mean number of rows alone, from 48 and from
-// 96 on, it was 20 %).  Measured with 64 / 128 / 256, us: 128 experts of 4096 x (2 x 1280) gated, 8 rows 455 / 531 / 591, 64 rows 671 / 511 / 619, 128 rows 996 / 826 /
-// 601; 16 of 2048 x 1408 with 128 rows, gradient of the pre-activations 32 / 48 / 61; 16 of 4096 x (2 x 1280) with 230 rows 224 / 185 / 127, its
-// gradient of the pre-activations 120 / 90 / 136.
-template <int STORE>
-int tile_rows(const fusco_layout *L, const ProductArgs &a)
-{
-    const int units = STORE == kStoreGated ? kTileA / 2 : kTileA;
-    const double across = (a.NA + units - 1) / units, takes[] = {1.0, 1.2, 1.4};
-    int best = 256;
-    double least = INFINITY;
-    for (int i = 2; i >= 0; --i) {
-        const int rows = 64 << i;
-        const double tiles = fmax((double)L->E, (double)L->P / rows + 0.4 * L->E) * across;
-        const double time = ceil(tiles / kCus) * takes[i];
-        if (time < least) {
-            least = time;
-            best = rows;
-        }
-    }
-    return best;
-}
-
-// Rows per tile, 16 for few_rows_kernel: below eight rows per expert (4 rows: 437 us, 441 in tiles of 64; 8 rows: 482 / 455), unless its
-// workgroups for very many outputs come to more threads than a launch may have
-template <int AMODE, int STORE>
-int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
-{
-    if (AMODE == kAlongC && L->P / L->E < 8 && few_workgroups<STORE>(L, a) * few_waves(a) * kWave <= UINT32_MAX) return 16;
-    return tile_rows<STORE>(L, a);
-}
-
-template <int AMODE, int STORE>
-int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
-{
-    const int rows = rows_per_tile<AMODE, STORE>(L, a);
-    if constexpr (AMODE == kAlongC) {
-        if (rows == 16) return few_waves(a) == 8 ? launch_few<8, STORE>(L, a, s) : launch_few<4, STORE>(L, a, s);
-    }
-    if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE>, a, s);
-    else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE>, a, s);
-    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
-    return launch_status();
-}
-
 // ---- rows of one workgroup each
-
-bool dtype_ok(int t) { return t == FUSCO_BF16 || t == FUSCO_F32; }
 
 // threads of a workgroup whose threads take `cpt` chunks each
 unsigned row_threads(int chunks, int cpt) { return (unsigned)((chunks + cpt * kWave - 1) / (cpt * kWave) * kWave); }

@@ -1,0 +1,116 @@
+// The MoE block in 8 bits for MI355X (gfx950): rows and weights to e4m3 and back (eight.h), the experts' products on them (products.h).  C entry points, declared in
+// fusco.h.
+#include "block_host.h"
+#include "eight.h"
+
+namespace {
+
+// rows of e4m3 that the kernels take
+bool eight_row_ok(int32_t elements) { return elements > 0 && elements % 16 == 0 && (size_t)elements <= FUSCO_MAX_ROW_BYTES; }
+int32_t blocks_of(int32_t n) { return (n + kBlockColumns - 1) / kBlockColumns; }
+// scales of a row: loads inside a tile's are addressed with 31 bits
+bool scale_stride_ok(int32_t stride, int32_t columns) { return stride >= blocks_of(columns) && stride <= FUSCO_MAX_SCALE_STRIDE; }
+
+int fp8_check(const fusco_fp8 *f)
+{
+    if (!f || f->rows < 0 || !eight_row_ok(f->columns) || f->matrix_rows < 0 || !scale_stride_ok(f->scale_stride, f->columns)) return FUSCO_ERR_INVALID_ARG;
+    if (f->rows > INT32_MAX || f->rows * blocks_of(f->columns) > INT32_MAX) return FUSCO_ERR_INVALID_ARG;
+    if (f->matrix_rows && (f->rows % f->matrix_rows != 0 || f->scale_stride != blocks_of(f->columns))) return FUSCO_ERR_INVALID_ARG;
+    return dtype_ok(f->dtype) ? FUSCO_OK : FUSCO_ERR_UNSUPPORTED;
+}
+
+EightArgs eight_args(const fusco_fp8 *f, const void *in, void *out, const float *scale)
+{
+    const int32_t per_row = blocks_of(f->columns);
+    return {(const char *)in, (char *)out, const_cast<float *>(scale), (uint32_t)(f->rows * per_row), (uint32_t)per_row, f->columns, f->scale_stride,
+            f->matrix_rows, blocks_of(f->matrix_rows)};
+}
+
+// blocks per group of lanes: one where that leaves compute units without work
+constexpr int kEachMany = 4;
+bool few_blocks(const EightArgs &a) { return a.blocks < (uint32_t)(kCus * kEightGroups * kEachMany); }
+dim3 block_grid(const EightArgs &a, int each) { return dim3((a.blocks + kEightGroups * each - 1) / (kEightGroups * each)); }
+
+template <bool BF16, bool PAST>
+void launch_to_eight(const fusco_fp8 *f, const EightArgs &a, hipStream_t s)
+{
+    if (f->matrix_rows) hipLaunchKernelGGL((matrix_to_eight_kernel<BF16, PAST>), dim3((unsigned)(f->rows / f->matrix_rows * a.scale_rows * a.per_row)), dim3(kEightThreads), 0, s, a);
+    else if (few_blocks(a)) hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST, 1>), block_grid(a, 1), dim3(kEightThreads), 0, s, a);
+    else hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST, kEachMany>), block_grid(a, kEachMany), dim3(kEightThreads), 0, s, a);
+}
+
+template <bool BF16>
+void launch_from_eight(const EightArgs &a, hipStream_t s)
+{
+    if (few_blocks(a)) hipLaunchKernelGGL((from_eight_kernel<BF16, 1>), block_grid(a, 1), dim3(kEightThreads), 0, s, a);
+    else hipLaunchKernelGGL((from_eight_kernel<BF16, kEachMany>), block_grid(a, kEachMany), dim3(kEightThreads), 0, s, a);
+}
+
+// arguments of a product of e4m3 rows [P, C] with e4m3 weights; gated: `outputs` units
+ProductArgs eight_product(const fusco_layout *L, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, const void *d_w, const float *d_w_scale, void *d_out, void *d_pre,
+                          int32_t outputs, int32_t C, bool gated)
+{
+    ProductArgs a = {L->exp_off, (const char *)d_x, (const char *)d_w, (char *)d_out, (char *)d_pre, L->E, outputs, 0, C / 2};
+    a.row_scale = d_x_scale;
+    a.weight_scale = d_w_scale;
+    a.row_scales = x_scale_stride;
+    a.scale_rows = blocks_of(outputs) * (gated ? 2 : 1);
+    a.scales = blocks_of(C);
+    return a;
+}
+
+}   // namespace
+
+extern "C" {
+
+int fusco_to_fp8(const fusco_fp8 *f, const void *d_x, void *d_q, float *d_scale, void *stream)
+{
+    const int rc = fp8_check(f);
+    if (rc != FUSCO_OK) return rc;
+    const void *const p[] = {d_x, d_q, d_scale};
+    if (check_pointers(f->rows == 0, p, 3) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (f->rows == 0) return FUSCO_OK;
+    const EightArgs a = eight_args(f, d_x, d_q, d_scale);
+    const bool bf16 = f->dtype == FUSCO_BF16, past = f->rows * f->columns * (bf16 ? 2 : 4) > kCacheBytes;
+    hipStream_t s = (hipStream_t)stream;
+    if (bf16) past ? launch_to_eight<true, true>(f, a, s) : launch_to_eight<true, false>(f, a, s);
+    else past ? launch_to_eight<false, true>(f, a, s) : launch_to_eight<false, false>(f, a, s);
+    return launch_status();
+}
+
+int fusco_from_fp8(const fusco_fp8 *f, const void *d_q, const float *d_scale, void *d_x, void *stream)
+{
+    const int rc = fp8_check(f);
+    if (rc != FUSCO_OK) return rc;
+    const void *const p[] = {d_q, d_scale, d_x};
+    if (check_pointers(f->rows == 0, p, 3) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (f->rows == 0) return FUSCO_OK;
+    const EightArgs a = eight_args(f, d_q, d_x, d_scale);
+    if (f->dtype == FUSCO_BF16) launch_from_eight<true>(a, (hipStream_t)stream);
+    else launch_from_eight<false>(a, (hipStream_t)stream);
+    return launch_status();
+}
+
+int fusco_experts_gated_fp8(const fusco_layout *L, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, const void *d_w, const float *d_w_scale, void *d_h, void *d_pre,
+                            int32_t H, int32_t I, void *stream)
+{
+    if (!layout_ok(L) || !eight_row_ok(H) || !row_ok(I) || !row_ok(2 * I) || 2 * (int64_t)I * H >= (int64_t)kNowhere || !scale_stride_ok(x_scale_stride, H)) return FUSCO_ERR_INVALID_ARG;
+    const void *const p[] = {d_x, d_x_scale, d_w, d_w_scale, d_h};
+    if (check_pointers(L->N == 0, p, 5) != FUSCO_OK || !aligned16(d_pre)) return FUSCO_ERR_INVALID_ARG;
+    if (L->N == 0) return FUSCO_OK;
+    const ProductArgs a = eight_product(L, d_x, d_x_scale, x_scale_stride, d_w, d_w_scale, d_h, d_pre, I, H, true);
+    return launch_by_rows<kAlongC, kStoreGated, true>(L, a, (hipStream_t)stream);
+}
+
+int fusco_experts_linear_fp8(const fusco_layout *L, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, const void *d_w, const float *d_w_scale, void *d_y, int32_t C, int32_t M,
+                             void *stream)
+{
+    if (!layout_ok(L) || !eight_row_ok(C) || !row_ok(M) || (int64_t)M * C >= (int64_t)kNowhere || !scale_stride_ok(x_scale_stride, C)) return FUSCO_ERR_INVALID_ARG;
+    const void *const p[] = {d_x, d_x_scale, d_w, d_w_scale, d_y};
+    if (check_pointers(L->N == 0, p, 5) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (L->N == 0) return FUSCO_OK;
+    const ProductArgs a = eight_product(L, d_x, d_x_scale, x_scale_stride, d_w, d_w_scale, d_y, nullptr, M, C, false);
+    return launch_by_rows<kAlongC, kStoreBf16, true>(L, a, (hipStream_t)stream);
+}
+
+}   // extern "C"

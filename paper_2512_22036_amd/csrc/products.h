@@ -35,6 +35,10 @@ struct ProductArgs {
     char *out;                         // [P, NA], or [E, NB, NA]
     char *pre;                         // gated forms: pre-activations [P, 2 * units] (written by forward where not null, read by the gradient)
     int32_t E, NA, NB, C;              // NA: outputs along a (gated forward: units); NB, C: weight gradient has NB outputs along b, others sum over C
+    // operands of e4m3: their bytes are addressed as C pairs, and every 128 of them along the sum have a scale
+    const float *row_scale;            // [P, row_scales]
+    const float *weight_scale;         // [E, scale_rows, scales]; a row holds 128 weight rows, gate and up rows (gated) have rows of their own
+    int32_t row_scales, scale_rows, scales;
 };
 
 // 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal: off by some (|g| + 4) * 2^-23 of itself, below 2^-16 where it is not 0 (g > -87), and what comes
@@ -54,6 +58,12 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, ui
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 16, (int)offset, uniform, 0, 0);
 }
 
+// the same with 4 bytes per lane
+__device__ __forceinline__ void to_lds_single(__amdgpu_buffer_rsrc_t from, char *to, uint32_t offset, int uniform)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 4, (int)offset, uniform, 0, 0);
+}
+
 // One operand of a tile: where a stage of it (KC elements of the summed dimension) comes from and how it lies in LDS.  A fragment is 32 outputs
 // by 16 elements of the sum, slice `ks` of the stage; lane l has output l % 32 and elements l / 32 * 8 + 0 .. 7.
 //   OUT (operand A): the outputs of a fragment are dealt out so that the 16 results of a lane are neighbours: output i of the matrix
@@ -62,7 +72,10 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t from, char *to, ui
 //            served together (0-3, 12-15, 20-27 and so on) hit all banks in either order of the rows.
 //   kAcross: LDS rows of W elements, one per c; windows of 32 outputs (64 bytes) of row c at place window ^ (c & 3): the transposing read of 32
 //            lanes takes one window of each of four rows.
-template <int MODE, int W, int KC, bool OUT>
+//   PLACES (kAlongC): how the rows of a thread's loads are found.  kOwnPlaces: kept in registers.  kEvenPlaces: 64 rows further down with every load, which is left to
+//   the view it is made through; kPairedPlaces: the same for gate rows and, every other load, the up rows of the same units.
+enum { kOwnPlaces, kEvenPlaces, kPairedPlaces };
+template <int MODE, int W, int KC, bool OUT, int PLACES = kOwnPlaces>
 struct Operand {
     static constexpr int kBytes = W * KC * 2;
     static constexpr int kRowLanes = KC / 8;   // kAlongC: lanes that load one row
@@ -72,13 +85,33 @@ struct Operand {
     int64_t ld;            // bytes from row to row
     int64_t limit;         // kAlongC: readable bytes from base; kAcross: bytes that are missing from a whole last row
     int32_t c_size;        // elements (kAlongC) or rows (kAcross) of the summed dimension
-    uint32_t at[kLoads];   // this thread's byte offsets
-    int32_t chunk;         // kAlongC: the chunk of its row that this thread loads
+    uint32_t at[kLoads];   // own places: this thread's byte offsets
+    int32_t chunk;         // own places, kAlongC: the chunk of its row that this thread loads
+    int32_t left;          // even and paired places: rows (units) from base on
+    int64_t up;            // paired places: bytes from a gate row to the up row
 
-    __device__ __forceinline__ void load(int stage, int i, char *lds, int wave) const
+    // even and paired places: worked out for every stage
+    struct Place {
+        int32_t chunk;
+        uint32_t at;
+    };
+    __device__ __forceinline__ Place place() const
+    {
+        if (PLACES == kOwnPlaces) return {};
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        return {chunk_of(tid), (uint32_t)(row_of(0, tid) * (int)ld) + (chunk_of(tid) << 4)};
+    }
+
+    __device__ __forceinline__ void load(int stage, int i, char *lds, int wave, const Place &place) const
     {
         if (kLoadWaves < kTileThreads / kWave && wave >= kLoadWaves) return;
-        if (MODE == kAlongC) {
+        if (PLACES != kOwnPlaces) {
+            const bool in = stage * KC + place.chunk * 8 < c_size;
+            const int down = (PLACES == kPairedPlaces ? i / 2 : i) * (kTileThreads / kRowLanes);
+            const char *from = base + (int64_t)down * (int)ld + (PLACES == kPairedPlaces && i % 2 ? up : 0);
+            to_lds(view(from, (int64_t)(left - down) * (int)ld), lds + (i * kTileThreads + wave * kWave) * 16, in ? place.at : kNowhere, stage * KC * 2);
+        } else if (MODE == kAlongC) {
             const bool in = stage * KC + chunk * 8 < c_size;
             to_lds(view(base, limit), lds + (i * kTileThreads + wave * kWave) * 16, in ? at[i] : kNowhere, stage * KC * 2);
         } else {
@@ -122,18 +155,26 @@ struct Operand {
 // rows of 128 bytes, whole lines of the L2, which leaves room for two stages; rows of operands across c are long anyway, and four stages of
 // half the length keep more in flight (8 experts of 16384 rows, 4096 x 2560, TF/s: two of 64 / four of 32: forward 1225 / 1190, input
 // gradient 1103 / 1150, weight gradient 1206 / 1345).
-template <int AMODE, int BMODE, int BB, int FA, int FB>
+//
+// EIGHT: operands of e4m3, both along c, in the same LDS rows of 128 bytes, so that a stage is one block of scales.  They come with it: the first waves load
+// those of 64 rows each (as many as the tile has rows), the next one those of the weights, the others nothing (every wave counts the same loads).
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false>
 struct TileState {
     static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
-    typedef Operand<AMODE, kTileA, kStageC, true> A;
-    typedef Operand<BMODE, BB, kStageC, false> B;
+    static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no register to spare
+    typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces> A;
+    typedef Operand<BMODE, BB, kStageC, false, kSpared ? kEvenPlaces : kOwnPlaces> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes, kLoads = A::kLoads;
+    static constexpr int kScaleLoads = EIGHT ? 1 : 0, kSlotBytes = kStageBytes + (EIGHT ? kTileThreads * 4 : 0), kWeightScales = kStageBytes + BB * 4;
     static_assert(A::kLoads >= B::kLoads, "the wider operand");
     A a;
     B b;
     uint32_t a_lane, b_lane;
     int wave;
     int stages, turn;
+    const char *scales;    // EIGHT: what this wave loads of them: bytes from there on, one from lane to lane
+    int32_t scale_bytes, scale_step;
+    uint32_t row_scale_lane, weight_scale_wave;   // where a lane and a wave read them
 
     // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
     __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots - 1) / kSlots : 1; }
@@ -145,17 +186,22 @@ struct TileState {
         const int i = s + turn;
         return s >= stages ? stages : i >= stages ? i - stages : i;
     }
-    __device__ __forceinline__ void load(int s, int i, char *slot) const
+    __device__ __forceinline__ void load(int s, int i, char *slot) const { load(s, i, slot, a.place()); }
+    __device__ __forceinline__ void load(int s, int i, char *slot, const typename A::Place &place) const   // one of both operands, whose rows are as long
     {
         const int at = stage_of(s);
-        if (i < A::kLoads) a.load(at, i, slot, wave);
-        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave);
+        if (i < A::kLoads) a.load(at, i, slot, wave, place);
+        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, {place.chunk, place.at});
+        if (EIGHT && i == 0) {
+            const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
+            to_lds_single(view(scales, scale_bytes), slot + kStageBytes + wave * (kWave * 4), at < stages ? place : kNowhere, at * 4);
+        }
     }
     // waits until at most the loads of `behind` stages and `more` stores are on their way and nothing is being read from LDS
     template <int behind, int more = 0>
     __device__ __forceinline__ void wait() const
     {
-        constexpr int kAll = (A::kLoads + B::kLoads) * behind + more, kSome = A::kLoads * behind + more;
+        constexpr int kAll = (A::kLoads + B::kLoads + kScaleLoads) * behind + more, kSome = (A::kLoads + kScaleLoads) * behind + more;
         static_assert(kAll < 64, "what the hardware counts");
         if (B::kLoadWaves == kTileThreads / kWave || wave < B::kLoadWaves) __builtin_amdgcn_s_waitcnt((kAll & 15) | (kAll >> 4) << 14 | 0x70);
         else __builtin_amdgcn_s_waitcnt((kSome & 15) | (kSome >> 4) << 14 | 0x70);
@@ -210,6 +256,95 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
             __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
+
+// Stages of e4m3 operands: a matrix instruction takes 64 elements of the sum, and the two of a stage and fragment pair make one partial sum, which is
+// scaled and added to the pair's results.  A wave adds while the other one of its SIMD multiplies; a second partial sum on the way would take
+// registers that the tile of 256 x 256 does not have (and fragments of a are read where those before them were).
+typedef int words8 __attribute__((ext_vector_type(8)));
+
+template <int FB>
+struct Eights {
+    words8 a[2], b[FB][2];      // fragments: one of a, all of b; two halves of the stage
+    float rows[FB], weight[2];  // scales of the stage: of the lane's rows of b, of the wave's rows of a (gated: gate and up)
+};
+
+// two pieces of 16 bytes as an operand of the matrix instructions
+__device__ __forceinline__ words8 joined(const bf16x8 (&v)[2])
+{
+    typedef int words __attribute__((ext_vector_type(4)));
+    return __builtin_shufflevector(__builtin_bit_cast(words, v[0]), __builtin_bit_cast(words, v[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+template <typename Op>
+__device__ __forceinline__ words8 half_stage(const char *lds, uint32_t at, int f, int half)
+{
+    const bf16x8 v[2] = {Op::fragment(lds, at, f, 2 * half), Op::fragment(lds, at, f, 2 * half + 1)};
+    return joined(v);
+}
+
+template <bool GATED, int FB, typename S>
+__device__ __forceinline__ void read_scales(const S &t, const char *slot, int j, Eights<FB> &x)
+{
+    x.rows[j] = *(const float *)(slot + S::kStageBytes + t.row_scale_lane + j * 128);
+    if (j > 0) return;
+    x.weight[0] = *(const float *)(slot + S::kWeightScales + t.weight_scale_wave);
+    if (GATED) x.weight[1] = *(const float *)(slot + S::kWeightScales + 4);
+}
+
+template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x16 (&acc)[FA][FB])
+{
+    uint32_t a_at = t.a_lane, b_at = t.b_lane;
+    asm volatile("" : "+v"(a_at), "+v"(b_at));
+    float scale[GATED ? 2 : 1][FB];
+#pragma unroll
+    for (int g = 0; g < (GATED ? 2 : 1); ++g)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) scale[g][j] = x.weight[g] * x.rows[j];
+#pragma unroll
+    for (int f = 0; f < FA; ++f) {
+        const bool last = f == FA - 1;
+        if (last) {
+            t.template wait<S::kSlots - 2, STORES>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!ACTIVE && !last) continue;
+        typename S::A::Place place = {};
+        if (last) place = t.a.place();
+#pragma unroll
+        for (int j = 0; j < FB; ++j) {
+            f32x16 part = {};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (ACTIVE) part = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x.a[h], x.b[j][h], part, 0, 0, 0, 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == FB - 1) x.a[h] = half_stage<typename S::A>(last ? nxt : cur, a_at, (f + 1) % FA, h);
+                if (last) x.b[j][h] = half_stage<typename S::B>(nxt + S::A::kBytes, b_at, j, h);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (last) {
+                read_scales<GATED>(t, nxt, j, x);
+                constexpr int kEach = (S::kLoads + FB - 1) / FB;
+#pragma unroll
+                for (int i = j * kEach; i < (j + 1) * kEach && i < S::kLoads; ++i) t.load(ask, i, cur, place);
+            }
+            if (ACTIVE) {
+#pragma unroll
+                for (int q = 0; q < 16; ++q) acc[f][j][q] = fmaf(scale[GATED ? f / (FA / 2) : 0][j], part[q], acc[f][j][q]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
+template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_turn8(const S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x16 (&acc)[FA][FB])
+{
+    static_assert(S::kSlots == 2, "operands along c");
+    tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, ask, x, acc);
+    tile_stage8<ACTIVE, 0, GATED>(t, slot1, slot0, ask + 1, x, acc);
 }
 
 // One turn through the slots, while stage ask, ask + 1, ... of this tile or the next are asked for.  STORES: stores that were issued after
@@ -331,10 +466,10 @@ __device__ __forceinline__ int tile_in_list(int i)
 // forward, 1.15 to 1.20 input gradient, 1.20 to 1.38 weight gradient; 128 uneven ones of 1024 rows gated 1.13), by the weights where they have few (128 experts
 // with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
 // of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
-template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE>
+template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
-    typedef TileState<AMODE, BMODE, BB, FA, FB> State;
+    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated> State;
     constexpr int kWavesA = kTileA / (32 * FA), kWavesB = BB / (32 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
     constexpr bool kGated = STORE == kStoreGated;
@@ -342,7 +477,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
-    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[kMore], slot3[kMore];
+    __shared__ __align__(1024) char slot0[State::kSlotBytes], slot1[State::kSlotBytes], slot2[kMore], slot3[kMore];
     __shared__ int offsets[FUSCO_MAX_E + 1], prefix[kByRows ? FUSCO_MAX_E + 1 : 1];
     __shared__ int part[kTileThreads / kWave];
 
@@ -370,6 +505,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     s.a_lane = State::A::lane_at(lane, wa * FA * 32);
     s.b_lane = State::B::lane_at(lane, wb * FB * 32);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
+    if constexpr (EIGHT) {
+        s.row_scale_lane = (wb * FB * 32 + (lane & 31)) * 4;
+        s.weight_scale_wave = kGated ? 0 : wa * FA * 32 / 128 * 4;
+        asm volatile("" : "+v"(s.row_scale_lane), "+v"(s.weight_scale_wave));
+    }
 
     // the tile at hand
     int a0 = 0, a_left = 0, b_left = 0;
@@ -417,8 +557,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.a.limit = (rows_e - a0) * s.a.ld;
             s.a.c_size = p.C;
             s.a.chunk = State::A::chunk_of(tid);
+            s.a.left = a_left;
+            s.a.up = (int64_t)p.NA * s.a.ld;
 #pragma unroll
-            for (int j = 0; j < State::A::kLoads; ++j) {
+            for (int j = 0; !State::kSpared && j < State::A::kLoads; ++j) {
                 const int r = State::A::row_of(j, tid);
                 int unit = r, up = 0;
                 if (kGated) {   // a wave's rows: FA * 16 gate rows, then the up rows of the same units
@@ -445,8 +587,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.b.limit = (b_left < BB ? b_left : BB) * s.b.ld;
             s.b.c_size = p.C;
             s.b.chunk = State::B::chunk_of(tid);
+            s.b.left = b_left < BB ? b_left : BB;
 #pragma unroll
-            for (int j = 0; j < State::B::kLoads; ++j) s.b.at[j] = (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + (s.b.chunk << 4);
+            for (int j = 0; !State::kSpared && j < State::B::kLoads; ++j) s.b.at[j] = (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + (s.b.chunk << 4);
             s.stages = (p.C + State::kStageC - 1) / State::kStageC;
         } else {
             s.b.ld = (int64_t)p.NB * 2;
@@ -459,6 +602,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                 s.b.at[j] = output < b_left ? (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + output * 2 : kNowhere;
             }
             s.stages = (rows + State::kStageC - 1) / State::kStageC;
+        }
+        if constexpr (EIGHT) {
+            constexpr int kRowWaves = BB / kWave;   // waves that load scales of rows
+            const int rows = (b_left < BB ? b_left : BB) - s.wave * kWave, block = a0 / 128, blocks = p.scale_rows - block;
+            if (s.wave < kRowWaves) {
+                s.scales = (const char *)(p.row_scale + ((int64_t)first + b0 + s.wave * kWave) * p.row_scales);
+                s.scale_step = p.row_scales * 4;
+                s.scale_bytes = rows > 0 ? rows * s.scale_step : 0;
+            } else {   // the next one's first two lanes: two neighbouring blocks of weight rows, or those of the gate and up rows
+                s.scales = (const char *)(p.weight_scale + ((int64_t)e * p.scale_rows + block) * p.scales);
+                s.scale_step = p.scales * (kGated ? p.scale_rows / 2 : 1) * 4;
+                s.scale_bytes = s.wave > kRowWaves ? 0 : kGated ? s.scale_step + p.scales * 4 : (blocks < 2 ? blocks : 2) * s.scale_step;
+            }
         }
         // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
         s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
@@ -580,9 +736,30 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     s.template wait<State::kSlots - 1, kStores>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    Slice<FA, FB> x[2];
+    typename std::conditional<EIGHT, Eights<FB>, Slice<FA, FB>[2]>::type x;
+    if constexpr (EIGHT) {
 #pragma unroll
-    for (int m = 0; m < FA * FB; ++m) read_after(s, slot0, s.a_lane, s.b_lane, 0, m, x[0]);
+        for (int h = 0; h < 2; ++h) {
+            x.a[h] = half_stage<typename State::A>(slot0, s.a_lane, 0, h);
+#pragma unroll
+            for (int j = 0; j < FB; ++j) x.b[j][h] = half_stage<typename State::B>(slot0 + State::A::kBytes, s.b_lane, j, h);
+        }
+#pragma unroll
+        for (int j = 0; j < FB; ++j) read_scales<kGated>(s, slot0, j, x);
+    } else {
+#pragma unroll
+        for (int m = 0; m < FA * FB; ++m) read_after(s, slot0, s.a_lane, s.b_lane, 0, m, x[0]);
+    }
+    auto turn = [&](auto multiplied, auto stores, int ask) {
+        constexpr bool kMultiplied = decltype(multiplied)::value;
+        constexpr int kBehind = decltype(stores)::value;
+        if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, ask, x, acc);
+        else tile_turn<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    const std::integral_constant<int, kStores> behind;
+    const std::integral_constant<int, 0> none;
     for (int i = 1;; ++i) {
         const int now_a0 = a0, now_a = a_left, now_b = b_left;
         const int64_t now_row = row0;
@@ -591,11 +768,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         int ask = State::kSlots;
         if (turns > 1) {
             if (active) {
-                tile_turn<true, kStores>(s, slot0, slot1, slot2, slot3, ask, x, acc);
-                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) tile_turn<true, 0>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+                turn(yes, behind, ask);
+                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) turn(yes, none, ask);
             } else {
-                tile_turn<false, kStores>(s, slot0, slot1, slot2, slot3, ask, x, acc);
-                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) tile_turn<false, 0>(s, slot0, slot1, slot2, slot3, ask, x, acc);
+                turn(no, behind, ask);
+                for (ask += State::kSlots; ask < turns * State::kSlots; ask += State::kSlots) turn(no, none, ask);
             }
         }
         t = tile_in_list(i);
@@ -605,8 +782,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         } else {
             s.stages = s.a.c_size = s.b.c_size = 0;
         }
-        if (active) tile_turn<true, 0>(s, slot0, slot1, slot2, slot3, 0, x, acc);
-        else tile_turn<false, 0>(s, slot0, slot1, slot2, slot3, 0, x, acc);
+        if (active) turn(yes, none, 0);
+        else turn(no, none, 0);
         store(now_a0, now_a, now_b, now_row);
         if (!more) break;
         clear();
@@ -675,7 +852,7 @@ struct FewTile {
     }
 };
 
-template <int F, int WAVES, int STORE>
+template <int F, int WAVES, int STORE, bool EIGHT = false>
 __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
 {
     constexpr bool kGated = STORE == kStoreGated;
@@ -705,6 +882,10 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
     // piece (rows of 8 KiB: 6.1 TB/s, 5.0 without).  The order of a sum depends on the weights' place alone, not on the batch.
     const int turn = mine > 0 ? (int)(((uint32_t)(block + at.e * blocks) * 2654435761u >> 12) % (uint32_t)mine) : 0;
     bf16x8 w[F][2], x[2];
+    // e4m3: a piece is one block of scales
+    const __amdgpu_buffer_rsrc_t vs = view(EIGHT ? (const char *)(p.row_scale + (int64_t)at.first * p.row_scales) : nullptr, EIGHT ? (int64_t)at.rows * p.row_scales * 4 : 0);
+    const __amdgpu_buffer_rsrc_t vt = view(EIGHT ? (const char *)(p.weight_scale + (int64_t)at.e * p.scale_rows * p.scales) : nullptr, EIGHT ? (int64_t)p.scale_rows * p.scales * 4 : 0);
+    float row_scale, weight_scale[2];
     auto load = [&](int i) {
         int j = i + turn;
         j = j >= mine ? j - mine : j;
@@ -716,6 +897,12 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
 #pragma unroll
             for (int f = 0; f < F; ++f) w[f][ks] = load_fragment(vw, in ? w_at[f] + c * 2 : kNowhere);
             x[ks] = load_fragment(vx, in ? x_at + c * 2 : kNowhere);
+        }
+        if constexpr (EIGHT) {
+            const uint32_t block = wave + j * WAVES;
+            row_scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(vs, i < mine ? (int)(((lane & 15) * p.row_scales + block) * 4) : (int)kNowhere, 0, 0));
+            weight_scale[0] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(vt, i < mine ? (int)((a0 / 128 * p.scales + block) * 4) : (int)kNowhere, 0, 0));
+            if (kGated) weight_scale[1] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(vt, i < mine ? (int)(((a0 / 128 + p.scale_rows / 2) * p.scales + block) * 4) : (int)kNowhere, 0, 0));
         }
     };
     load(0);
@@ -730,7 +917,18 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
             for (int f = 0; f < F; ++f) wn[f][ks] = w[f][ks];
             xn[ks] = x[ks];
         }
+        const float scale[2] = {EIGHT ? row_scale * weight_scale[0] : 1.0f, EIGHT && kGated ? row_scale * weight_scale[1] : 1.0f};
         if (i + 1 < mine) load(i + 1);
+        if constexpr (EIGHT) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const f32x4 zero = {};
+                const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(joined(wn[f]), joined(xn), zero, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[f][q] = fmaf(scale[kGated && f >= kOut], part[q], acc[f][q]);
+            }
+            continue;
+        }
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks)
 #pragma unroll

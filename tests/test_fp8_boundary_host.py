@@ -1,0 +1,64 @@
+"""Argument checks of the calls for e4m3 without a GPU: bad sizes, types and pointers are refused before anything is launched, and the
+ctypes struct lies in memory as the header's does."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from test_block_boundary_host import BUF, ROOT, layout, lib  # noqa: F401
+
+
+def test_struct_lies_as_in_the_header(tmp_path):
+    from paper_2512_22036_amd.binding import _CFp8
+    names = [f for f, _ in _CFp8._fields_]
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "fusco.h"', "int main(void) {"]
+    lines += ['printf("%%zu\\n", offsetof(fusco_fp8, %s));' % f for f in names] + ['printf("%zu\\n", sizeof(fusco_fp8));', "return 0; }"]
+    (tmp_path / "a.c").write_text("\n".join(lines))
+    subprocess.check_call(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(tmp_path / "a"), str(tmp_path / "a.c")])
+    said = [int(v) for v in subprocess.check_output([str(tmp_path / "a")]).split()]
+    assert said == [getattr(_CFp8, f).offset for f in names] + [ctypes.sizeof(_CFp8)]
+
+
+def fp8(**kw):
+    from paper_2512_22036_amd.binding import _CFp8
+    return _CFp8(**{**dict(rows=64, columns=256, dtype=0, matrix_rows=0, scale_stride=2), **kw})
+
+
+@pytest.mark.parametrize("name", ["fusco_to_fp8", "fusco_from_fp8"])
+def test_there_and_back(lib, name):  # noqa: F811
+    call = lambda f, *a: getattr(lib, name)(ctypes.byref(f), *a)
+    for bad in (dict(rows=-1), dict(columns=0), dict(columns=-16), dict(columns=8), dict(columns=24), dict(columns=(1 << 20) + 16), dict(matrix_rows=-1), dict(scale_stride=1), dict(scale_stride=-1),
+                dict(scale_stride=65537), dict(matrix_rows=60), dict(matrix_rows=32, scale_stride=3), dict(rows=1 << 31), dict(rows=1 << 30, columns=512, scale_stride=4),
+                dict(rows=1 << 62)):
+        assert call(fp8(**bad), BUF, BUF, BUF, None) == -1, bad
+    for bad in (dict(dtype=2), dict(dtype=-1)):
+        assert call(fp8(**bad), BUF, BUF, BUF, None) == -3, bad
+    for i in range(3):
+        assert call(fp8(), *[None if j == i else BUF for j in range(3)], None) == -1
+        assert call(fp8(), *[BUF + 8 if j == i else BUF for j in range(3)], None) == -1
+    assert getattr(lib, name)(None, BUF, BUF, BUF, None) == -1
+    assert call(fp8(rows=0), None, None, None, None) == 0
+    assert call(fp8(rows=0, columns=8), None, None, None, None) == -1
+
+
+def test_products(lib):  # noqa: F811
+    L, empty = layout(lib), layout(lib, N=0)
+    g = lambda *a: lib.fusco_experts_gated_fp8(ctypes.byref(L), *a)
+    good = [BUF, BUF, 1, BUF, BUF, BUF, None, 64, 64, None]
+    for i in (0, 1, 3, 4, 5):
+        assert g(*[None if j == i else v for j, v in enumerate(good)]) == -1, i
+        assert g(*[BUF + 4 if j == i else v for j, v in enumerate(good)]) == -1, i
+    assert g(*[BUF + 2 if j == 6 else v for j, v in enumerate(good)]) == -1
+    for H, I, stride in ((0, 64, 1), (64, 0, 1), (24, 64, 1), (64, 4, 1), (-16, 64, 1), ((1 << 20) + 16, 64, 8193), (64, 1 << 19, 1), (1 << 16, 1 << 15, 512), (256, 64, 1), (64, 64, 65537)):
+        assert g(BUF, BUF, stride, BUF, BUF, BUF, None, H, I, None) == -1, (H, I, stride)
+    assert lib.fusco_experts_gated_fp8(None, *good) == -1
+    assert lib.fusco_experts_gated_fp8(ctypes.byref(empty), None, None, 1, None, None, None, None, 64, 64, None) == 0
+    assert lib.fusco_experts_gated_fp8(ctypes.byref(empty), None, None, 1, None, None, None, None, 72, 64, None) == -1
+    y = lambda *a: lib.fusco_experts_linear_fp8(ctypes.byref(L), *a)
+    good = [BUF, BUF, 1, BUF, BUF, BUF, 64, 64, None]
+    for i in (0, 1, 3, 4, 5):
+        assert y(*[None if j == i else v for j, v in enumerate(good)]) == -1, i
+    for C, M, stride in ((8, 64, 1), (64, 6, 1), (0, 64, 1), (144, 64, 1), (1 << 20, 1 << 11, 8192)):
+        assert y(BUF, BUF, stride, BUF, BUF, BUF, C, M, None) == -1, (C, M, stride)
+    assert lib.fusco_experts_linear_fp8(ctypes.byref(empty), None, None, 1, None, None, None, 64, 64, None) == 0
