@@ -502,6 +502,21 @@ int fusco_experts_input_grad(const fusco_layout *L, const void *d_dy, const void
 int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const void *d_x, void *d_dw, int dw_dtype, int32_t M,
                               int32_t C, void *stream);
 
+/*
+ * The same gradients from activations that were kept in e4m3 with a scale per 128 columns of a row (fusco_to_fp8 of what the forward pass
+ * wrote: half the bytes).
+ *
+ * fusco_experts_input_grad_fp8: fusco_experts_input_grad with pre-activations d_pre [P, 2 C] of e4m3, d_pre_scale [P, pre_scale_stride] (blocks of the
+ * whole row of 2 C columns), used as fp32.  C: a multiple of 16.
+ *
+ * fusco_experts_weight_grad_fp8: fusco_experts_weight_grad with d_x [P, C] of e4m3, d_x_scale [P, x_scale_stride].  x * scale is rounded to bf16 before
+ * the product, which changes nothing for scales that are powers of two.  C: a multiple of 16.
+ */
+int fusco_experts_input_grad_fp8(const fusco_layout *L, const void *d_dy, const void *d_w, void *d_dpre, const void *d_pre, const float *d_pre_scale,
+                                 int32_t pre_scale_stride, int32_t M, int32_t C, void *stream);
+int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, void *d_dw,
+                                  int dw_dtype, int32_t M, int32_t C, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,7 +31,8 @@ EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_
            "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
            "fusco_norm_before_backward", "fusco_norm_after_backward",
            "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad",
-           "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8")
+           "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8",
+           "fusco_experts_input_grad_fp8", "fusco_experts_weight_grad_fp8")
 
 
 class FuscoError(RuntimeError):
@@ -191,6 +192,10 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_experts_gated_fp8.argtypes = [lp, vp, vp, i32, vp, vp, vp, vp, i32, i32, vp]
     lib.fusco_experts_linear_fp8.restype = ctypes.c_int
     lib.fusco_experts_linear_fp8.argtypes = [lp, vp, vp, i32, vp, vp, vp, i32, i32, vp]
+    lib.fusco_experts_input_grad_fp8.restype = ctypes.c_int
+    lib.fusco_experts_input_grad_fp8.argtypes = [lp, vp, vp, vp, vp, vp, i32, i32, i32, vp]
+    lib.fusco_experts_weight_grad_fp8.restype = ctypes.c_int
+    lib.fusco_experts_weight_grad_fp8.argtypes = [lp, vp, vp, vp, i32, vp, ctypes.c_int, i32, i32, vp]
     _lib = lib
     _fast = _bind_fastcall(lib)
     return lib
@@ -638,25 +643,40 @@ def fusco_experts_linear(layout: Layout, x: torch.Tensor, w: torch.Tensor, y: to
 
 
 def fusco_experts_input_grad(layout: Layout, dy: torch.Tensor, w: torch.Tensor, dx: torch.Tensor,
-                             pre: Optional[torch.Tensor] = None, stream=None) -> None:
+                             pre: Optional[torch.Tensor] = None, stream=None, *, pre_scale: Optional[torch.Tensor] = None) -> None:
     """dx = dy W, expert by expert: dy [P, M], w [E, M, C], dx [P, C], all bfloat16.  With pre [P, 2 C] (from
-    fusco_experts_gated) dx is the gradient of pre, [P, 2 C]."""
+    fusco_experts_gated) dx is the gradient of pre, [P, 2 C].  pre may have been kept as float8_e4m3fn: then pre_scale, float32
+    [P, S], has its scales (fusco_to_fp8)."""
     _weights(layout, w, "w")
     M, C = w.shape[1], w.shape[2]
     _bf16(dy, "dy", (layout.P, M))
     _bf16(dx, "dx", (layout.P, C if pre is None else 2 * C))
+    if pre_scale is not None:
+        if pre is None:
+            raise FuscoError("pre_scale goes with pre")
+        _fp8(pre, "pre", (layout.P, 2 * C))
+        stride = _row_scale(pre_scale, "pre_scale", layout.P, 2 * C)
+        return _check(load_library().fusco_experts_input_grad_fp8(ctypes.byref(layout.c), dy.data_ptr(), w.data_ptr(), dx.data_ptr(), pre.data_ptr(), pre_scale.data_ptr(), stride, M, C,
+                                                                  _stream(stream)), "fusco_experts_input_grad_fp8")
     if pre is not None:
         _bf16(pre, "pre", (layout.P, 2 * C))
     _check(load_library().fusco_experts_input_grad(ctypes.byref(layout.c), dy.data_ptr(), w.data_ptr(), dx.data_ptr(), _ptr(pre),
                                                    M, C, _stream(stream)), "fusco_experts_input_grad")
 
 
-def fusco_experts_weight_grad(layout: Layout, dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, stream=None) -> None:
-    """dw = dy^T x, expert by expert: dy [P, M], x [P, C] bfloat16, dw [E, M, C] bfloat16 or float32."""
+def fusco_experts_weight_grad(layout: Layout, dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor,
+                              stream=None, *, x_scale: Optional[torch.Tensor] = None) -> None:
+    """dw = dy^T x, expert by expert: dy [P, M], x [P, C] bfloat16, dw [E, M, C] bfloat16 or float32.  x may have been kept as
+    float8_e4m3fn: then x_scale, float32 [P, S], has its scales (fusco_to_fp8)."""
     if not dw.is_cuda or dw.dim() != 3 or dw.shape[0] != layout.E or not dw.is_contiguous():
         raise FuscoError("dw must be a contiguous device tensor of three dimensions, the first of them the %d experts" % layout.E)
     M, C = dw.shape[1], dw.shape[2]
     _bf16(dy, "dy", (layout.P, M))
+    if x_scale is not None:
+        _fp8(x, "x", (layout.P, C))
+        stride = _row_scale(x_scale, "x_scale", layout.P, C)
+        return _check(load_library().fusco_experts_weight_grad_fp8(ctypes.byref(layout.c), dy.data_ptr(), x.data_ptr(), x_scale.data_ptr(), stride, dw.data_ptr(), _dtype_code(dw, "dw"), M, C,
+                                                                   _stream(stream)), "fusco_experts_weight_grad_fp8")
     _bf16(x, "x", (layout.P, C))
     _check(load_library().fusco_experts_weight_grad(ctypes.byref(layout.c), dy.data_ptr(), x.data_ptr(), dw.data_ptr(),
                                                     _dtype_code(dw, "dw"), M, C, _stream(stream)), "fusco_experts_weight_grad")

@@ -113,4 +113,33 @@ int fusco_experts_linear_fp8(const fusco_layout *L, const void *d_x, const float
     return launch_by_rows<kAlongC, kStoreBf16, true>(L, a, (hipStream_t)stream);
 }
 
+int fusco_experts_input_grad_fp8(const fusco_layout *L, const void *d_dy, const void *d_w, void *d_dpre, const void *d_pre, const float *d_pre_scale, int32_t pre_scale_stride, int32_t M,
+                                 int32_t C, void *stream)
+{
+    if (!layout_ok(L) || !row_ok(M) || !row_ok(2 * C) || !weights_ok(M, C) || C % 16 != 0 || !scale_stride_ok(pre_scale_stride, 2 * C)) return FUSCO_ERR_INVALID_ARG;
+    const void *const p[] = {d_dy, d_w, d_dpre, d_pre, d_pre_scale};
+    if (check_pointers(L->N == 0, p, 5) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (L->N == 0) return FUSCO_OK;
+    ProductArgs a = {L->exp_off, (const char *)d_dy, (const char *)d_w, (char *)d_dpre, (char *)const_cast<void *>(d_pre), L->E, C, 0, M};
+    a.row_scale = d_pre_scale;
+    a.row_scales = pre_scale_stride;
+    return launch_by_rows<kAcross, kStoreGatedGradKept>(L, a, (hipStream_t)stream);
+}
+
+int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const void *d_x, const float *d_x_scale, int32_t x_scale_stride, void *d_dw, int dw_dtype, int32_t M, int32_t C,
+                                  void *stream)
+{
+    if (!layout_ok(L) || !row_ok(M) || !row_ok(C) || !eight_row_ok(C) || !weights_ok(M, C) || !scale_stride_ok(x_scale_stride, C)) return FUSCO_ERR_INVALID_ARG;
+    if (!dtype_ok(dw_dtype)) return FUSCO_ERR_UNSUPPORTED;
+    const void *const rows[] = {d_dy, d_x, d_x_scale}, *const weights[] = {d_dw};
+    if (check_pointers(L->N == 0, rows, 3) != FUSCO_OK || check_pointers(false, weights, 1) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (((int64_t)L->E * ((M + 255) / 256)) * ((C + 255) / 256) >= (int64_t)1 << 30) return FUSCO_ERR_INVALID_ARG;
+    ProductArgs a = {L->exp_off, (const char *)d_x, (const char *)d_dy, (char *)d_dw, nullptr, L->E, C, M, 0};
+    a.row_scale = d_x_scale;
+    a.row_scales = x_scale_stride;
+    if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32, false, true>, a, (hipStream_t)stream);
+    else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16, false, true>, a, (hipStream_t)stream);
+    return launch_status();
+}
+
 }   // extern "C"

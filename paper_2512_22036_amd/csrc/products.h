@@ -26,7 +26,7 @@ constexpr uint32_t kNowhere = 0x7f000000u;   // byte offset past every buffer: s
 
 // How the tiles of one product lie in memory
 enum { kAlongC, kAcross };             // operand contiguous along the summed dimension, or across it
-enum { kStoreBf16, kStoreF32, kStoreGated, kStoreGatedGrad };
+enum { kStoreBf16, kStoreF32, kStoreGated, kStoreGatedGrad, kStoreGatedGradKept };   // the last one: pre-activations of e4m3
 
 struct ProductArgs {
     const int32_t *exp_off;            // [E + 1]
@@ -36,7 +36,7 @@ struct ProductArgs {
     char *pre;                         // gated forms: pre-activations [P, 2 * units] (written by forward where not null, read by the gradient)
     int32_t E, NA, NB, C;              // NA: outputs along a (gated forward: units); NB, C: weight gradient has NB outputs along b, others sum over C
     // operands of e4m3: their bytes are addressed as C pairs, and every 128 of them along the sum have a scale
-    const float *row_scale;            // [P, row_scales]
+    const float *row_scale;            // [P, row_scales]; those of kept rows (weight gradient) or pre-activations (input gradient) too
     const float *weight_scale;         // [E, scale_rows, scales]; a row holds 128 weight rows, gate and up rows (gated) have rows of their own
     int32_t row_scales, scale_rows, scales;
 };
@@ -151,6 +151,21 @@ struct Operand {
     }
 };
 
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+
+// eight values of e4m3 times a scale
+__device__ __forceinline__ void wide_eight(uint32_t first, uint32_t second, float scale, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? second : first), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)(i ? second : first), true);
+        v[4 * i] = lo[0] * scale;
+        v[4 * i + 1] = lo[1] * scale;
+        v[4 * i + 2] = hi[0] * scale;
+        v[4 * i + 3] = hi[1] * scale;
+    }
+}
+
 // Everything a wave keeps over a tile.  Of the stages in LDS one is multiplied while the others are on their way.  Operands along c come in
 // rows of 128 bytes, whole lines of the L2, which leaves room for two stages; rows of operands across c are long anyway, and four stages of
 // half the length keep more in flight (8 experts of 16384 rows, 4096 x 2560, TF/s: two of 64 / four of 32: forward 1225 / 1190, input
@@ -158,7 +173,10 @@ struct Operand {
 //
 // EIGHT: operands of e4m3, both along c, in the same LDS rows of 128 bytes, so that a stage is one block of scales.  They come with it: the first waves load
 // those of 64 rows each (as many as the tile has rows), the next one those of the weights, the others nothing (every wave counts the same loads).
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false>
+//
+// KEPT: operand A is rows of e4m3 with their scales, across c.  They pass registers on their way to LDS, where they become bf16 (with scales that are powers of two without
+// a rounding): a thread holds 16 outputs of one row of two stages.
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false>
 struct TileState {
     static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
     static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no register to spare
@@ -174,6 +192,7 @@ struct TileState {
     int stages, turn;
     const char *scales;    // EIGHT: what this wave loads of them: bytes from there on, one from lane to lane
     int32_t scale_bytes, scale_step;
+    uint32_t scale_at;     // KEPT: this thread's byte offset
     uint32_t row_scale_lane, weight_scale_wave;   // where a lane and a wave read them
 
     // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
@@ -190,11 +209,38 @@ struct TileState {
     __device__ __forceinline__ void load(int s, int i, char *slot, const typename A::Place &place) const   // one of both operands, whose rows are as long
     {
         const int at = stage_of(s);
-        if (i < A::kLoads) a.load(at, i, slot, wave, place);
+        if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place);
         if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, {place.chunk, place.at});
         if (EIGHT && i == 0) {
             const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
             to_lds_single(view(scales, scale_bytes), slot + kStageBytes + wave * (kWave * 4), at < stages ? place : kNowhere, at * 4);
+        }
+    }
+    struct Held {
+        words4 q;
+        float scale;
+    };
+    static constexpr int kHeldLanes = kTileA / 16;   // threads that share a row
+    __device__ __forceinline__ Held hold(int s) const
+    {
+        const int at = stage_of(s), left = __builtin_amdgcn_readfirstlane(min(max(a.c_size - at * kStageC, 0), kStageC));
+        Held h;
+        h.q = __builtin_amdgcn_raw_buffer_load_b128(view(a.base + (int64_t)at * (kStageC * (int)a.ld), left * (int)a.ld - a.limit), (int)a.at[0], 0, 0);
+        h.scale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(view(scales + (int64_t)at * (kStageC * scale_step), left * scale_step), (int)scale_at, 0, 0));
+        return h;
+    }
+    __device__ __forceinline__ void put(const Held &h, char *slot) const
+    {
+        const int c = (int)threadIdx.x / kHeldLanes, chunk = (int)threadIdx.x % kHeldLanes * 2;
+        bf16x8 *to = (bf16x8 *)(slot + (c * (kTileA / 8) + (chunk ^ (c & 3) << 2)) * 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float v[8];
+            wide_eight(h.q[2 * i], h.q[2 * i + 1], h.scale, v);
+            bf16x8 o;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o[q] = (__bf16)v[q];
+            to[i] = o;
         }
     }
     // waits until at most the loads of `behind` stages and `more` stores are on their way and nothing is being read from LDS
@@ -228,8 +274,8 @@ __device__ __forceinline__ void read_after(const S &t, const char *slot, uint32_
     }
 }
 
-template <bool ACTIVE, int STORES, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nxt, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
+template <bool ACTIVE, int STORES, int FA, int FB, typename S, typename X>
+__device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nxt, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB], X then)
 {
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
     asm volatile("" : "+v"(a_at), "+v"(b_at));   // fragments' places are worked out where they are used, not kept in registers over the loop
@@ -247,6 +293,7 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
         for (int m = 0; m < FA * FB; ++m) {
             if (ACTIVE) acc[m / FB][m % FB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[ks % 2].a[m / FB], x[ks % 2].b[m % FB], acc[m / FB][m % FB], 0, 0, 0);
             read_after(t, last ? nxt : cur, a_at, b_at, next, m, x[next % 2]);
+            if (last && m == 0) then();
             if (last) {                  // loads behind the last matrix instructions
                 constexpr int kEach = (S::kLoads + FA * FB - 1) / (FA * FB), kBegin = FA * FB - S::kLoads / kEach;
 #pragma unroll
@@ -353,18 +400,32 @@ __device__ __forceinline__ void tile_turn8(const S &t, char *slot0, char *slot1,
 template <bool ACTIVE, int STORES, int FA, int FB, typename S>
 __device__ __forceinline__ void tile_turn(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB])
 {
+    auto none = [] {};
     if constexpr (S::kSlots == 2) {
-        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc);
-        tile_stage<ACTIVE, 0>(t, slot1, slot0, ask + 1, x, acc);
+        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc, none);
+        tile_stage<ACTIVE, 0>(t, slot1, slot0, ask + 1, x, acc, none);
     } else {
-        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc);
-        tile_stage<ACTIVE, STORES>(t, slot1, slot2, ask + 1, x, acc);
-        tile_stage<ACTIVE, STORES>(t, slot2, slot3, ask + 2, x, acc);
-        tile_stage<ACTIVE, 0>(t, slot3, slot0, ask + 3, x, acc);
+        tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc, none);
+        tile_stage<ACTIVE, STORES>(t, slot1, slot2, ask + 1, x, acc, none);
+        tile_stage<ACTIVE, STORES>(t, slot2, slot3, ask + 2, x, acc, none);
+        tile_stage<ACTIVE, 0>(t, slot3, slot0, ask + 3, x, acc, none);
     }
 }
 
-typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+// The same with kept rows: those asked for two stages ago go to LDS, two stages ahead of their use, behind the barrier that says that nobody reads there.
+template <bool ACTIVE, int STORES, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_turn_kept(const S &t, char *slot0, char *slot1, char *slot2, char *slot3, int ask, Slice<FA, FB> (&x)[2], f32x16 (&acc)[FA][FB],
+                                               typename S::Held (&held)[2])
+{
+    auto pass = [&](typename S::Held &h, char *later, int i) {
+        t.put(h, later);
+        h = t.hold(i);
+    };
+    tile_stage<ACTIVE, STORES>(t, slot0, slot1, ask, x, acc, [&] { pass(held[0], slot2, ask); });
+    tile_stage<ACTIVE, STORES>(t, slot1, slot2, ask + 1, x, acc, [&] { pass(held[1], slot3, ask + 1); });
+    tile_stage<ACTIVE, STORES>(t, slot2, slot3, ask + 2, x, acc, [&] { pass(held[0], slot0, ask + 2); });
+    tile_stage<ACTIVE, 0>(t, slot3, slot0, ask + 3, x, acc, [&] { pass(held[1], slot1, ask + 3); });
+}
 
 // Outputs of a wave.  Stores go through a bounds-checked view, so that their number is the same for every tile: what lies outside is dropped.
 struct Target {
@@ -466,13 +527,13 @@ __device__ __forceinline__ int tile_in_list(int i)
 // forward, 1.15 to 1.20 input gradient, 1.20 to 1.38 weight gradient; 128 uneven ones of 1024 rows gated 1.13), by the weights where they have few (128 experts
 // with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
 // of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
-template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false>
+template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
-    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated> State;
+    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated, KEPT> State;
     constexpr int kWavesA = kTileA / (32 * FA), kWavesB = BB / (32 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
-    constexpr bool kGated = STORE == kStoreGated;
+    constexpr bool kGated = STORE == kStoreGated, kGatedGrad = STORE == kStoreGatedGrad || STORE == kStoreGatedGradKept;
     constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
@@ -569,6 +630,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                 }
                 s.a.at[j] = unit < a_left ? (uint32_t)((unit + up * p.NA) * s.a.ld) + (s.a.chunk << 4) : kNowhere;
             }
+        } else if constexpr (KEPT) {
+            const int output = tid % State::kHeldLanes * 16, c = tid / State::kHeldLanes;
+            s.a.ld = p.NA;
+            s.a.limit = a0;
+            s.a.c_size = rows;
+            s.a.base = p.rows + first * s.a.ld + a0;
+            s.a.at[0] = output < a_left ? (uint32_t)(c * s.a.ld) + output : kNowhere;
+            s.scales = (const char *)(p.row_scale + (int64_t)first * p.row_scales);
+            s.scale_step = p.row_scales * 4;
+            s.scale_at = output < a_left ? (uint32_t)(c * s.scale_step) + (a0 + output) / 128 * 4 : kNowhere;
         } else {
             s.a.ld = (int64_t)p.NA * 2;
             s.a.limit = (int64_t)a0 * 2;
@@ -627,7 +698,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         constexpr int kSize = STORE == kStoreF32 ? 4 : 2;
         const int rows = b_left < BB ? b_left : BB;
         Target out, pre;
-        out.open(p.out, row0, (int64_t)p.NA * (STORE == kStoreGatedGrad ? 2 : 1) * kSize, (int64_t)a0 * kSize, rows);
+        out.open(p.out, row0, (int64_t)p.NA * (kGatedGrad ? 2 : 1) * kSize, (int64_t)a0 * kSize, rows);
+        __amdgpu_buffer_rsrc_t kept_scale;
+        if (STORE == kStoreGatedGradKept) {
+            pre.open(p.pre, row0, (int64_t)p.NA * 2, a0, rows);
+            kept_scale = view((const char *)(p.row_scale + row0 * p.row_scales), rows > 0 ? (int64_t)rows * p.row_scales * 4 : 0);
+        }
         if ((kGated && p.pre) || STORE == kStoreGatedGrad) pre.open(p.pre, row0, (int64_t)p.NA * 2 * kSize, (int64_t)a0 * kSize, rows);
         const uint32_t second = (uint32_t)p.NA * kSize;
         int lane = tid & 63;
@@ -636,6 +712,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         for (int j = 0; j < FB; ++j) {
             const int b = (wb * FB + j) * 32 + (lane & 31);
             bf16x8 gates[STORE == kStoreGatedGrad ? kOutA : 1][2], ups[STORE == kStoreGatedGrad ? kOutA : 1][2];
+            words4 kept[STORE == kStoreGatedGradKept ? kOutA : 1][2];      // sixteen of a lane's are one load, and lie in one block of scales
+            float scale[STORE == kStoreGatedGradKept ? kOutA : 1][2];
+            if constexpr (STORE == kStoreGatedGradKept) {
+#pragma unroll
+                for (int f = 0; f < kOutA; ++f)
+#pragma unroll
+                    for (int up = 0; up < 2; ++up) {
+                        const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16, column = a0 + a + up * p.NA;
+                        const bool in = a < a_left && b < b_left;
+                        kept[f][up] = __builtin_amdgcn_raw_buffer_load_b128(pre.to, in ? (int)(b * pre.ld + a + up * p.NA) : (int)kNowhere, 0, 0);
+                        scale[f][up] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(kept_scale, in ? (b * p.row_scales + column / 128) * 4 : (int)kNowhere, 0, 0));
+                    }
+            }
             if constexpr (STORE == kStoreGatedGrad) {   // all pre-activations at once, not one after the other
 #pragma unroll
                 for (int f = 0; f < kOutA; ++f)
@@ -690,12 +779,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                         for (int q = 0; q < 8; ++q) v[q] = silu(v[q]) * up[q];
                         out.put8(v, at);
                     } else {
-                        float dup[8];
+                        float dup[8], gate[8], up[8];
+                        if constexpr (STORE == kStoreGatedGradKept) {
+                            wide_eight(kept[f][0][2 * h], kept[f][0][2 * h + 1], scale[f][0], gate);
+                            wide_eight(kept[f][1][2 * h], kept[f][1][2 * h + 1], scale[f][1], up);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q) {
+                                gate[q] = (float)gates[f][h][q];
+                                up[q] = (float)ups[f][h][q];
+                            }
+                        }
 #pragma unroll
                         for (int q = 0; q < 8; ++q) {
-                            const float g = (float)gates[f][h][q], sig = sigmoid(g);
+                            const float g = gate[q], sig = sigmoid(g);
                             dup[q] = v[q] * g * sig;
-                            v[q] = v[q] * (float)ups[f][h][q] * sig * (1.0f + g * (1.0f - sig));
+                            v[q] = v[q] * up[q] * sig * (1.0f + g * (1.0f - sig));
                         }
                         out.put8(v, at);
                         out.put8(dup, at + second);
@@ -714,13 +813,22 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                 for (int q = 0; q < 16; ++q) acc[f][j][q] = 0.0f;
     };
     // stores of one tile and wave; the activation's gradient waits for loads in between and counts as none
-    constexpr int kStores = STORE == kStoreGatedGrad ? 0 : FB * kOutA * (STORE == kStoreF32 ? 4 : 2);
+    constexpr int kStores = kGatedGrad ? 0 : FB * kOutA * (STORE == kStoreF32 ? 4 : 2);
 
     // Tiles follow one another without a pause: the last turn of one asks for the first stages of the next, whose first fragments it reads.
     int t = tile_in_list(0);
     if (t >= total) return;
     clear();
     begin(t);
+    typename std::conditional<KEPT, typename State::Held[2], char>::type held;
+    if constexpr (KEPT) {
+        held[0] = s.hold(0);
+        held[1] = s.hold(1);
+        s.put(held[0], slot0);
+        s.put(held[1], slot1);
+        held[0] = s.hold(2);
+        held[1] = s.hold(3);
+    }
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(0, i, slot0);
 #pragma unroll
@@ -754,6 +862,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         constexpr bool kMultiplied = decltype(multiplied)::value;
         constexpr int kBehind = decltype(stores)::value;
         if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, ask, x, acc);
+        else if constexpr (KEPT) tile_turn_kept<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc, held);
         else tile_turn<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc);
     };
     const std::true_type yes;

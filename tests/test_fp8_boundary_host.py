@@ -62,3 +62,24 @@ def test_products(lib):  # noqa: F811
     for C, M, stride in ((8, 64, 1), (64, 6, 1), (0, 64, 1), (144, 64, 1), (1 << 20, 1 << 11, 8192)):
         assert y(BUF, BUF, stride, BUF, BUF, BUF, C, M, None) == -1, (C, M, stride)
     assert lib.fusco_experts_linear_fp8(ctypes.byref(empty), None, None, 1, None, None, None, 64, 64, None) == 0
+
+
+def test_gradients(lib):  # noqa: F811
+    L, empty = layout(lib), layout(lib, N=0)
+    i = lambda *a: lib.fusco_experts_input_grad_fp8(ctypes.byref(L), *a)
+    good = [BUF, BUF, BUF, BUF, BUF, 1, 64, 64, None]
+    for n in range(5):
+        assert i(*[None if j == n else v for j, v in enumerate(good)]) == -1, n
+        assert i(*[BUF + 8 if j == n else v for j, v in enumerate(good)]) == -1, n
+    for stride, M, C in ((1, 64, 72), (1, 64, 128), (1, 4, 64), (0, 64, 64), (8192, 64, 1 << 19), (65537, 64, 64)):
+        assert i(BUF, BUF, BUF, BUF, BUF, stride, M, C, None) == -1, (stride, M, C)
+    assert lib.fusco_experts_input_grad_fp8(ctypes.byref(empty), None, None, None, None, None, 1, 64, 64, None) == 0
+    w = lambda *a: lib.fusco_experts_weight_grad_fp8(ctypes.byref(L), *a)
+    good = [BUF, BUF, BUF, 1, BUF, 0, 64, 64, None]
+    for n in (0, 1, 2, 4):
+        assert w(*[None if j == n else v for j, v in enumerate(good)]) == -1, n
+        assert w(*[BUF + 8 if j == n else v for j, v in enumerate(good)]) == -1, n
+    assert w(BUF, BUF, BUF, 1, BUF, 2, 64, 64, None) == -3
+    for stride, M, C in ((1, 64, 72), (1, 64, 144), (1, 4, 64), (1, 64, 0), (4096, 64, (1 << 19) + 16)):
+        assert w(BUF, BUF, BUF, stride, BUF, 0, M, C, None) == -1, (stride, M, C)
+    assert lib.fusco_experts_weight_grad_fp8(ctypes.byref(empty), None, None, None, 1, None, 0, 64, 64, None) == -1   # dw is written even then
