@@ -15,7 +15,7 @@ from .binding import (BF16, F32, DISPATCH_EXPERT, DISPATCH_WIRE, DISPATCH_TWO_HO
                       fusco_combine_backward, fusco_route, fusco_route_backward, fusco_norm_before, fusco_norm_after, fusco_norm_scratch_bytes,
                       fusco_norm_before_backward, fusco_norm_after_backward, SCORE_SOFTMAX, SCORE_SIGMOID, GATE_NONE, GATE_CHANNEL, GATE_TOKEN,
                       fusco_experts_gated, fusco_experts_linear, fusco_experts_input_grad, fusco_experts_weight_grad,
-                      fusco_to_fp8, fusco_from_fp8, fusco_experts_gated_fp8, fusco_experts_linear_fp8)
+                      fusco_to_fp8, fusco_from_fp8, fusco_experts_gated_fp8, fusco_experts_linear_fp8, fusco_moe_few_scratch_bytes, fusco_moe_few)
 
 __all__ = ["BF16", "F32", "DISPATCH_EXPERT", "DISPATCH_WIRE", "DISPATCH_TWO_HOP", "DISPATCH_STREAMING", "FuscoError", "Layout",
            "ROUTE_TOKENS", "ROUTE_TILES", "ROUTE_BOTH_BY_TILES", "ROUTE_TILES_THEN_TOKENS", "WALK_PLAIN", "WALK_STREAMING", "WALK_THROUGH", "PRODUCT_GATED", "PRODUCT_LINEAR", "PRODUCT_INPUT_GRAD", "PRODUCT_INPUT_GRAD_ACTIVATION",
@@ -26,4 +26,4 @@ __all__ = ["BF16", "F32", "DISPATCH_EXPERT", "DISPATCH_WIRE", "DISPATCH_TWO_HOP"
            "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
            "fusco_norm_before_backward", "fusco_norm_after_backward", "SCORE_SOFTMAX", "SCORE_SIGMOID", "GATE_NONE", "GATE_CHANNEL", "GATE_TOKEN",
            "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad",
-           "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8"]
+           "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8", "fusco_moe_few_scratch_bytes", "fusco_moe_few"]

@@ -16,7 +16,7 @@ from typing import Optional
 
 import torch
 
-BF16, F32 = 0, 1
+BF16, F32, E4M3 = 0, 1, 2
 DISPATCH_EXPERT, DISPATCH_WIRE, DISPATCH_TWO_HOP, DISPATCH_STREAMING = 1, 2, 4, 8
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN = 0, 1, 2
@@ -32,7 +32,7 @@ EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_
            "fusco_norm_before_backward", "fusco_norm_after_backward",
            "fusco_experts_gated", "fusco_experts_linear", "fusco_experts_input_grad", "fusco_experts_weight_grad",
            "fusco_to_fp8", "fusco_from_fp8", "fusco_experts_gated_fp8", "fusco_experts_linear_fp8",
-           "fusco_experts_input_grad_fp8", "fusco_experts_weight_grad_fp8")
+           "fusco_experts_input_grad_fp8", "fusco_experts_weight_grad_fp8", "fusco_moe_few_scratch_bytes", "fusco_moe_few")
 
 
 class FuscoError(RuntimeError):
@@ -67,6 +67,11 @@ class _CNorm(ctypes.Structure):
 class _CFp8(ctypes.Structure):
     """Mirror of struct fusco_fp8."""
     _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("columns", "dtype", "matrix_rows", "scale_stride")]
+
+
+class _CFew(ctypes.Structure):
+    """Mirror of struct fusco_few."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "E", "k", "H", "I", "weight_dtype", "out_dtype")]
 
 
 _lib = None
@@ -196,6 +201,10 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_experts_input_grad_fp8.argtypes = [lp, vp, vp, vp, vp, vp, i32, i32, i32, vp]
     lib.fusco_experts_weight_grad_fp8.restype = ctypes.c_int
     lib.fusco_experts_weight_grad_fp8.argtypes = [lp, vp, vp, vp, i32, vp, ctypes.c_int, i32, i32, vp]
+    lib.fusco_moe_few_scratch_bytes.restype = sz
+    lib.fusco_moe_few_scratch_bytes.argtypes = [i32, i32, i32]
+    lib.fusco_moe_few.restype = ctypes.c_int
+    lib.fusco_moe_few.argtypes = [ctypes.POINTER(_CFew)] + [vp] * 9 + [sz, vp]
     _lib = lib
     _fast = _bind_fastcall(lib)
     return lib
@@ -538,6 +547,10 @@ def fusco_norm_scratch_bytes(N: int, H: int) -> int:
 
 
 def _norm_scratch(n: _CNorm, scratch: Optional[torch.Tensor], device, stream) -> torch.Tensor:
+    return _scratch(fusco_norm_scratch_bytes(n.N, n.H), scratch, device, stream)
+
+
+def _scratch(nbytes: int, scratch: Optional[torch.Tensor], device, stream) -> torch.Tensor:
     """The caller's scratch, or one for this call alone.  That one is given up when the call returns, with its kernels still to
     run: it is made on their stream, whose later work is all that may get the block again."""
     if scratch is None:
@@ -545,7 +558,7 @@ def _norm_scratch(n: _CNorm, scratch: Optional[torch.Tensor], device, stream) ->
         if stream is not None:
             own = torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=device))
         with own:
-            return torch.empty(fusco_norm_scratch_bytes(n.N, n.H), dtype=torch.uint8, device=device)
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
     if not scratch.is_cuda or not scratch.is_contiguous():
         raise FuscoError("scratch must be a contiguous device tensor")
     return scratch
@@ -763,6 +776,41 @@ def fusco_experts_linear_fp8(layout: Layout, x: torch.Tensor, x_scale: torch.Ten
     _bf16(y, "y", (layout.P, M))
     _check(load_library().fusco_experts_linear_fp8(ctypes.byref(layout.c), x.data_ptr(), x_scale.data_ptr(), stride, w.data_ptr(), w_scale.data_ptr(), y.data_ptr(), C, M,
                                                    _stream(stream)), "fusco_experts_linear_fp8")
+
+
+def fusco_moe_few_scratch_bytes(N: int, k: int, I: int) -> int:
+    return load_library().fusco_moe_few_scratch_bytes(N, k, I)
+
+
+def fusco_moe_few(x: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, out: torch.Tensor,
+                  w_in_scale: Optional[torch.Tensor] = None, w_out_scale: Optional[torch.Tensor] = None, scratch: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """The experts of a layer for a few tokens, N of 1 to 64: x [N, H] bfloat16, topk_idx [N, k] int32, w [N, k] float32 as
+    fusco_route writes them, out [N, H] bfloat16 or float32.  Weights w_in [E, 2 I, H] and w_out [E, H, I] are bfloat16, or
+    float8_e4m3fn with the scales that fusco_experts_gated_fp8 and fusco_experts_linear_fp8 take.  scratch:
+    fusco_moe_few_scratch_bytes(N, k, I) bytes, made here on the call's stream if not given."""
+    if not x.is_cuda or x.dim() != 2 or w_in.dim() != 3 or w_in.shape[1] % 2:
+        raise FuscoError("x must be a 2-D device tensor, w_in have three dimensions and an even number of rows per expert")
+    (N, H), E, I = x.shape, w_in.shape[0], w_in.shape[1] // 2
+    if not topk_idx.is_cuda or topk_idx.dtype != torch.int32 or not topk_idx.is_contiguous() or topk_idx.dim() != 2 or topk_idx.shape[0] != N:
+        raise FuscoError("topk_idx must be a contiguous int32 device tensor of shape [N, k]")
+    _bf16(x, "x", (N, H))
+    _fp32(w, "w", topk_idx.shape)
+    if (w_in_scale is None) != (w_out_scale is None):
+        raise FuscoError("w_in_scale and w_out_scale go together")
+    weights = _bf16 if w_in_scale is None else _fp8
+    weights(w_in, "w_in", (E, 2 * I, H))
+    weights(w_out, "w_out", (E, H, I))
+    if w_in_scale is not None:
+        _fp32(w_in_scale, "w_in_scale", (E, 2 * _blocks(I), _blocks(H)))
+        _fp32(w_out_scale, "w_out_scale", (E, _blocks(H), _blocks(I)))
+    if not out.is_cuda or not out.is_contiguous() or tuple(out.shape) != (N, H):
+        raise FuscoError("out must be a contiguous device tensor of shape [%d, %d]" % (N, H))
+    f = _CFew(N, E, topk_idx.shape[1], H, I, BF16 if w_in_scale is None else E4M3, _dtype_code(out, "out"))
+    scratch = _scratch(fusco_moe_few_scratch_bytes(N, f.k, I), scratch, x.device, stream)
+    _check(load_library().fusco_moe_few(ctypes.byref(f), x.data_ptr(), topk_idx.data_ptr(), w.data_ptr(), w_in.data_ptr(), _ptr(w_in_scale), w_out.data_ptr(),
+                                        _ptr(w_out_scale), out.data_ptr(), scratch.data_ptr(), scratch.numel() * scratch.element_size(), _stream(stream)),
+           "fusco_moe_few")
 
 
 def fusco_combine_two_hop(layout: Layout, y: torch.Tensor, w: torch.Tensor, partial: torch.Tensor,

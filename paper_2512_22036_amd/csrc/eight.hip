@@ -1,7 +1,8 @@
-// The MoE block in 8 bits for MI355X (gfx950): rows and weights to e4m3 and back (eight.h), the experts' products on them (products.h).  C entry points, declared in
-// fusco.h.
+// The MoE block in 8 bits for MI355X (gfx950): rows and weights to e4m3 and back (eight.h), the experts' products on them and the gradients from kept rows (products.h);
+// and the whole layer for a few tokens with weights of either type (few.h).  C entry points, declared in fusco.h.
 #include "block_host.h"
 #include "eight.h"
+#include "few.h"
 
 namespace {
 
@@ -57,6 +58,41 @@ ProductArgs eight_product(const fusco_layout *L, const void *d_x, const float *d
     a.scale_rows = blocks_of(outputs) * (gated ? 2 : 1);
     a.scales = blocks_of(C);
     return a;
+}
+
+// ---- the layer for a few tokens
+
+int few_check(const fusco_few *f)
+{
+    if (!f || f->N < 0 || f->N > FUSCO_MAX_FEW_TOKENS || f->E < 1 || f->E > FUSCO_MAX_E || f->k < 1 || f->k > FUSCO_MAX_K) return FUSCO_ERR_INVALID_ARG;
+    if ((f->weight_dtype != FUSCO_BF16 && f->weight_dtype != FUSCO_E4M3) || !dtype_ok(f->out_dtype)) return FUSCO_ERR_UNSUPPORTED;
+    const bool eight = f->weight_dtype == FUSCO_E4M3;
+    if (!row_ok(f->H) || !row_ok(f->I) || (eight && (f->H % 16 != 0 || f->I % 16 != 0))) return FUSCO_ERR_INVALID_ARG;
+    // loads inside one expert's weights, inside x and inside h are addressed with 31 bits
+    if (2 * (int64_t)f->I * f->H * (eight ? 1 : 2) >= (int64_t)kNowhere || (int64_t)f->N * f->k * f->I * 2 >= (int64_t)kNowhere || (int64_t)f->N * f->H * 2 >= (int64_t)kNowhere)
+        return FUSCO_ERR_INVALID_ARG;
+    return FUSCO_OK;
+}
+
+constexpr int kFewUnits = 16, kFewOutputs = 16;   // of a workgroup's block
+
+template <bool EIGHT>
+int launch_moe_few(const FewArgs &a, hipStream_t s)
+{
+    const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
+    const int64_t gated = (int64_t)slots * ((a.I + kFewUnits - 1) / kFewUnits) + 1, linear = (a.H + kFewOutputs - 1) / kFewOutputs;
+    const dim3 first((unsigned)gated), second((unsigned)linear);
+    if (a.N <= 16) {
+        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
+        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 16, 1, 2>), second, dim3(16 * kWave), 0, s, a);
+    } else if (a.N <= 32) {
+        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
+        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 2, EIGHT ? 1 : 2>), second, dim3(8 * kWave), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 2>), first, dim3(8 * kWave), 0, s, a);
+        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 4, 1>), second, dim3(8 * kWave), 0, s, a);
+    }
+    return launch_status();
 }
 
 }   // namespace
@@ -140,6 +176,30 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
     if (dw_dtype == FUSCO_F32) launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreF32, false, true>, a, (hipStream_t)stream);
     else launch_product(product_kernel<kAcross, kAcross, 256, 4, 2, kStoreBf16, false, true>, a, (hipStream_t)stream);
     return launch_status();
+}
+
+size_t fusco_moe_few_scratch_bytes(int32_t N, int32_t k, int32_t I)
+{
+    if (N < 0 || N > FUSCO_MAX_FEW_TOKENS || k < 1 || k > FUSCO_MAX_K || !row_ok(I)) return 0;
+    return (size_t)kUsedInts * 4 + (size_t)N * k * I * 4;
+}
+
+int fusco_moe_few(const fusco_few *f, const void *d_x, const int32_t *d_topk_idx, const float *d_w, const void *d_w_in, const float *d_w_in_scale, const void *d_w_out,
+                  const float *d_w_out_scale, void *d_out, void *d_scratch, size_t scratch_bytes, void *stream)
+{
+    const int rc = few_check(f);
+    if (rc != FUSCO_OK) return rc;
+    const bool empty = f->N == 0, eight = f->weight_dtype == FUSCO_E4M3;
+    const void *const p[] = {d_x, d_topk_idx, d_w, d_w_in, d_w_out, d_out, d_scratch}, *const scales[] = {d_w_in_scale, d_w_out_scale};
+    if (check_pointers(empty, p, 7) != FUSCO_OK || check_pointers(empty || !eight, scales, 2) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
+    if (empty) return FUSCO_OK;
+    if (scratch_bytes < fusco_moe_few_scratch_bytes(f->N, f->k, f->I)) return FUSCO_ERR_WORKSPACE;
+    FewArgs a = {};
+    a.x = (const char *)d_x; a.chosen = d_topk_idx; a.w = d_w;
+    a.w_in = (const char *)d_w_in; a.w_out = (const char *)d_w_out; a.w_in_scale = d_w_in_scale; a.w_out_scale = d_w_out_scale;
+    a.out = (char *)d_out; a.used = (int32_t *)d_scratch; a.h = (char *)d_scratch + kUsedInts * 4;
+    a.N = f->N; a.E = f->E; a.k = f->k; a.H = f->H; a.I = f->I; a.out_f32 = f->out_dtype == FUSCO_F32;
+    return eight ? launch_moe_few<true>(a, (hipStream_t)stream) : launch_moe_few<false>(a, (hipStream_t)stream);
 }
 
 }   // extern "C"

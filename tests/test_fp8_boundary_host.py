@@ -83,3 +83,41 @@ def test_gradients(lib):  # noqa: F811
     for stride, M, C in ((1, 64, 72), (1, 64, 144), (1, 4, 64), (1, 64, 0), (4096, 64, (1 << 19) + 16)):
         assert w(BUF, BUF, BUF, stride, BUF, 0, M, C, None) == -1, (stride, M, C)
     assert lib.fusco_experts_weight_grad_fp8(ctypes.byref(empty), None, None, None, 1, None, 0, 64, 64, None) == -1   # dw is written even then
+
+
+def few(**kw):
+    from paper_2512_22036_amd.binding import _CFew
+    return _CFew(**{**dict(N=4, E=8, k=2, H=64, I=32, weight_dtype=0, out_dtype=0), **kw})
+
+
+def test_few_struct_lies_as_in_the_header(tmp_path):
+    from paper_2512_22036_amd.binding import _CFew
+    names = [f for f, _ in _CFew._fields_]
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "fusco.h"', "int main(void) {"]
+    lines += ['printf("%%zu\\n", offsetof(fusco_few, %s));' % f for f in names] + ['printf("%zu\\n", sizeof(fusco_few));', "return 0; }"]
+    (tmp_path / "a.c").write_text("\n".join(lines))
+    subprocess.check_call(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(tmp_path / "a"), str(tmp_path / "a.c")])
+    said = [int(v) for v in subprocess.check_output([str(tmp_path / "a")]).split()]
+    assert said == [getattr(_CFew, f).offset for f in names] + [ctypes.sizeof(_CFew)]
+
+
+def test_few(lib):  # noqa: F811
+    need = lib.fusco_moe_few_scratch_bytes(4, 2, 32)
+    assert need >= 4 * 2 * 32 * 4 and lib.fusco_moe_few_scratch_bytes(65, 2, 32) == lib.fusco_moe_few_scratch_bytes(-1, 2, 32) == lib.fusco_moe_few_scratch_bytes(4, 65, 32) == 0
+    call = lambda f, *a: lib.fusco_moe_few(ctypes.byref(f), *a)
+    good = [BUF, BUF, BUF, BUF, None, BUF, None, BUF, BUF, need, None]
+    for bad in (dict(N=-1), dict(N=65), dict(E=0), dict(E=1025), dict(k=0), dict(k=65), dict(H=0), dict(H=12), dict(I=4), dict(I=-8), dict(H=1 << 20), dict(H=1 << 15, I=1 << 15)):
+        assert call(few(**bad), *good[:9], 1 << 40, None) == -1, bad
+    for bad in (dict(weight_dtype=1), dict(weight_dtype=3), dict(out_dtype=2), dict(out_dtype=-1)):
+        assert call(few(**bad), *good) == -3, bad
+    for i in (0, 1, 2, 3, 5, 7, 8):
+        assert call(few(), *[None if j == i else v for j, v in enumerate(good)]) == -1, i
+        assert call(few(), *[BUF + 8 if j == i else v for j, v in enumerate(good)]) == -1, i
+    assert call(few(), *good[:9], need - 1, None) == -2
+    eight = [BUF, BUF, BUF, BUF, BUF, BUF, BUF, BUF, BUF, need, None]
+    for i in (4, 6):
+        assert call(few(weight_dtype=2), *[None if j == i else v for j, v in enumerate(eight)]) == -1, i
+    for bad in (dict(H=72), dict(I=40)):
+        assert call(few(weight_dtype=2, **bad), *eight[:9], 1 << 20, None) == -1, bad
+    assert lib.fusco_moe_few(None, *good) == -1
+    assert call(few(N=0), None, None, None, None, None, None, None, None, None, 0, None) == 0
