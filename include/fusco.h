@@ -521,7 +521,7 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
  * The experts of an MoE layer for a few tokens (one to FUSCO_MAX_FEW_TOKENS), from their rows and routing to the weighted sum, without a layout:
  *     out[t, :] = sum_j w[t, j] * W_out[e] (silu(g) * u),   g and u = gate and up rows of W_in[e] times x[t, :],   e = topk_idx[t, j]
  * as fusco_plan_dispatch, fusco_experts_gated, fusco_experts_linear and fusco_combine compute it, in two launches that read the weights of the chosen
- * experts once.  Sums are fp32, silu(g) * u is kept to 16 bits (2^-17 of it), the result is rounded once.  Pairs whose expert is not in [0, E) count
+ * experts once.  Sums and silu(g) * u are fp32, the result is rounded once.  Pairs whose expert is not in [0, E) count
  * nothing; a token's equal experts count together.  An expert's weights reach only the tokens that chose it.
  * d_x [N, H] bf16, d_topk_idx and d_w [N, k], d_out [N, H] of out_dtype (FUSCO_BF16 or FUSCO_F32).  weight_dtype FUSCO_BF16: d_w_in [E, 2 I, H] and
  * d_w_out [E, H, I] as for fusco_experts_gated and fusco_experts_linear, H and I multiples of 8, scales NULL.  FUSCO_E4M3: weights and scales as for

@@ -80,18 +80,13 @@ template <bool EIGHT>
 int launch_moe_few(const FewArgs &a, hipStream_t s)
 {
     const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
-    const int64_t gated = (int64_t)slots * ((a.I + kFewUnits - 1) / kFewUnits) + 1, linear = (a.H + kFewOutputs - 1) / kFewOutputs;
-    const dim3 first((unsigned)gated), second((unsigned)linear);
-    if (a.N <= 16) {
-        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
-        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 16, 1, 2>), second, dim3(16 * kWave), 0, s, a);
-    } else if (a.N <= 32) {
-        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
-        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 2, EIGHT ? 1 : 2>), second, dim3(8 * kWave), 0, s, a);
-    } else {
-        hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 2>), first, dim3(8 * kWave), 0, s, a);
-        hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 4, 1>), second, dim3(8 * kWave), 0, s, a);
-    }
+    const int64_t gated = (int64_t)slots * ((a.I + kFewUnits - 1) / kFewUnits) + 1;
+    const int blocks = (a.H + kFewOutputs - 1) / kFewOutputs, groups = a.N <= 16 ? 1 : (a.N + 31) / 32;
+    const dim3 first((unsigned)gated), second((unsigned)((blocks + kXcds - 1) / kXcds * kXcds * groups));
+    if (a.N <= 32) hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
+    else hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 2>), first, dim3(8 * kWave), 0, s, a);
+    if (a.N <= 16) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 16, 1, EIGHT ? 1 : 2>), second, dim3(16 * kWave), 0, s, a);
+    else hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 2, EIGHT ? 1 : 2>), second, dim3(8 * kWave), 0, s, a);
     return launch_status();
 }
 
@@ -181,7 +176,7 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
 size_t fusco_moe_few_scratch_bytes(int32_t N, int32_t k, int32_t I)
 {
     if (N < 0 || N > FUSCO_MAX_FEW_TOKENS || k < 1 || k > FUSCO_MAX_K || !row_ok(I)) return 0;
-    return (size_t)kUsedInts * 4 + (size_t)N * k * I * 4;
+    return (size_t)kUsedInts * 4 + (size_t)N * k * I * 2 * kParts;
 }
 
 int fusco_moe_few(const fusco_few *f, const void *d_x, const int32_t *d_topk_idx, const float *d_w, const void *d_w_in, const float *d_w_in_scale, const void *d_w_out,

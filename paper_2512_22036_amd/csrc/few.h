@@ -2,8 +2,8 @@
 //
 // Bound by the weights of the chosen experts, every one of which is read once: few_gated_kernel reads those of the gated product, finds an expert's tokens in the
 // routing itself and leaves h in scratch memory; few_linear_kernel reads those of the down product and adds up a token's experts in registers.
-// Nothing is moved or planned in between.  h is kept as two numbers of bf16, its rounding and that of the rest (17 significant bits together), so that the only rounding
-// of the whole to 8 bits is that of the result.
+// Nothing is moved or planned in between.  h is kept as three numbers of bf16, its rounding and those of what is left, which hold an fp32 number: nothing is rounded to fewer
+// bits but a result of bf16.  (Two of them, 17 bits, were 2.5e-6 off in the norm where fp32 throughout is 8e-7.)
 //
 // Weights of e4m3 become bf16 on their way to the matrix instructions, which is exact; their scales are applied to the fp32 sums of 128 columns.
 #ifndef FUSCO_CSRC_FEW_H
@@ -21,10 +21,11 @@ struct FewArgs {
     const float *w_in_scale, *w_out_scale;
     char *out;                         // [N, H]
     int32_t *used;                     // scratch: how many experts any token has, and which, ascending
-    char *h;                           // scratch: [2, N k, I] bf16
+    char *h;                           // scratch: [kParts, N k, I] bf16
     int32_t N, E, k, H, I, out_f32;
 };
 
+constexpr int kParts = 3;
 constexpr int kUsedInts = FUSCO_MAX_E + 4;
 constexpr int kFewTokens = FUSCO_MAX_FEW_TOKENS;
 
@@ -194,23 +195,28 @@ __global__ __launch_bounds__(WAVES *kWave) void few_gated_kernel(FewArgs p)
                 up += sums[v][f + kOut][g][lane];
             }
             if (col >= n || a >= p.I) continue;
-            bf16x4 hi, lo;
+            f32x4 rest;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float h = silu(gate[q]) * up[q];
-                hi[q] = (__bf16)h;
-                lo[q] = (__bf16)(h - (float)hi[q]);
-            }
+            for (int q = 0; q < 4; ++q) rest[q] = silu(gate[q]) * up[q];
             const int64_t at = (int64_t)pairs[col] * p.I + a;
-            *(bf16x4 *)(p.h + at * 2) = hi;
-            *(bf16x4 *)(p.h + ((int64_t)P * p.I + at) * 2) = lo;
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) {
+                bf16x4 part;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    part[q] = (__bf16)rest[q];
+                    rest[q] -= (float)part[q];
+                }
+                *(bf16x4 *)(p.h + ((int64_t)i * P * p.I + at) * 2) = part;
+            }
         }
         __syncthreads();
     }
 }
 
-// A workgroup per block of 16 outputs of all tokens, which are the columns, 16 * G of them.  Its waves share the pieces of all experts that have tokens, each a run of them; a wave
-// that goes on to another expert adds what it has of the last one, times the tokens' weights, to the tokens that chose it and to no others.
+// A workgroup per block of 16 outputs and up to 16 * G tokens, which are the columns (the workgroups of one block's other tokens run on the same XCD at the same time and find
+// the weights in its L2).  Its waves share the pieces of all experts that have tokens, each a run of them; a wave that goes on to another expert
+// adds what it has of the last one, times the tokens' weights, to the tokens that chose it and to no others.
 template <bool EIGHT, int WAVES, int G, int CHUNKS>
 __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
 {
@@ -218,19 +224,24 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
     __shared__ int chosen[16 * G * FUSCO_MAX_K];
     __shared__ f32x4 sums[WAVES][G][kWave];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int P = p.N * p.k, a0 = blockIdx.x * 16, ld = p.I * (EIGHT ? 1 : 2);
-    for (int i = tid; i < P; i += WAVES * kWave) chosen[i] = p.chosen[i];
+    const int P = p.N * p.k, ld = p.I * (EIGHT ? 1 : 2);
+    const int groups = (p.N + 16 * G - 1) / (16 * G), block = (int)blockIdx.x / (kXcds * groups) * kXcds + (int)blockIdx.x % kXcds;
+    const int a0 = block * 16, t0 = (int)blockIdx.x / kXcds % groups * (16 * G), tokens = min(p.N - t0, 16 * G);
+    if (a0 >= p.H) return;
+    for (int i = tid; i < tokens * p.k; i += WAVES * kWave) chosen[i] = p.chosen[t0 * p.k + i];
     const int pieces = (p.I + Piece::kElements - 1) / Piece::kElements;
     const int64_t total = (int64_t)__builtin_amdgcn_readfirstlane(p.used[0]) * pieces;
     // blocks begin at different experts: the waves' runs are dealt out from another place in every block
-    const int run = (wave + blockIdx.x) % WAVES;
+    const int run = (wave + block) % WAVES;
     const int begin = (int)(total * run / WAVES), end = (int)(total * (run + 1) / WAVES);
     __syncthreads();
 
-    const __amdgpu_buffer_rsrc_t vh = view(p.h, (int64_t)P * p.I * 2), vl = view(p.h + (int64_t)P * p.I * 2, (int64_t)P * p.I * 2);
+    __amdgpu_buffer_rsrc_t vh[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) vh[i] = view(p.h + (int64_t)i * P * p.I * 2, (int64_t)P * p.I * 2);
     const uint32_t w_row = a0 + (lane & 15) < p.H ? (uint32_t)((lane & 15) * ld) : kNowhere;
     Piece w;
-    bf16x8 hi[G][Piece::kSteps], lo[G][Piece::kSteps];
+    bf16x8 h[G][Piece::kSteps][kParts];
     float scale = 1.0f, weight[G];
     uint32_t h_at[G];
     int e = 0, piece = begin % (pieces > 0 ? pieces : 1), at = begin / (pieces > 0 ? pieces : 1);
@@ -242,10 +253,11 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
             const int t = g * 16 + (lane & 15);
             h_at[g] = kNowhere;
             weight[g] = 0.0f;
-            for (int j = 0; j < p.k && t < p.N; ++j) {
+            for (int j = 0; j < p.k && t < tokens; ++j) {
                 if (chosen[t * p.k + j] != e) continue;
-                if (h_at[g] == kNowhere) h_at[g] = (uint32_t)((t * p.k + j) * (p.I * 2));
-                weight[g] += p.w[t * p.k + j];
+                const int pair = (t0 + t) * p.k + j;
+                if (h_at[g] == kNowhere) h_at[g] = (uint32_t)(pair * (p.I * 2));
+                weight[g] += p.w[pair];
             }
         }
     };
@@ -258,8 +270,8 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const uint32_t place = c < p.I && h_at[g] != kNowhere ? h_at[g] + c * 2 : kNowhere;
-                hi[g][s] = load_fragment(vh, place);
-                lo[g][s] = load_fragment(vl, place);
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) h[g][s][i] = load_fragment(vh[i], place);
             }
         }
         if (EIGHT) scale = p.w_out_scale[((int64_t)e * ((p.H + 127) / 128) + a0 / 128) * ((p.I + 127) / 128) + c0 / 128];
@@ -273,7 +285,7 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
     }
     for (int i = begin; i < end; ++i) {
         const Piece wn = w;
-        bf16x8 hn[G][Piece::kSteps], ln[G][Piece::kSteps];
+        bf16x8 hn[G][Piece::kSteps][kParts];
         float weight_now[G];
         bool chose[G];
 #pragma unroll
@@ -281,10 +293,9 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
             weight_now[g] = weight[g];
             chose[g] = h_at[g] != kNowhere;
 #pragma unroll
-            for (int s = 0; s < Piece::kSteps; ++s) {
-                hn[g][s] = hi[g][s];
-                ln[g][s] = lo[g][s];
-            }
+            for (int s = 0; s < Piece::kSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) hn[g][s][i] = h[g][s][i];
         }
         const float scale_now = scale;
         const bool last = piece == pieces - 1 || i == end - 1;   // of this expert here
@@ -301,10 +312,9 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
         for (int g = 0; g < G; ++g) {
             f32x4 part = EIGHT ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[g];
 #pragma unroll
-            for (int s = 0; s < Piece::kSteps; ++s) {
-                part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], hn[g][s], part, 0, 0, 0);
-                part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], ln[g][s], part, 0, 0, 0);
-            }
+            for (int s = 0; s < Piece::kSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], hn[g][s][i], part, 0, 0, 0);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 acc[g][q] = EIGHT ? fmaf(scale_now, part[q], acc[g][q]) : part[q];
@@ -323,8 +333,8 @@ __global__ __launch_bounds__(WAVES *kWave) void few_linear_kernel(FewArgs p)
         f32x4 v = sums[0][g][lane];
 #pragma unroll
         for (int s = 1; s < WAVES; ++s) v += sums[s][g][lane];
-        if (t >= p.N || a >= p.H) continue;
-        const int64_t to = (int64_t)t * p.H + a;
+        if (t >= tokens || a >= p.H) continue;
+        const int64_t to = (int64_t)(t0 + t) * p.H + a;
         if (p.out_f32) *(f32x4 *)(p.out + to * 4) = v;
         else store4(p.out, to, v);
     }

@@ -826,22 +826,28 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         held[1] = s.hold(1);
         s.put(held[0], slot0);
         s.put(held[1], slot1);
-        held[0] = s.hold(2);
-        held[1] = s.hold(3);
     }
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(0, i, slot0);
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(1, i, slot1);
     if constexpr (State::kSlots == 4) {
+        // kept rows are asked for before the other operand of their stage, as in the loop: the waits count on that order
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (KEPT) held[0] = s.hold(2);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < State::kLoads; ++i) s.load(2, i, slot2);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (KEPT) held[1] = s.hold(3);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < State::kLoads; ++i) s.load(3, i, slot3);
     }
     __builtin_amdgcn_sched_barrier(0);
     store(0, 0, 0, 0);   // nothing, but the stores are counted
-    s.template wait<State::kSlots - 1, kStores>();
+    // the first stage's rows of A are in LDS already, the second's too: two loads less are behind the first stage's than in the loop
+    s.template wait<State::kSlots - 1, kStores - (KEPT ? 2 : 0)>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     typename std::conditional<EIGHT, Eights<FB>, Slice<FA, FB>[2]>::type x;

@@ -1,7 +1,7 @@
 """The whole layer for a few tokens against the formulas in 64 bits.
 
 Tolerance.  fp32 sums of n exact products are at most n * 2^-23 * sum |terms| off (test_gpu_experts); with weights of e4m3 two more units for the scales.  h = silu(g) u
-carries the errors of g and u by its derivatives and (12 + |g|) units of its own, and is kept as a bf16 number and a bf16 rest: 2^-8 * 2^-8 of it.
+carries the errors of g and u by its derivatives and (12 + |g|) units of its own, and is kept as three numbers of bf16: 2^-24 of it is left.
 The second product and the tokens' weights, k of them, add their own sums; a result of bf16 is rounded by up to 2^-8 of itself, one of fp32 by 2^-24.
 
 An inner product's smallest rest may be below the normal numbers of bf16, 2^-126: TINY covers it."""
@@ -54,10 +54,10 @@ def definition(x, chosen, w, wide_in, wide_out, scaled):
         s = g * torch.sigmoid(g)
         h = s * u
         dh = 1.1 * dg * (u.abs() + du) + s.abs() * du + (12 + g.abs()) * U23 * h.abs()
-        dh = dh + BF16 * BF16 * (h.abs() + dh) + 2.0 ** -130
+        dh = dh + BF16 ** 3 * (h.abs() + dh) + 2.0 ** -130
         terms = (h.abs() + dh) @ wide_out[e].abs().t()
         out.index_add_(0, t, wt * (h @ wide_out[e].t()))
-        off.index_add_(0, t, wt * (dh @ wide_out[e].abs().t() + 2 * (I + more) * U23 * terms))   # both parts of h are added up
+        off.index_add_(0, t, wt * (dh @ wide_out[e].abs().t() + 3 * (I + more) * U23 * terms))   # three parts of h are added up
         size.index_add_(0, t, wt * terms)
     return out, off + (chosen.shape[1] + 24) * U23 * size   # the tokens' weights, the waves' parts
 
