@@ -69,24 +69,72 @@ int few_check(const fusco_few *f)
     const bool eight = f->weight_dtype == FUSCO_E4M3;
     if (!row_ok(f->H) || !row_ok(f->I) || (eight && (f->H % 16 != 0 || f->I % 16 != 0))) return FUSCO_ERR_INVALID_ARG;
     // loads inside one expert's weights, inside x and inside h are addressed with 31 bits
-    if (2 * (int64_t)f->I * f->H * (eight ? 1 : 2) >= (int64_t)kNowhere || (int64_t)f->N * f->k * f->I * 2 >= (int64_t)kNowhere || (int64_t)f->N * f->H * 2 >= (int64_t)kNowhere)
+    if (2 * (int64_t)f->I * f->H * (eight ? 1 : 2) >= (int64_t)kNowhere || (int64_t)f->N * f->k * f->I * 2 * kParts >= (int64_t)kNowhere || (int64_t)f->N * f->H * 2 >= (int64_t)kNowhere)
         return FUSCO_ERR_INVALID_ARG;
     return FUSCO_OK;
 }
 
-constexpr int kFewUnits = 16, kFewOutputs = 16;   // of a workgroup's block
+constexpr int kFewOutputs = 16;   // of a workgroup's block
 
+// Parts of the list of groups: where there are fewer blocks of outputs than compute units, as many (up to four) as leave the fewest units without work.  Down
+// product, parts 1 / 2 / 4, us: 128 blocks of 1408 (16 tokens, 64 experts, bf16) 77 / 47 / 47; 180 blocks of 1040 (5 tokens, 30 experts, bf16) 39 / 41 / 38; 256
+// blocks of 1280 (16 tokens, 83 experts, e4m3) 89 / 97 / 100.
+constexpr int kFewPartial = 4 * kCus;   // workgroups that leave sums
+int few_parts(int32_t H)
+{
+    const int blocks = (H + kFewOutputs - 1) / kFewOutputs;
+    if (blocks >= kCus) return 1;
+    int best = 1;
+    double most = 0.0;
+    for (int parts = 1; parts <= 4; ++parts) {
+        const double busy = (double)blocks * parts / (ceil((double)blocks * parts / kCus) * kCus);
+        if (busy > most + 0.05) {
+            most = busy;
+            best = parts;
+        }
+    }
+    return best;
+}
+
+// scratch: groups, listed pairs and their weights, parts that are done, h, sums of the parts, each on a boundary of 16 bytes
+struct FewScratch {
+    size_t listed, listed_w, arrived, h, partial, bytes;
+    FewScratch(int32_t N, int32_t k, int32_t I)
+    {
+        const size_t list = ((size_t)N * k + 4) / 4 * 16;
+        listed = list;
+        listed_w = 2 * list;
+        arrived = 3 * list;
+        h = arrived + kFewPartial * 4;
+        partial = h + (size_t)N * k * I * 2 * kParts;
+        bytes = partial + (size_t)kFewPartial * N * kFewOutputs * 4;
+    }
+};
+
+template <bool EIGHT, int F, int G>
+void launch_few_gated(const FewArgs &a, hipStream_t s)
+{
+    constexpr int kUnits = 8 * F, kWaves = 4;
+    const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
+    const int64_t grid = (int64_t)slots * ((a.I + kUnits - 1) / kUnits) + 1;   // and the one that makes the groups
+    hipLaunchKernelGGL((few_gated_kernel<EIGHT, F, kWaves, G, 2, G == 1 ? 4 : 3>), dim3((unsigned)grid), dim3(kWaves * kWave), 0, s, a);
+}
+
+// Gated product: blocks of 8 units in bf16 where those of 16 would leave less than four workgroups per compute unit (one token with 8 experts of 4096 x (2 x 1280), 640 blocks
+// of 16: 32 us / 35 with 16; 5 tokens with 30 experts of 2880 x (2 x 1040): 60 / 55; e4m3 20.7 / 19.5 for one token).  Its four waves hold two pieces each: 16 tokens with 83
+// experts of 4096 x (2 x 1280) in e4m3, four waves with one, two, three pieces 159 / 160 / 183 us, eight waves 177 / 186 / -; one expert's 2 x 16 columns at a time from 33 tokens on.
+// Down product: eight waves with two pieces of e4m3 or three of bf16: 16 tokens with 83 experts of 1280 x 4096 in e4m3, one, two, three pieces 103 / 91 / 89 us, sixteen waves 91 /
+// 95 / 95; one token 17.0 / 15.7 / 16.3; bf16, 5 tokens with 30 experts of 1040 x 2880 46 / 40 / 39.
 template <bool EIGHT>
 int launch_moe_few(const FewArgs &a, hipStream_t s)
 {
     const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
-    const int64_t gated = (int64_t)slots * ((a.I + kFewUnits - 1) / kFewUnits) + 1;
-    const int blocks = (a.H + kFewOutputs - 1) / kFewOutputs, groups = a.N <= 16 ? 1 : (a.N + 31) / 32;
-    const dim3 first((unsigned)gated), second((unsigned)((blocks + kXcds - 1) / kXcds * kXcds * groups));
-    if (a.N <= 32) hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 1>), first, dim3(8 * kWave), 0, s, a);
-    else hipLaunchKernelGGL((few_gated_kernel<EIGHT, 2, 8, 2>), first, dim3(8 * kWave), 0, s, a);
-    if (a.N <= 16) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 16, 1, EIGHT ? 1 : 2>), second, dim3(16 * kWave), 0, s, a);
-    else hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 2, EIGHT ? 1 : 2>), second, dim3(8 * kWave), 0, s, a);
+    if (a.N > 32) launch_few_gated<EIGHT, 2, 2>(a, s);
+    else if (!EIGHT && (int64_t)slots * ((a.I + 15) / 16) < 4 * kCus) launch_few_gated<EIGHT, EIGHT ? 2 : 1, 1>(a, s);
+    else launch_few_gated<EIGHT, 2, 1>(a, s);
+    const dim3 grid((unsigned)((a.H + kFewOutputs - 1) / kFewOutputs * a.parts)), block(8 * kWave);
+    if (a.N <= 16) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 16, 2, EIGHT ? 2 : 3, 4>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 64, 2, EIGHT ? 2 : 3, 4>), grid, block, 0, s, a);
     return launch_status();
 }
 
@@ -176,7 +224,7 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
 size_t fusco_moe_few_scratch_bytes(int32_t N, int32_t k, int32_t I)
 {
     if (N < 0 || N > FUSCO_MAX_FEW_TOKENS || k < 1 || k > FUSCO_MAX_K || !row_ok(I)) return 0;
-    return (size_t)kUsedInts * 4 + (size_t)N * k * I * 2 * kParts;
+    return FewScratch(N, k, I).bytes;
 }
 
 int fusco_moe_few(const fusco_few *f, const void *d_x, const int32_t *d_topk_idx, const float *d_w, const void *d_w_in, const float *d_w_in_scale, const void *d_w_out,
@@ -192,7 +240,12 @@ int fusco_moe_few(const fusco_few *f, const void *d_x, const int32_t *d_topk_idx
     FewArgs a = {};
     a.x = (const char *)d_x; a.chosen = d_topk_idx; a.w = d_w;
     a.w_in = (const char *)d_w_in; a.w_out = (const char *)d_w_out; a.w_in_scale = d_w_in_scale; a.w_out_scale = d_w_out_scale;
-    a.out = (char *)d_out; a.used = (int32_t *)d_scratch; a.h = (char *)d_scratch + kUsedInts * 4;
+    a.out = (char *)d_out;
+    const FewScratch at(f->N, f->k, f->I);
+    char *scratch = (char *)d_scratch;
+    a.groups = (int32_t *)scratch; a.listed = (int32_t *)(scratch + at.listed); a.listed_w = (float *)(scratch + at.listed_w); a.arrived = (uint32_t *)(scratch + at.arrived);
+    a.h = scratch + at.h; a.partial = (float *)(scratch + at.partial);
+    a.parts = few_parts(f->H);
     a.N = f->N; a.E = f->E; a.k = f->k; a.H = f->H; a.I = f->I; a.out_f32 = f->out_dtype == FUSCO_F32;
     return eight ? launch_moe_few<true>(a, (hipStream_t)stream) : launch_moe_few<false>(a, (hipStream_t)stream);
 }
