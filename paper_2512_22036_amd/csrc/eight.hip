@@ -111,30 +111,38 @@ struct FewScratch {
     }
 };
 
+int few_slots(const FewArgs &a) { return a.N * a.k < a.E ? a.N * a.k : a.E; }
+
 template <bool EIGHT, int F, int G>
 void launch_few_gated(const FewArgs &a, hipStream_t s)
 {
-    constexpr int kUnits = 8 * F, kWaves = 4;
-    const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
-    const int64_t grid = (int64_t)slots * ((a.I + kUnits - 1) / kUnits) + 1;   // and the one that makes the groups
-    hipLaunchKernelGGL((few_gated_kernel<EIGHT, F, kWaves, G, 2, G == 1 ? 4 : 3>), dim3((unsigned)grid), dim3(kWaves * kWave), 0, s, a);
+    constexpr int kUnits = 8 * F, kWaves = 4, kSimd = F == 4 ? 2 : G == 2 ? 3 : 4;
+    const int64_t grid = (int64_t)few_slots(a) * ((a.I + kUnits - 1) / kUnits) + 1;   // and the one that makes the groups
+    hipLaunchKernelGGL((few_gated_kernel<EIGHT, F, kWaves, G, 2, kSimd>), dim3((unsigned)grid), dim3(kWaves * kWave), 0, s, a);
 }
 
-// Gated product: blocks of 8 units in bf16 where those of 16 would leave less than four workgroups per compute unit (one token with 8 experts of 4096 x (2 x 1280), 640 blocks
-// of 16: 32 us / 35 with 16; 5 tokens with 30 experts of 2880 x (2 x 1040): 60 / 55; e4m3 20.7 / 19.5 for one token).  Its four waves hold two pieces each: 16 tokens with 83
-// experts of 4096 x (2 x 1280) in e4m3, four waves with one, two, three pieces 159 / 160 / 183 us, eight waves 177 / 186 / -; one expert's 2 x 16 columns at a time from 33 tokens on.
-// Down product: eight waves with two pieces of e4m3 or three of bf16: 16 tokens with 83 experts of 1280 x 4096 in e4m3, one, two, three pieces 103 / 91 / 89 us, sixteen waves 91 /
-// 95 / 95; one token 17.0 / 15.7 / 16.3; bf16, 5 tokens with 30 experts of 1040 x 2880 46 / 40 / 39.
+// Gated product, experts of 4096 x (2 x 1280), us: blocks of 8 units in bf16 where those of 16 would leave less than four workgroups per compute unit (one token with 8
+// experts, 640 blocks of 16: 32 / 35 with 16; 5 tokens with 30 experts of 2880 x (2 x 1040): 60 / 55; e4m3 for one token 20.7 / 19.5); blocks of 32, which take a row of x
+// half as often, where there are more than eight (64 tokens with all of 128 experts, e4m3 281 / 318, bf16 452 / 484; 16 tokens with 83, e4m3 158 / 160; but bf16 with one pair per
+// expert, 16 tokens with 41 of 64 experts of 2048 x (2 x 1408), 89 / 84); 2 x 16 columns at a time from eight pairs per expert on (64 tokens with 8 experts 44 / 51; 64 tokens with
+// 128 experts 474 / 452).  The four waves hold two pieces each: 16 tokens with 83 experts in e4m3, one, two, three pieces 159 / 160 / 183, eight waves 177 / 186.
+// Down product: eight waves with two pieces of e4m3 or three of bf16: 16 tokens with 83 experts of 1280 x 4096 in e4m3, one, two, three pieces 103 / 91 / 89, sixteen waves 91 /
+// 95 / 95; one token 17.0 / 15.7 / 16.3; bf16, 5 tokens with 30 experts of 1040 x 2880 46 / 40 / 39.  Groups of fifteen pairs from three per expert on: 64 tokens with 32 experts of
+// 1280 x 4096 in e4m3 79 / 93 with five.
 template <bool EIGHT>
 int launch_moe_few(const FewArgs &a, hipStream_t s)
 {
-    const int slots = a.N * a.k < a.E ? a.N * a.k : a.E;
-    if (a.N > 32) launch_few_gated<EIGHT, 2, 2>(a, s);
-    else if (!EIGHT && (int64_t)slots * ((a.I + 15) / 16) < 4 * kCus) launch_few_gated<EIGHT, EIGHT ? 2 : 1, 1>(a, s);
+    const int64_t blocks = (int64_t)few_slots(a) * ((a.I + 15) / 16);
+    const int pairs = a.N * a.k / a.E;   // per expert
+    if (pairs >= 8) launch_few_gated<EIGHT, 2, 2>(a, s);
+    else if (!EIGHT && blocks < 4 * kCus) launch_few_gated<EIGHT, EIGHT ? 2 : 1, 1>(a, s);
+    else if (blocks > 8 * kCus && (EIGHT || pairs >= 3)) launch_few_gated<EIGHT, 4, 1>(a, s);
     else launch_few_gated<EIGHT, 2, 1>(a, s);
     const dim3 grid((unsigned)((a.H + kFewOutputs - 1) / kFewOutputs * a.parts)), block(8 * kWave);
-    if (a.N <= 16) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 16, 2, EIGHT ? 2 : 3, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 64, 2, EIGHT ? 2 : 3, 4>), grid, block, 0, s, a);
+    constexpr int kDepth = EIGHT ? 2 : 3;
+    if (a.group > kFive) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 64, kManyFives, 2, kDepth, 2>), grid, block, 0, s, a);
+    else if (a.N <= 16) hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 16, 1, 2, kDepth, 4>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((few_linear_kernel<EIGHT, 8, 64, 1, 2, kDepth, 4>), grid, block, 0, s, a);
     return launch_status();
 }
 
@@ -246,6 +254,7 @@ int fusco_moe_few(const fusco_few *f, const void *d_x, const int32_t *d_topk_idx
     a.groups = (int32_t *)scratch; a.listed = (int32_t *)(scratch + at.listed); a.listed_w = (float *)(scratch + at.listed_w); a.arrived = (uint32_t *)(scratch + at.arrived);
     a.h = scratch + at.h; a.partial = (float *)(scratch + at.partial);
     a.parts = few_parts(f->H);
+    a.group = f->N * f->k >= 3 * f->E ? kFive * kManyFives : kFive;
     a.N = f->N; a.E = f->E; a.k = f->k; a.H = f->H; a.I = f->I; a.out_f32 = f->out_dtype == FUSCO_F32;
     return eight ? launch_moe_few<true>(a, (hipStream_t)stream) : launch_moe_few<false>(a, (hipStream_t)stream);
 }

@@ -20,7 +20,7 @@ struct FewArgs {
     const char *w_in, *w_out;          // [E, 2 I, H], [E, H, I]
     const float *w_in_scale, *w_out_scale;
     char *out;                         // [N, H]
-    int32_t *groups;                   // scratch: how many groups there are; [N k] groups: expert | pairs << 10 | place of the first pair << 13
+    int32_t *groups;                   // scratch: how many groups there are; [N k] groups: expert | pairs << 10 | place of the first pair << 14
     int32_t *listed;                   // scratch: [N k] pairs, group by group
     float *listed_w;                   // scratch: [N k] their weights
     float *partial;                    // scratch: [blocks of outputs, parts, N, 16] sums of the parts of the groups, where there is more than one
@@ -28,11 +28,13 @@ struct FewArgs {
     char *h;                           // scratch: [kParts, N k, I] bf16
     int32_t N, E, k, H, I, out_f32;
     int32_t parts;                     // of the list of groups, a workgroup of few_linear_kernel each
+    int32_t group;                     // pairs of a group: kFive, or kManyFives times that
 };
 
 constexpr int kParts = 3;
-constexpr int kGroup = 5;   // pairs: kParts columns each of the sixteen of a matrix instruction
-static_assert(FUSCO_MAX_E <= 1 << 10 && kGroup < 1 << 3 && FUSCO_MAX_FEW_TOKENS * FUSCO_MAX_K <= 1 << 18, "a group in 32 bits");
+constexpr int kFive = 5;       // pairs: kParts columns each of the sixteen of a matrix instruction
+constexpr int kManyFives = 3;
+static_assert(FUSCO_MAX_E <= 1 << 10 && kFive * kManyFives < 1 << 4 && FUSCO_MAX_FEW_TOKENS * FUSCO_MAX_K <= 1 << 17, "a group in 31 bits");
 constexpr int kFewTokens = FUSCO_MAX_FEW_TOKENS;
 
 // A wave's part of 16 weight rows and the rows that they are multiplied with, one piece of the sum: CHUNKS times 64 bytes of a row, within one block of scales.
@@ -70,7 +72,7 @@ struct FewPiece {
     }
 };
 
-// The pairs by expert, in groups of up to kGroup of one expert, in ascending order throughout, for few_linear_kernel.  Pairs that name no expert are left out; a token that names
+// The pairs by expert, in groups of up to p.group of one expert, in ascending order throughout, for few_linear_kernel.  Pairs that name no expert are left out; a token that names
 // one several times is in its list once, with the weights together.  `key` and `lists` are LDS.
 template <int WAVES>
 __device__ __forceinline__ void few_groups(const FewArgs &p, int16_t *__restrict__ key, int (*__restrict__ lists)[FUSCO_MAX_E])
@@ -95,7 +97,7 @@ __device__ __forceinline__ void few_groups(const FewArgs &p, int16_t *__restrict
     if (wave == 0) {
         int groups = 0, pairs = 0;
         for (int e0 = 0; e0 < p.E; e0 += kWave) {
-            const int n = e0 + lane < p.E ? count[e0 + lane] : 0, g = (n + kGroup - 1) / kGroup;
+            const int n = e0 + lane < p.E ? count[e0 + lane] : 0, g = (n + p.group - 1) / p.group;
             int g_sum = g, n_sum = n;
 #pragma unroll
             for (int d = 1; d < kWave; d *= 2) {
@@ -117,7 +119,7 @@ __device__ __forceinline__ void few_groups(const FewArgs &p, int16_t *__restrict
     __syncthreads();
     for (int e = wave; e < p.E; e += WAVES) {
         const int n = count[e], first = pairs_before[e];
-        for (int g = lane; g * kGroup < n; g += kWave) p.groups[1 + groups_before[e] + g] = e | min(n - g * kGroup, kGroup) << 10 | (first + g * kGroup) << 13;
+        for (int g = lane; g * p.group < n; g += kWave) p.groups[1 + groups_before[e] + g] = e | min(n - g * p.group, p.group) << 10 | (first + g * p.group) << 14;
         int done = 0;
         for (int base = 0; base < P && done < n; base += kWave) {
             const bool mine = base + lane < P && key[base + lane] == e;
@@ -294,8 +296,9 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
 // A workgroup per block of 16 outputs of all tokens and part of the pieces of all groups.  Its waves share them, each a run of them.  The three parts of h of a group's pairs are columns of
 // their own, five by five, so that one load and one matrix instruction take them all (in columns of the tokens, with a load and an instruction for each part: 16 tokens
 // with 8 of 128 experts of 4096 x 1280 in e4m3 147 us, a quarter of the memory's rate).  A wave that goes on to another group adds up the parts of the last one and adds them, times
-// the tokens' weights, to sums of its own in LDS, of the group's tokens and no others.  Weights are DEPTH pieces ahead of their use, h, from the L2, one.
-template <bool EIGHT, int WAVES, int TOKENS, int CHUNKS, int DEPTH, int SIMD>
+// the tokens' weights, to sums of its own in LDS, of the group's tokens and no others.  Weights are DEPTH pieces ahead of their use, h, from the L2, one.  A group has up to
+// FIVES times five pairs.
+template <bool EIGHT, int WAVES, int TOKENS, int FIVES, int CHUNKS, int DEPTH, int SIMD>
 __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_linear_kernel(FewArgs p)
 {
     typedef FewPiece<EIGHT, CHUNKS> Piece;
@@ -317,7 +320,7 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_linear_kernel(FewArgs 
 
     const __amdgpu_buffer_rsrc_t vh = view(p.h, (int64_t)kParts * P * p.I * 2);
     const uint32_t w_row = a0 + (lane & 15) < p.H ? (uint32_t)((lane & 15) * ld) : kNowhere;
-    const int column = lane & 15, in_group = column % kGroup, part = column / kGroup;
+    const int column = lane & 15, in_five = column % kFive, part = column / kFive;
     // a place in the list of all groups' pieces
     struct Place {
         int at, piece;
@@ -338,30 +341,50 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_linear_kernel(FewArgs 
         if (EIGHT) scale[d] = p.w_out_scale[((int64_t)e * ((p.H + 127) / 128) + a0 / 128) * ((p.I + 127) / 128) + (more ? c0 / 128 : 0)];
         weights.next(pieces);
     };
-    bf16x8 h[Piece::kSteps];
-    uint32_t h_at = kNowhere;   // this lane's column in h
-    int token = 0;              // lanes of the first part: the token of their pair, and the weight that it gives the expert
-    float weight = 0.0f;
-    bool chose = false;
+    bf16x8 h[FIVES][Piece::kSteps];
+    uint32_t h_at[FIVES];       // this lane's columns in h
+    int token[FIVES];           // lanes of the first part: the token of their pair, and the weight that it gives the expert
+    float weight[FIVES];
+    bool chose[FIVES];
+    int fives = 0;              // of this group
     auto open = [&] {
-        const int group = __builtin_amdgcn_readfirstlane(groups[1 + rows.at]), place = (group >> 13) + in_group;
-        chose = in_group < (group >> 10 & 7) && part < kParts;
-        h_at = kNowhere;
-        if (!chose) return;
-        const int pair = listed[place];
-        token = pair / p.k;
-        weight = p.listed_w[place];
-        h_at = (uint32_t)((part * P + pair) * (p.I * 2));
+        const int group = __builtin_amdgcn_readfirstlane(groups[1 + rows.at]), n = group >> 10 & 15;
+        fives = (n + kFive - 1) / kFive;
+#pragma unroll
+        for (int b = 0; b < FIVES; ++b) {
+            const int i = b * kFive + in_five;
+            chose[b] = i < n && part < kParts;
+            h_at[b] = kNowhere;
+            if (!chose[b]) continue;
+            const int place = (group >> 14) + i, pair = listed[place];
+            token[b] = pair / p.k;
+            weight[b] = p.listed_w[place];
+            h_at[b] = (uint32_t)((part * P + pair) * (p.I * 2));
+        }
     };
     auto load_h = [&](bool more) {
         const int c0 = more ? rows.piece * Piece::kElements : p.I;
 #pragma unroll
-        for (int s = 0; s < Piece::kSteps; ++s) {
-            const int c = c0 + Piece::element(lane, s);
-            h[s] = load_fragment(vh, c < p.I && h_at != kNowhere ? h_at + c * 2 : kNowhere);
+        for (int b = 0; b < FIVES; ++b) {
+            if (b > 0 && b >= fives) break;
+#pragma unroll
+            for (int s = 0; s < Piece::kSteps; ++s) {
+                const int c = c0 + Piece::element(lane, s);
+                h[b][s] = load_fragment(vh, c < p.I && h_at[b] != kNowhere ? h_at[b] + c * 2 : kNowhere);
+            }
         }
     };
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[FIVES];
+#pragma unroll
+    for (int b = 0; b < FIVES; ++b) {
+        acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        h_at[b] = kNowhere;
+        token[b] = 0;
+        weight[b] = 0.0f;
+        chose[b] = false;
+#pragma unroll
+        for (int s = 0; s < Piece::kSteps; ++s) h[b][s] = {};
+    }
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) load(begin + d < end, d);
     if (begin < end) open();
@@ -372,35 +395,49 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_linear_kernel(FewArgs 
             const int i = i0 + d;
             if (i >= end) break;
             const Piece wn = w[d];
-            bf16x8 hn[Piece::kSteps];
+            bf16x8 hn[FIVES][Piece::kSteps];
+            float weight_now[FIVES];
+            int token_now[FIVES];
+            bool chose_now[FIVES];
 #pragma unroll
-            for (int s = 0; s < Piece::kSteps; ++s) hn[s] = h[s];
-            const float scale_now = scale[d], weight_now = weight;
-            const int token_now = token;
-            const bool chose_now = chose;
-            const int at = rows.at;
+            for (int b = 0; b < FIVES; ++b) {
+                weight_now[b] = weight[b];
+                token_now[b] = token[b];
+                chose_now[b] = chose[b];
+#pragma unroll
+                for (int s = 0; s < Piece::kSteps; ++s) hn[b][s] = h[b][s];
+            }
+            const float scale_now = scale[d];
+            const int at = rows.at, fives_now = fives;
             rows.next(pieces);
             const bool more = i + 1 < end;
             if (more && rows.at != at) open();
             load_h(more);
             load(i + DEPTH < end, d);
-            f32x4 sum = EIGHT ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc;
+            bf16x8 a[Piece::kSteps];
 #pragma unroll
-            for (int s = 0; s < Piece::kSteps; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wn.operand(s), hn[s], sum, 0, 0, 0);
+            for (int s = 0; s < Piece::kSteps; ++s) a[s] = wn.operand(s);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc[q] = EIGHT ? fmaf(scale_now, sum[q], acc[q]) : sum[q];
-            if (rows.at != at || !more) {   // the last piece of this group here
-                f32x4 v = acc;
+            for (int b = 0; b < FIVES; ++b) {
+                if (b > 0 && b >= fives_now) break;
+                f32x4 sum = EIGHT ? f32x4{0.0f, 0.0f, 0.0f, 0.0f} : acc[b];
 #pragma unroll
-                for (int j = 1; j < kParts; ++j)
+                for (int s = 0; s < Piece::kSteps; ++s) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[s], hn[b][s], sum, 0, 0, 0);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[q] += __shfl(acc[q], (lane & 48) | ((column + j * kGroup) & 15));
-                if (chose_now && part == 0) {
-                    f32x4 &to = sums[wave][token_now][lane >> 4];
+                for (int q = 0; q < 4; ++q) acc[b][q] = EIGHT ? fmaf(scale_now, sum[q], acc[b][q]) : sum[q];
+                if (rows.at != at || !more) {   // the last piece of this group here
+                    f32x4 v = acc[b];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) to[q] = fmaf(weight_now, v[q], to[q]);
+                    for (int j = 1; j < kParts; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) v[q] += __shfl(acc[b][q], (lane & 48) | ((column + j * kFive) & 15));
+                    if (chose_now[b] && part == 0) {
+                        f32x4 &to = sums[wave][token_now[b]][lane >> 4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) to[q] = fmaf(weight_now[b], v[q], to[q]);
+                    }
+                    acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
                 }
-                acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             }
         }
     }

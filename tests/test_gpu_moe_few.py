@@ -70,7 +70,7 @@ def within(got, want, off, dtype):
 
 SIZES = [(1, 1, 1, 16, 16), (1, 8, 2, 64, 48), (1, 16, 8, 512, 256), (2, 5, 3, 144, 32), (3, 4, 4, 272, 400), (5, 60, 6, 1040, 528), (8, 3, 2, 208, 1040), (15, 128, 8, 256, 128), (16, 32, 4, 640, 272),
          (17, 8, 2, 384, 208), (31, 64, 6, 528, 144), (32, 2, 1, 128, 128), (33, 16, 4, 272, 336), (64, 128, 8, 256, 192), (64, 3, 3, 400, 272), (64, 1024, 1, 64, 32), (7, 2, 8, 128, 64),
-         (2, 1024, 64, 48, 16), (64, 80, 64, 32, 16)]
+         (2, 1024, 64, 48, 16), (64, 80, 64, 32, 16), (64, 128, 8, 144, 288), (20, 128, 8, 80, 304), (64, 32, 4, 2064, 48)]
 
 
 @pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
