@@ -64,6 +64,15 @@ __device__ __forceinline__ void to_lds_single(__amdgpu_buffer_rsrc_t from, char 
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_byte *)to, 4, (int)offset, uniform, 0, 0);
 }
 
+typedef int words8 __attribute__((ext_vector_type(8)));
+
+// two pieces of 16 bytes as an operand of the matrix instructions
+__device__ __forceinline__ words8 joined(const bf16x8 (&v)[2])
+{
+    typedef int words __attribute__((ext_vector_type(4)));
+    return __builtin_shufflevector(__builtin_bit_cast(words, v[0]), __builtin_bit_cast(words, v[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
 // One operand of a tile: where a stage of it (KC elements of the summed dimension) comes from and how it lies in LDS.  A fragment is 32 outputs
 // by 16 elements of the sum, slice `ks` of the stage; lane l has output l % 32 and elements l / 32 * 8 + 0 .. 7.
 //   OUT (operand A): the outputs of a fragment are dealt out so that the 16 results of a lane are neighbours: output i of the matrix
@@ -74,8 +83,11 @@ __device__ __forceinline__ void to_lds_single(__amdgpu_buffer_rsrc_t from, char 
 //            lanes takes one window of each of four rows.
 //   PLACES (kAlongC): how the rows of a thread's loads are found.  kOwnPlaces: kept in registers.  kEvenPlaces: 64 rows further down with every load, which is left to
 //   the view it is made through; kPairedPlaces: the same for gate rows and, every other load, the up rows of the same units.
+//   RUN (kAlongC, e4m3): fragments of 16 outputs by 128 elements of the sum, all of a stage; lane l has output l % 16 and the chunks l / 16 and l / 16 + 4.  Operand A deals
+//   outputs so that those of a lane come in runs of RUN neighbours: output i of fragment f is row (i >> 2) * RUN + (f % (RUN / 4)) * 4 + (i & 3) of 4 * RUN.  Operand B
+//   (RUN 0) keeps its order.  Again the lanes that are served together hit all banks.
 enum { kOwnPlaces, kEvenPlaces, kPairedPlaces };
-template <int MODE, int W, int KC, bool OUT, int PLACES = kOwnPlaces>
+template <int MODE, int W, int KC, bool OUT, int PLACES = kOwnPlaces, int RUN = 0>
 struct Operand {
     static constexpr int kBytes = W * KC * 2;
     static constexpr int kRowLanes = KC / 8;   // kAlongC: lanes that load one row
@@ -124,7 +136,11 @@ struct Operand {
 
     // Load i of thread tid: which row of the stage's LDS (an output for kAlongC, a c for kAcross), and the first output (kAcross)
     static __device__ __forceinline__ int row_of(int i, int tid) { return MODE == kAlongC ? (i * kTileThreads + tid) / kRowLanes : (i * kTileThreads + tid) / (W / 8); }
-    static __device__ __forceinline__ int swizzle(int row) { return KC == 64 ? row >> 1 & 7 : row >> 2 & 3; }
+    static __device__ __forceinline__ int swizzle(int row)
+    {
+        if (RUN > 0) return (row / (RUN > 0 ? RUN : 1) & 3) << 1 | (row >> 1 & 1);
+        return KC == 64 ? row >> 1 & 7 : row >> 2 & 3;
+    }
     static __device__ __forceinline__ int chunk_of(int tid) { return (tid & (kRowLanes - 1)) ^ swizzle(tid / kRowLanes); }
     static __device__ __forceinline__ int output_of(int i, int tid) { return ((tid & (W / 8 - 1)) ^ ((row_of(i, tid) & 3) << 2)) * 8; }
 
@@ -139,6 +155,20 @@ struct Operand {
         const int c = (lane >> 5) * 8 + (lane >> 2 & 3), m = lane & 3, half = lane >> 4 & 1;
         const int output = OUT ? (m & 1) * 16 + (half * 2 + (m >> 1)) * 4 : half * 16 + m * 4;
         return c * (W * 2) + (((first >> 5) ^ (c & 3)) << 6) + output * 2;
+    }
+
+    // e4m3: where the wave's first fragment begins, and fragment f
+    static __device__ __forceinline__ uint32_t lane_at8(int lane, int first)
+    {
+        const int i = lane & 15, row = RUN > 0 ? (i >> 2) * RUN + (i & 3) : i;
+        return (first + row) * (KC * 2) + (((lane >> 4) ^ swizzle(row)) << 4);
+    }
+    static __device__ __forceinline__ words8 fragment8(const char *lds, uint32_t at, int f)
+    {
+        constexpr int kEach = RUN > 0 ? RUN / 4 : 1;   // fragments whose outputs share runs
+        const int down = RUN > 0 ? f / kEach * (4 * RUN) + f % kEach * 4 : f * 16;
+        const bf16x8 v[2] = {*(const bf16x8 *)(lds + at + down * (KC * 2)), *(const bf16x8 *)(lds + (at ^ 64) + down * (KC * 2))};
+        return joined(v);
     }
 
     static __device__ __forceinline__ bf16x8 fragment(const char *lds, uint32_t at, int f, int ks)
@@ -180,7 +210,8 @@ template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool
 struct TileState {
     static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
     static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no register to spare
-    typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces> A;
+    static constexpr int kRun = GATED && FA == 2 ? 8 : 16;   // a lane's neighbouring outputs
+    typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
     typedef Operand<BMODE, BB, kStageC, false, kSpared ? kEvenPlaces : kOwnPlaces> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes, kLoads = A::kLoads;
     static constexpr int kScaleLoads = EIGHT ? 1 : 0, kSlotBytes = kStageBytes + (EIGHT ? kTileThreads * 4 : 0), kWeightScales = kStageBytes + BB * 4;
@@ -205,12 +236,17 @@ struct TileState {
         const int i = s + turn;
         return s >= stages ? stages : i >= stages ? i - stages : i;
     }
-    __device__ __forceinline__ void load(int s, int i, char *slot) const { load(s, i, slot, a.place()); }
-    __device__ __forceinline__ void load(int s, int i, char *slot, const typename A::Place &place) const   // one of both operands, whose rows are as long
+    struct Places {
+        typename A::Place a;
+        typename B::Place b;
+    };
+    __device__ __forceinline__ Places places() const { return {a.place(), b.place()}; }
+    __device__ __forceinline__ void load(int s, int i, char *slot) const { load(s, i, slot, places()); }
+    __device__ __forceinline__ void load(int s, int i, char *slot, const Places &place) const
     {
         const int at = stage_of(s);
-        if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place);
-        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, {place.chunk, place.at});
+        if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place.a);
+        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, place.b);
         if (EIGHT && i == 0) {
             const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
             to_lds_single(view(scales, scale_bytes), slot + kStageBytes + wave * (kWave * 4), at < stages ? place : kNowhere, at * 4);
@@ -305,89 +341,86 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
     }
 }
 
-// Stages of e4m3 operands: a matrix instruction takes 64 elements of the sum, and the two of a stage and fragment pair make one partial sum, which is
-// scaled and added to the pair's results.  A wave adds while the other one of its SIMD multiplies; a second partial sum on the way would take
-// registers that the tile of 256 x 256 does not have (and fragments of a are read where those before them were).
-typedef int words8 __attribute__((ext_vector_type(8)));
+// Stages of e4m3 operands: a matrix instruction takes a whole stage of 16 x 16 outputs, and its result, scaled, is added to the pair's sums two instructions
+// later.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
+// fragments ahead.)
+constexpr int kRing = 4, kAhead = 2;   // fragments of a in registers, and how far ahead of their use they are read
+constexpr int kLate = 2, kParts8 = 4;  // instructions between a product and its use, products in registers
 
 template <int FB>
 struct Eights {
-    words8 a[2], b[FB][2];      // fragments: one of a, all of b; two halves of the stage
+    words8 a[kRing], b[FB];
     float rows[FB], weight[2];  // scales of the stage: of the lane's rows of b, of the wave's rows of a (gated: gate and up)
+    float scale[FB];            // both together, as they are in use
+    f32x4 part[kParts8];
 };
-
-// two pieces of 16 bytes as an operand of the matrix instructions
-__device__ __forceinline__ words8 joined(const bf16x8 (&v)[2])
-{
-    typedef int words __attribute__((ext_vector_type(4)));
-    return __builtin_shufflevector(__builtin_bit_cast(words, v[0]), __builtin_bit_cast(words, v[1]), 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-template <typename Op>
-__device__ __forceinline__ words8 half_stage(const char *lds, uint32_t at, int f, int half)
-{
-    const bf16x8 v[2] = {Op::fragment(lds, at, f, 2 * half), Op::fragment(lds, at, f, 2 * half + 1)};
-    return joined(v);
-}
 
 template <bool GATED, int FB, typename S>
 __device__ __forceinline__ void read_scales(const S &t, const char *slot, int j, Eights<FB> &x)
 {
-    x.rows[j] = *(const float *)(slot + S::kStageBytes + t.row_scale_lane + j * 128);
+    x.rows[j] = *(const float *)(slot + S::kStageBytes + t.row_scale_lane + j * 64);
     if (j > 0) return;
     x.weight[0] = *(const float *)(slot + S::kWeightScales + t.weight_scale_wave);
     if (GATED) x.weight[1] = *(const float *)(slot + S::kWeightScales + 4);
 }
 
-template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x16 (&acc)[FA][FB])
+template <int FA, int FB>
+__device__ __forceinline__ void add_part(Eights<FB> &x, int m, f32x4 (&acc)[FA][FB])
 {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc[m / FB][m % FB][q] = fmaf(x.scale[m % FB], x.part[m % kParts8][q], acc[m / FB][m % FB][q]);
+}
+
+template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
+__device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+{
+    static_assert(FA % kRing == 0 && FA * FB % kParts8 == 0 && FB >= kLate, "registers take turns");
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
     asm volatile("" : "+v"(a_at), "+v"(b_at));
-    float scale[GATED ? 2 : 1][FB];
-#pragma unroll
-    for (int g = 0; g < (GATED ? 2 : 1); ++g)
-#pragma unroll
-        for (int j = 0; j < FB; ++j) scale[g][j] = x.weight[g] * x.rows[j];
+    typename S::Places place = {};
 #pragma unroll
     for (int f = 0; f < FA; ++f) {
-        const bool last = f == FA - 1;
-        if (last) {
+        const bool past = f + kAhead >= FA;   // reads are of the next stage
+        if (f + kAhead == FA) {
             t.template wait<S::kSlots - 2, STORES>();
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
+            place = t.places();
         }
-        if (!ACTIVE && !last) continue;
-        typename S::A::Place place = {};
-        if (last) place = t.a.place();
+        if (!ACTIVE && !past) continue;
 #pragma unroll
         for (int j = 0; j < FB; ++j) {
-            f32x16 part = {};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (ACTIVE) part = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x.a[h], x.b[j][h], part, 0, 0, 0, 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                if (j == FB - 1) x.a[h] = half_stage<typename S::A>(last ? nxt : cur, a_at, (f + 1) % FA, h);
-                if (last) x.b[j][h] = half_stage<typename S::B>(nxt + S::A::kBytes, b_at, j, h);
+            const int m = f * FB + j;
+            if (ACTIVE) {
+                const f32x4 zero = {};
+                x.part[m % kParts8] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x.a[f % kRing], x.b[j], zero, 0, 0, 0, 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (last) {
-                read_scales<GATED>(t, nxt, j, x);
-                constexpr int kEach = (S::kLoads + FB - 1) / FB;
+            if (j == 0) x.a[(f + kAhead) % kRing] = S::A::fragment8(past ? nxt : cur, a_at, (f + kAhead) % FA);
+            if (f == FA - 1) x.b[j] = S::B::fragment8(nxt + S::A::kBytes, b_at, j);
+            if (past) {
+                const int step = (f + kAhead - FA) * FB + j;
+                constexpr int kEach = (S::kLoads + kAhead * FB - 1) / (kAhead * FB);
 #pragma unroll
-                for (int i = j * kEach; i < (j + 1) * kEach && i < S::kLoads; ++i) t.load(ask, i, cur, place);
+                for (int i = step * kEach; i < (step + 1) * kEach && i < S::kLoads; ++i) t.load(ask, i, cur, place);
             }
             if (ACTIVE) {
-#pragma unroll
-                for (int q = 0; q < 16; ++q) acc[f][j][q] = fmaf(scale[GATED ? f / (FA / 2) : 0][j], part[q], acc[f][j][q]);
+                const int of = (m + FA * FB - kLate) % (FA * FB);
+                // the pair's scale changes with the stage and from gate to up rows
+                if (of < FB) x.scale[of] = x.weight[0] * x.rows[of];
+                if (GATED && of / FB == FA / 2) x.scale[of % FB] = x.weight[1] * x.rows[of % FB];
+                add_part(x, of, acc);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            if (f == FA - 1 && j == FB - 1)
+#pragma unroll
+                for (int i = 0; i < FB; ++i) read_scales<GATED>(t, nxt, i, x);
         }
     }
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_turn8(const S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x16 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_turn8(const S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
     static_assert(S::kSlots == 2, "operands along c");
     tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, ask, x, acc);
@@ -563,11 +596,11 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 
     State s;
     s.wave = wave;
-    s.a_lane = State::A::lane_at(lane, wa * FA * 32);
-    s.b_lane = State::B::lane_at(lane, wb * FB * 32);
+    s.a_lane = EIGHT ? State::A::lane_at8(lane, wa * FA * 32) : State::A::lane_at(lane, wa * FA * 32);
+    s.b_lane = EIGHT ? State::B::lane_at8(lane, wb * FB * 32) : State::B::lane_at(lane, wb * FB * 32);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
     if constexpr (EIGHT) {
-        s.row_scale_lane = (wb * FB * 32 + (lane & 31)) * 4;
+        s.row_scale_lane = (wb * FB * 32 + (lane & 15)) * 4;
         s.weight_scale_wave = kGated ? 0 : wa * FA * 32 / 128 * 4;
         asm volatile("" : "+v"(s.row_scale_lane), "+v"(s.weight_scale_wave));
     }
@@ -693,8 +726,60 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 
     // Lane l holds, of fragment (f, j), the outputs a = 32 * f + l / 32 * 16 + 0 .. 15 of b = 32 * j + l % 32.
     constexpr int kOutA = kGated ? FA / 2 : FA;
-    f32x16 acc[FA][FB];
-    auto store = [&](int a0, int a_left, int b_left, int64_t row0) {
+    typename std::conditional<EIGHT, f32x4[2 * FA][2 * FB], f32x16[FA][FB]>::type acc;
+    // e4m3: a lane holds runs of kRun outputs (gated: units, gate and up) of b = 16 * j + l % 16; the four lanes of one b hold neighbouring runs
+    auto store_runs = [&](const auto &acc, int a0, int a_left, int b_left, int64_t row0) __attribute__((always_inline)) {
+        constexpr int kRun = State::kRun, kEach = kRun / 4, kRuns = (kGated ? FA : 2 * FA) / kEach;   // fragments of a run, runs of a wave
+        const int rows = b_left < BB ? b_left : BB;
+        Target out, pre;
+        out.open(p.out, row0, (int64_t)p.NA * 2, (int64_t)a0 * 2, rows);
+        if (kGated && p.pre) pre.open(p.pre, row0, (int64_t)p.NA * 4, (int64_t)a0 * 2, rows);
+        int lane = tid & 63;
+        asm volatile("" : "+v"(lane));
+#pragma unroll
+        for (int j = 0; j < 2 * FB; ++j) {
+            const int b = wb * FB * 32 + j * 16 + (lane & 15);
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) {
+                const int a = wa * (kGated ? FA * 16 : FA * 32) + (r * 4 + (lane >> 4)) * kRun;
+                words4 v[kRun / 8];
+#pragma unroll
+                for (int h = 0; h < kRun / 8; ++h) {
+                    float value[8], up[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        value[q] = acc[r * kEach + h * 2 + q / 4][j][q % 4];
+                        if (kGated) up[q] = acc[FA + r * kEach + h * 2 + q / 4][j][q % 4];
+                    }
+                    if (kGated) {
+                        if (p.pre) {
+                            const uint32_t to = a + h * 8 < a_left && b < b_left ? b * pre.ld + (a + h * 8) * 2 : kNowhere;
+                            pre.put8(value, to);
+                            pre.put8(up, to + (uint32_t)p.NA * 2);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) value[q] = silu(value[q]) * up[q];
+                    }
+                    bf16x8 o;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) o[q] = (__bf16)value[q];
+                    v[h] = __builtin_bit_cast(words4, o);
+                }
+                if constexpr (kRun == 16) {   // two neighbouring rows' 32 bytes of a lane, so that a store meets whole pieces of a row
+                    exchange<0xb1>(lane & 1, v[0], v[1]);
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int row = (b & ~1) + k, column = a + (lane & 1) * 8;
+                        __builtin_amdgcn_raw_buffer_store_b128(v[k], out.to, (int)(column < a_left && row < b_left ? row * out.ld + column * 2 : kNowhere), 0, 0);
+                    }
+                } else {
+                    __builtin_amdgcn_raw_buffer_store_b128(v[0], out.to, (int)(a < a_left && b < b_left ? b * out.ld + a * 2 : kNowhere), 0, 0);
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto store_sixteens = [&](const auto &acc, int a0, int a_left, int b_left, int64_t row0) __attribute__((always_inline)) {
         constexpr int kSize = STORE == kStoreF32 ? 4 : 2;
         const int rows = b_left < BB ? b_left : BB;
         Target out, pre;
@@ -804,13 +889,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         }
         __builtin_amdgcn_sched_barrier(0);
     };
+    auto store = [&](int a0, int a_left, int b_left, int64_t row0) __attribute__((always_inline)) {
+        if constexpr (EIGHT) store_runs(acc, a0, a_left, b_left, row0);
+        else store_sixteens(acc, a0, a_left, b_left, row0);
+    };
     auto clear = [&] {
+        constexpr int kMore = EIGHT ? 2 : 1;
 #pragma unroll
-        for (int f = 0; f < FA; ++f)
+        for (int f = 0; f < kMore * FA; ++f)
 #pragma unroll
-            for (int j = 0; j < FB; ++j)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) acc[f][j][q] = 0.0f;
+            for (int j = 0; j < kMore * FB; ++j) acc[f][j] = {};
     };
     // stores of one tile and wave; the activation's gradient waits for loads in between and counts as none
     constexpr int kStores = kGatedGrad ? 0 : FB * kOutA * (STORE == kStoreF32 ? 4 : 2);
@@ -850,16 +938,18 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     s.template wait<State::kSlots - 1, kStores - (KEPT ? 2 : 0)>();
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    typename std::conditional<EIGHT, Eights<FB>, Slice<FA, FB>[2]>::type x;
+    typename std::conditional<EIGHT, Eights<2 * FB>, Slice<FA, FB>[2]>::type x;
     if constexpr (EIGHT) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            x.a[h] = half_stage<typename State::A>(slot0, s.a_lane, 0, h);
+        for (int f = 0; f < kAhead; ++f) x.a[f] = State::A::fragment8(slot0, s.a_lane, f);
 #pragma unroll
-            for (int j = 0; j < FB; ++j) x.b[j][h] = half_stage<typename State::B>(slot0 + State::A::kBytes, s.b_lane, j, h);
+        for (int j = 0; j < 2 * FB; ++j) {
+            x.b[j] = State::B::fragment8(slot0 + State::A::kBytes, s.b_lane, j);
+            read_scales<kGated>(s, slot0, j, x);
+            x.scale[j] = 0.0f;
         }
 #pragma unroll
-        for (int j = 0; j < FB; ++j) read_scales<kGated>(s, slot0, j, x);
+        for (int m = 0; m < kParts8; ++m) x.part[m] = {};
     } else {
 #pragma unroll
         for (int m = 0; m < FA * FB; ++m) read_after(s, slot0, s.a_lane, s.b_lane, 0, m, x[0]);
@@ -899,6 +989,14 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         }
         if (active) turn(yes, none, 0);
         else turn(no, none, 0);
+        if constexpr (EIGHT) {   // what the stages leave for later
+#pragma unroll
+            for (int m = 4 * FA * FB - kLate; m < 4 * FA * FB; ++m) {
+                if (active) add_part(x, m, acc);
+                x.part[m % kParts8] = {};
+                x.scale[m % (2 * FB)] = 0.0f;
+            }
+        }
         store(now_a0, now_a, now_b, now_row);
         if (!more) break;
         clear();
