@@ -201,8 +201,10 @@ __device__ __forceinline__ void wide_eight(uint32_t first, uint32_t second, floa
 // half the length keep more in flight (8 experts of 16384 rows, 4096 x 2560, TF/s: two of 64 / four of 32: forward 1225 / 1190, input
 // gradient 1103 / 1150, weight gradient 1206 / 1345).
 //
-// EIGHT: operands of e4m3, both along c, in the same LDS rows of 128 bytes, so that a stage is one block of scales.  They come with it: the first waves load
-// those of 64 rows each (as many as the tile has rows), the next one those of the weights, the others nothing (every wave counts the same loads).
+// EIGHT: operands of e4m3, both along c, in the same LDS rows of 128 bytes, so that a stage is one block of scales.  Those of rows lie far apart, a line of the L2 each, and
+// come four stages at once, into one of two places of their own in turn: the first waves load those of 64 rows each (as many as the tile has rows), the next one the weights',
+// the others nothing (every wave counts the same loads).  One stage at a time they cost half as many requests to the L2 as the operands: 131072 rows, gated 1510
+// us / 1410.
 //
 // KEPT: operand A is rows of e4m3 with their scales, across c.  They pass registers on their way to LDS, where they become bf16 (with scales that are powers of two without
 // a rounding): a thread holds 16 outputs of one row of two stages.
@@ -214,7 +216,7 @@ struct TileState {
     typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
     typedef Operand<BMODE, BB, kStageC, false, kSpared ? kEvenPlaces : kOwnPlaces> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes, kLoads = A::kLoads;
-    static constexpr int kScaleLoads = EIGHT ? 1 : 0, kSlotBytes = kStageBytes + (EIGHT ? kTileThreads * 4 : 0), kWeightScales = kStageBytes + BB * 4;
+    static constexpr int kScaleLoads = EIGHT ? 1 : 0, kScaleStages = 4, kScaleBytes = (BB + kWave) * kScaleStages * 4;
     static_assert(A::kLoads >= B::kLoads, "the wider operand");
     A a;
     B b;
@@ -225,6 +227,8 @@ struct TileState {
     int32_t scale_bytes, scale_step;
     uint32_t scale_at;     // KEPT: this thread's byte offset
     uint32_t row_scale_lane, weight_scale_wave;   // where a lane and a wave read them
+    char *groups;                                 // LDS of the scales, and behind both places room where nobody reads
+    int32_t side, asked, next;                    // which of the two places is in use; where the scales of the stage asked for last lie, and of the next one to come
 
     // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
     __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots - 1) / kSlots : 1; }
@@ -247,10 +251,16 @@ struct TileState {
         const int at = stage_of(s);
         if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place.a);
         if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, place.b);
-        if (EIGHT && i == 0) {
-            const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
-            to_lds_single(view(scales, scale_bytes), slot + kStageBytes + wave * (kWave * 4), at < stages ? place : kNowhere, at * 4);
-        }
+    }
+    // The scales of a stage that is asked for; where they will lie is known by then (asked, -1 past the last stage)
+    __device__ __forceinline__ void load_scales(int s)
+    {
+        const int at = stage_of(s), in = at < stages, fresh = in & (s == 0 | at % kScaleStages == 0);   // numbers: a branch would part the stage's instructions
+        side ^= fresh;
+        asked = in ? side * kScaleBytes + at % kScaleStages * 4 : -1;
+        const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
+        to_lds(view(scales, scale_bytes), groups + ((fresh & (wave <= BB / kWave)) ? side * kScaleBytes + wave * (kWave * 16) : 2 * kScaleBytes), fresh ? place : kNowhere,
+               at / kScaleStages * (kScaleStages * 4));
     }
     struct Held {
         words4 q;
@@ -344,24 +354,35 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
 // Stages of e4m3 operands: a matrix instruction takes a whole stage of 16 x 16 outputs, and its result, scaled, is added to the pair's sums two instructions
 // later.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
 // fragments ahead.)
-constexpr int kRing = 4, kAhead = 2;   // fragments of a in registers, and how far ahead of their use they are read
+constexpr int kRing = 2, kAhead = 1;   // fragments of a in registers, and how far ahead of their use they are read
 constexpr int kLate = 2, kParts8 = 4;  // instructions between a product and its use, products in registers
 
 template <int FB>
+struct Scales {
+    float rows[FB], weight[2];  // of a stage: of the lane's rows of b, of the wave's rows of a (gated: gate and up)
+};
+template <int FB>
 struct Eights {
     words8 a[kRing], b[FB];
-    float rows[FB], weight[2];  // scales of the stage: of the lane's rows of b, of the wave's rows of a (gated: gate and up)
+    Scales<FB> of;
     float scale[FB];            // both together, as they are in use
     f32x4 part[kParts8];
 };
 
+// of the stage whose scales lie at `at`; read before others are asked for, whose arrival the compiler would wait for
 template <bool GATED, int FB, typename S>
-__device__ __forceinline__ void read_scales(const S &t, const char *slot, int j, Eights<FB> &x)
+__device__ __forceinline__ void read_scales(const S &t, int at, Scales<FB> &x)
 {
-    x.rows[j] = *(const float *)(slot + S::kStageBytes + t.row_scale_lane + j * 64);
-    if (j > 0) return;
-    x.weight[0] = *(const float *)(slot + S::kWeightScales + t.weight_scale_wave);
-    if (GATED) x.weight[1] = *(const float *)(slot + S::kWeightScales + 4);
+#pragma unroll
+    for (int j = 0; j < FB; ++j) {
+        const float v = *(const float *)(t.groups + t.row_scale_lane + max(at, 0) + j * (16 * S::kScaleStages * 4));
+        x.rows[j] = at < 0 ? 0.0f : v;
+    }
+#pragma unroll
+    for (int g = 0; g < (GATED ? 2 : 1); ++g) {
+        const float v = *(const float *)(t.groups + t.weight_scale_wave + max(at, 0) + g * (S::kScaleStages * 4));
+        x.weight[g] = at < 0 ? 0.0f : v;   // what lies there may be NaN
+    }
 }
 
 template <int FA, int FB>
@@ -372,12 +393,13 @@ __device__ __forceinline__ void add_part(Eights<FB> &x, int m, f32x4 (&acc)[FA][
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
     static_assert(FA % kRing == 0 && FA * FB % kParts8 == 0 && FB >= kLate, "registers take turns");
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
     asm volatile("" : "+v"(a_at), "+v"(b_at));
     typename S::Places place = {};
+    Scales<FB> next;
 #pragma unroll
     for (int f = 0; f < FA; ++f) {
         const bool past = f + kAhead >= FA;   // reads are of the next stage
@@ -385,6 +407,7 @@ __device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *n
             t.template wait<S::kSlots - 2, STORES>();
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
+            read_scales<GATED>(t, t.next, next);
             place = t.places();
         }
         if (!ACTIVE && !past) continue;
@@ -403,24 +426,24 @@ __device__ __forceinline__ void tile_stage8(const S &t, char *cur, const char *n
                 constexpr int kEach = (S::kLoads + kAhead * FB - 1) / (kAhead * FB);
 #pragma unroll
                 for (int i = step * kEach; i < (step + 1) * kEach && i < S::kLoads; ++i) t.load(ask, i, cur, place);
+                if (step == kAhead * FB - 1) t.load_scales(ask);
             }
             if (ACTIVE) {
                 const int of = (m + FA * FB - kLate) % (FA * FB);
                 // the pair's scale changes with the stage and from gate to up rows
-                if (of < FB) x.scale[of] = x.weight[0] * x.rows[of];
-                if (GATED && of / FB == FA / 2) x.scale[of % FB] = x.weight[1] * x.rows[of % FB];
+                if (of < FB) x.scale[of] = x.of.weight[0] * x.of.rows[of];
+                if (GATED && of / FB == FA / 2) x.scale[of % FB] = x.of.weight[1] * x.of.rows[of % FB];
                 add_part(x, of, acc);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (f == FA - 1 && j == FB - 1)
-#pragma unroll
-                for (int i = 0; i < FB; ++i) read_scales<GATED>(t, nxt, i, x);
         }
     }
+    x.of = next;
+    t.next = t.asked;
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_turn8(const S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_turn8(S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
     static_assert(S::kSlots == 2, "operands along c");
     tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, ask, x, acc);
@@ -571,7 +594,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
-    __shared__ __align__(1024) char slot0[State::kSlotBytes], slot1[State::kSlotBytes], slot2[kMore], slot3[kMore];
+    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[kMore], slot3[kMore];
     __shared__ int offsets[FUSCO_MAX_E + 1], prefix[kByRows ? FUSCO_MAX_E + 1 : 1];
     __shared__ int part[kTileThreads / kWave];
 
@@ -599,9 +622,12 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     s.a_lane = EIGHT ? State::A::lane_at8(lane, wa * FA * 32) : State::A::lane_at(lane, wa * FA * 32);
     s.b_lane = EIGHT ? State::B::lane_at8(lane, wb * FB * 32) : State::B::lane_at(lane, wb * FB * 32);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
+    __shared__ __align__(16) char groups[EIGHT ? 2 * State::kScaleBytes + kWave * 16 : 16];
     if constexpr (EIGHT) {
-        s.row_scale_lane = (wb * FB * 32 + (lane & 15)) * 4;
-        s.weight_scale_wave = kGated ? 0 : wa * FA * 32 / 128 * 4;
+        s.groups = groups;
+        s.side = 0;
+        s.row_scale_lane = (wb * FB * 32 + (lane & 15)) * (State::kScaleStages * 4);
+        s.weight_scale_wave = (BB + (kGated ? 0 : wa * FA * 32 / 128)) * (State::kScaleStages * 4);
         asm volatile("" : "+v"(s.row_scale_lane), "+v"(s.weight_scale_wave));
     }
 
@@ -917,8 +943,13 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     }
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(0, i, slot0);
+    if constexpr (EIGHT) {
+        s.load_scales(0);
+        s.next = s.asked;
+    }
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(1, i, slot1);
+    if constexpr (EIGHT) s.load_scales(1);
     if constexpr (State::kSlots == 4) {
         // kept rows are asked for before the other operand of their stage, as in the loop: the waits count on that order
         __builtin_amdgcn_sched_barrier(0);
@@ -945,9 +976,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 #pragma unroll
         for (int j = 0; j < 2 * FB; ++j) {
             x.b[j] = State::B::fragment8(slot0 + State::A::kBytes, s.b_lane, j);
-            read_scales<kGated>(s, slot0, j, x);
             x.scale[j] = 0.0f;
         }
+        read_scales<kGated>(s, s.next, x.of);
+        s.next = s.asked;
 #pragma unroll
         for (int m = 0; m < kParts8; ++m) x.part[m] = {};
     } else {

@@ -70,3 +70,22 @@ def test_an_experts_values_stay_its_own(N, rows):
     L = f.Layout(N, 2, 4, 1)
     assert f.fusco_probe_experts_tile_rows(L, f.PRODUCT_LINEAR, 136, 104) == rows
     fp8.test_an_experts_values_stay_its_own(N)
+
+
+@pytest.mark.parametrize("C", [128, 384, 640])     # an odd number of stages, so that one of a tile's is filled up
+@pytest.mark.parametrize("N,E", [(10000, 16), (20000, 8)])
+def test_scales_of_a_tile_stay_its_own(N, E, C):
+    """Every other expert's weight scales are NaN: workgroups go from such tiles to others and back."""
+    f = fusco()
+    L, gen, bounds = make(N, 2, E, 14, "normal")
+    M = 520
+    assert f.fusco_probe_experts_tile_rows(L, f.PRODUCT_LINEAR, M, C) == 256
+    x, xs = fp8.eight(gen, L.P, C, scales=(L.P, fp8.blocks(C)), std=1.0)
+    w, ws = fp8.eight(gen, L.E, M, C, scales=(L.E, fp8.blocks(M), fp8.blocks(C)), std=1.0)
+    ws[::2] = float("nan")
+    y = torch.empty((L.P, M), dtype=torch.bfloat16, device="cuda")
+    for _ in range(3):
+        f.fusco_experts_linear_fp8(L, x, xs, w, ws, y)
+        for e in range(L.E):
+            part = y[bounds[e]:bounds[e + 1]]
+            assert bool(part.isnan().all() if e % 2 == 0 else part.isfinite().all()), e
