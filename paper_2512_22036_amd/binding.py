@@ -223,6 +223,7 @@ def _bind_fastcall(lib):
                      for name in ("fusco_plan", "fusco_dispatch", "fusco_plan_dispatch", "fusco_combine", "fusco_combine_two_hop")))
     _fastcall.bind_block(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
                            for name in ("fusco_route", "fusco_norm_before", "fusco_norm_after", "fusco_experts_gated", "fusco_experts_linear")))
+    _fastcall.bind_fp8(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in ("fusco_to_fp8", "fusco_from_fp8", "fusco_moe_few")))
     return _fastcall
 
 
@@ -719,6 +720,8 @@ def _row_scale(t: torch.Tensor, name: str, rows: int, columns: int) -> int:
 def _scaled(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> _CFp8:
     if not x.is_cuda or x.dim() not in (2, 3) or not x.is_contiguous():
         raise FuscoError("x must be a contiguous device tensor of rows or of matrices")
+    if max(x.shape) >= 2 ** 31 or scale.numel() and max(scale.shape) >= 2 ** 31:
+        raise FuscoError("x and scale must have fewer than 2^31 rows and columns")
     _fp8(q, "q", x.shape)
     if x.dim() == 2:
         return _CFp8(x.shape[0], x.shape[1], _dtype_code(x, "x"), 0, _row_scale(scale, "scale", *x.shape))
@@ -731,12 +734,20 @@ def fusco_to_fp8(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, stream=N
     """x, bfloat16 or float32, as q (float8_e4m3fn, of x's shape) with scales that are powers of two: per 128 columns of each
     row for x [R, C] (scale float32 [R, S], S at least ceil(C / 128)), per 128 x 128 for matrices [E, M, C] (scale
     [E, ceil(M / 128), ceil(C / 128)])."""
+    if stream is None and _fast is not None:
+        rc = _fast.to_fp8(x, q, scale)
+        if rc is not None:
+            return _check(rc, "fusco_to_fp8")
     f = _scaled(x, q, scale)
     _check(load_library().fusco_to_fp8(ctypes.byref(f), x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream)), "fusco_to_fp8")
 
 
 def fusco_from_fp8(q: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, stream=None) -> None:
     """x = q * scale, tensors as in fusco_to_fp8, scales any numbers."""
+    if stream is None and _fast is not None:
+        rc = _fast.from_fp8(q, scale, x)
+        if rc is not None:
+            return _check(rc, "fusco_from_fp8")
     f = _scaled(x, q, scale)
     _check(load_library().fusco_from_fp8(ctypes.byref(f), q.data_ptr(), scale.data_ptr(), x.data_ptr(), _stream(stream)), "fusco_from_fp8")
 
@@ -789,6 +800,10 @@ def fusco_moe_few(x: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, w_in
     fusco_route writes them, out [N, H] bfloat16 or float32.  Weights w_in [E, 2 I, H] and w_out [E, H, I] are bfloat16, or
     float8_e4m3fn with the scales that fusco_experts_gated_fp8 and fusco_experts_linear_fp8 take.  scratch:
     fusco_moe_few_scratch_bytes(N, k, I) bytes, made here on the call's stream if not given."""
+    if stream is None and scratch is not None and _fast is not None:
+        rc = _fast.moe_few(x, topk_idx, w, w_in, w_out, out, w_in_scale, w_out_scale, scratch)
+        if rc is not None:
+            return _check(rc, "fusco_moe_few")
     if not x.is_cuda or x.dim() != 2 or w_in.dim() != 3 or w_in.shape[1] % 2:
         raise FuscoError("x must be a 2-D device tensor, w_in have three dimensions and an even number of rows per expert")
     (N, H), E, I = x.shape, w_in.shape[0], w_in.shape[1] // 2
@@ -806,6 +821,8 @@ def fusco_moe_few(x: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, w_in
         _fp32(w_out_scale, "w_out_scale", (E, _blocks(H), _blocks(I)))
     if not out.is_cuda or not out.is_contiguous() or tuple(out.shape) != (N, H):
         raise FuscoError("out must be a contiguous device tensor of shape [%d, %d]" % (N, H))
+    if max(N, E, topk_idx.shape[1], H, I) >= 2 ** 31:
+        raise FuscoError("sizes must be below 2^31")
     f = _CFew(N, E, topk_idx.shape[1], H, I, BF16 if w_in_scale is None else E4M3, _dtype_code(out, "out"))
     scratch = _scratch(fusco_moe_few_scratch_bytes(N, f.k, I), scratch, x.device, stream)
     _check(load_library().fusco_moe_few(ctypes.byref(f), x.data_ptr(), topk_idx.data_ptr(), w.data_ptr(), w_in.data_ptr(), _ptr(w_in_scale), w_out.data_ptr(),

@@ -25,6 +25,9 @@ decltype(&fusco_norm_before) p_norm_before = nullptr;
 decltype(&fusco_norm_after) p_norm_after = nullptr;
 decltype(&fusco_experts_gated) p_experts_gated = nullptr;
 decltype(&fusco_experts_linear) p_experts_linear = nullptr;
+decltype(&fusco_to_fp8) p_to_fp8 = nullptr;
+decltype(&fusco_from_fp8) p_from_fp8 = nullptr;
+decltype(&fusco_moe_few) p_moe_few = nullptr;
 
 PyObject *s_c, *s_scratch;   // attribute names of Layout
 
@@ -399,6 +402,108 @@ PyObject *bind_block(PyObject *, PyObject *args)
     Py_RETURN_NONE;
 }
 
+// ---- e4m3 and the layer for a few tokens
+
+int64_t blocks_of(int64_t n) { return (n + 127) / 128; }
+
+bool cube_of(const at::Tensor &t, at::ScalarType type, int64_t a, int64_t b, int64_t c)
+{
+    return t.is_cuda() && t.scalar_type() == type && t.is_contiguous() && t.dim() == 3 && t.size(0) == a && t.size(1) == b && t.size(2) == c;
+}
+
+// binding.py's _scaled
+bool scaled(const at::Tensor &x, const at::Tensor &q, const at::Tensor &scale, fusco_fp8 &f)
+{
+    if (!x.is_cuda() || !x.is_contiguous() || (x.dim() != 2 && x.dim() != 3)) return false;
+    for (int i = 0; i < x.dim(); ++i)
+        if (x.size(i) > INT32_MAX) return false;
+    f.dtype = dtype_code(x);
+    if (f.dtype < 0) return false;
+    if (x.dim() == 2) {
+        f.rows = x.size(0);
+        f.columns = (int32_t)x.size(1);
+        f.matrix_rows = 0;
+        if (rows(scale, f.rows) < 0 || scale.scalar_type() != at::kFloat || scale.size(0) != f.rows || scale.size(1) < blocks_of(f.columns) || scale.size(1) > INT32_MAX) return false;
+        f.scale_stride = (int32_t)scale.size(1);
+        return matrix_of(q, at::kFloat8_e4m3fn, f.rows, f.columns);
+    }
+    const int64_t E = x.size(0), M = x.size(1), C = x.size(2);
+    f.rows = E * M;
+    f.columns = (int32_t)C;
+    f.matrix_rows = (int32_t)M;
+    f.scale_stride = (int32_t)blocks_of(C);
+    return cube_of(q, at::kFloat8_e4m3fn, E, M, C) && cube_of(scale, at::kFloat, E, blocks_of(M), blocks_of(C));
+}
+
+// to_fp8(x, q, scale)
+PyObject *to_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 3 || !p_to_fp8) Py_RETURN_NONE;
+    return guarded([&]() -> int {
+        const at::Tensor *x = tensor(args[0]), *q = tensor(args[1]), *scale = tensor(args[2]);
+        fusco_fp8 f;
+        if (!x || !q || !scale || !scaled(*x, *q, *scale, f)) return kElsewhere;
+        void *xp = x->data_ptr(), *qp = q->data_ptr(), *sp = scale->data_ptr(), *stream = current_stream();
+        return released([&] { return p_to_fp8(&f, xp, qp, (float *)sp, stream); });
+    });
+}
+
+// from_fp8(q, scale, x)
+PyObject *from_fp8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 3 || !p_from_fp8) Py_RETURN_NONE;
+    return guarded([&]() -> int {
+        const at::Tensor *q = tensor(args[0]), *scale = tensor(args[1]), *x = tensor(args[2]);
+        fusco_fp8 f;
+        if (!x || !q || !scale || !scaled(*x, *q, *scale, f)) return kElsewhere;
+        void *qp = q->data_ptr(), *sp = scale->data_ptr(), *xp = x->data_ptr(), *stream = current_stream();
+        return released([&] { return p_from_fp8(&f, qp, (const float *)sp, xp, stream); });
+    });
+}
+
+// moe_few(x, topk_idx, w, w_in, w_out, out, w_in_scale, w_out_scale, scratch): with the caller's scratch
+PyObject *moe_few(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 9 || !p_moe_few) Py_RETURN_NONE;
+    return guarded([&]() -> int {
+        const at::Tensor *t[9];
+        for (int i = 0; i < 9; ++i) {
+            t[i] = args[i] == Py_None ? nullptr : tensor(args[i]);
+            if (!t[i] && (args[i] != Py_None || (i != 6 && i != 7))) return kElsewhere;
+        }
+        const at::Tensor &x = *t[0], &idx = *t[1], &w_in = *t[3], &out = *t[5], &scratch = *t[8];
+        const bool eight = t[6];
+        if (eight != (t[7] != nullptr) || !x.is_cuda() || x.dim() != 2 || w_in.dim() != 3 || w_in.size(1) % 2 != 0 || idx.dim() != 2) return kElsewhere;
+        const int64_t N = x.size(0), H = x.size(1), E = w_in.size(0), I = w_in.size(1) / 2, k = idx.size(1);
+        if (N > FUSCO_MAX_FEW_TOKENS || H > INT32_MAX || E > FUSCO_MAX_E || I > INT32_MAX || k > FUSCO_MAX_K) return kElsewhere;
+        const at::ScalarType type = eight ? at::kFloat8_e4m3fn : at::kBFloat16;
+        if (!matrix_of(x, at::kBFloat16, N, H) || !matrix_of(idx, at::kInt, N, k) || !matrix_of(*t[2], at::kFloat, N, k) || !cube_of(w_in, type, E, 2 * I, H) ||
+            !cube_of(*t[4], type, E, H, I) || !matrix_of(out, out.scalar_type(), N, H) || !scratch.is_cuda() || !scratch.is_contiguous())
+            return kElsewhere;
+        if (eight && (!cube_of(*t[6], at::kFloat, E, 2 * blocks_of(I), blocks_of(H)) || !cube_of(*t[7], at::kFloat, E, blocks_of(H), blocks_of(I)))) return kElsewhere;
+        const fusco_few f = {(int32_t)N, (int32_t)E, (int32_t)k, (int32_t)H, (int32_t)I, eight ? FUSCO_E4M3 : FUSCO_BF16, dtype_code(out)};
+        if (f.out_dtype < 0) return kElsewhere;
+        void *p[9];
+        for (int i = 0; i < 9; ++i) p[i] = t[i] ? t[i]->data_ptr() : nullptr;
+        const size_t bytes = (size_t)scratch.numel() * scratch.element_size();
+        void *stream = current_stream();
+        return released([&] {
+            return p_moe_few(&f, p[0], (const int32_t *)p[1], (const float *)p[2], p[3], (const float *)p[6], p[4], (const float *)p[7], p[5], p[8], bytes, stream);
+        });
+    });
+}
+
+// bind_fp8(to_fp8, from_fp8, moe_few)
+PyObject *bind_fp8(PyObject *, PyObject *args)
+{
+    unsigned long long a[3];
+    if (!PyArg_ParseTuple(args, "KKK", a, a + 1, a + 2)) return nullptr;
+    p_to_fp8 = (decltype(p_to_fp8))(uintptr_t)a[0];
+    p_from_fp8 = (decltype(p_from_fp8))(uintptr_t)a[1];
+    p_moe_few = (decltype(p_moe_few))(uintptr_t)a[2];
+    Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"bind", (PyCFunction)bind, METH_VARARGS, nullptr},
     {"plan", (PyCFunction)(void (*)())plan, METH_FASTCALL, nullptr},
@@ -412,6 +517,10 @@ PyMethodDef methods[] = {
     {"norm_after", (PyCFunction)(void (*)())norm_after, METH_FASTCALL, nullptr},
     {"experts_gated", (PyCFunction)(void (*)())experts_gated, METH_FASTCALL, nullptr},
     {"experts_linear", (PyCFunction)(void (*)())experts_linear, METH_FASTCALL, nullptr},
+    {"bind_fp8", (PyCFunction)bind_fp8, METH_VARARGS, nullptr},
+    {"to_fp8", (PyCFunction)(void (*)())to_fp8, METH_FASTCALL, nullptr},
+    {"from_fp8", (PyCFunction)(void (*)())from_fp8, METH_FASTCALL, nullptr},
+    {"moe_few", (PyCFunction)(void (*)())moe_few, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
