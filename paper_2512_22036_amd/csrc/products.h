@@ -250,7 +250,12 @@ struct TileState {
     {
         const int at = stage_of(s);
         if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place.a);
-        if (i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, place.b);
+        if (!EIGHT && i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, place.b);
+    }
+    __device__ __forceinline__ void load_b(int s, char *slot) const
+    {
+#pragma unroll
+        for (int i = 0; i < B::kLoads; ++i) b.load(stage_of(s), i, slot, wave, b.place());
     }
     // The scales of a stage that is asked for; where they will lie is known by then (asked, -1 past the last stage)
     __device__ __forceinline__ void load_scales(int s)
@@ -290,10 +295,10 @@ struct TileState {
         }
     }
     // waits until at most the loads of `behind` stages and `more` stores are on their way and nothing is being read from LDS
-    template <int behind, int more = 0>
+    template <int behind, int more = 0, int early = 0>
     __device__ __forceinline__ void wait() const
     {
-        constexpr int kAll = (A::kLoads + B::kLoads + kScaleLoads) * behind + more, kSome = (A::kLoads + kScaleLoads) * behind + more;
+        constexpr int kAll = (A::kLoads + B::kLoads + kScaleLoads) * behind + more + early, kSome = (A::kLoads + kScaleLoads) * behind + more;
         static_assert(kAll < 64, "what the hardware counts");
         if (B::kLoadWaves == kTileThreads / kWave || wave < B::kLoadWaves) __builtin_amdgcn_s_waitcnt((kAll & 15) | (kAll >> 4) << 14 | 0x70);
         else __builtin_amdgcn_s_waitcnt((kSome & 15) | (kSome >> 4) << 14 | 0x70);
@@ -353,7 +358,8 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
 
 // Stages of e4m3 operands: a matrix instruction takes a whole stage of 16 x 16 outputs, and its result, scaled, is added to the pair's sums two instructions
 // later.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
-// fragments ahead.)
+// fragments ahead.)  In the middle of a stage all waves hold their fragments of b, and b's slot is asked for again: its loads then have one and a half stages, those of a one (131072
+// rows, linear 898 -> 799 us, gated 1408 -> 1390; the loads one by one over four instructions 816 and 1430; half of a's loads with them, in slots apart, 827 and 1510).
 constexpr int kRing = 2, kAhead = 1;   // fragments of a in registers, and how far ahead of their use they are read
 constexpr int kLate = 2, kParts8 = 4;  // instructions between a product and its use, products in registers
 
@@ -393,7 +399,7 @@ __device__ __forceinline__ void add_part(Eights<FB> &x, int m, f32x4 (&acc)[FA][
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, char *cur_b, const char *nxt_b, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
     static_assert(FA % kRing == 0 && FA * FB % kParts8 == 0 && FB >= kLate, "registers take turns");
     uint32_t a_at = t.a_lane, b_at = t.b_lane;
@@ -403,8 +409,14 @@ __device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, in
 #pragma unroll
     for (int f = 0; f < FA; ++f) {
         const bool past = f + kAhead >= FA;   // reads are of the next stage
+        if (f == FA / 2) {   // all waves have b's fragments in registers
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            t.load_b(ask, cur_b);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         if (f + kAhead == FA) {
-            t.template wait<S::kSlots - 2, STORES>();
+            t.template wait<S::kSlots - 2, STORES, S::B::kLoads>();
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
             read_scales<GATED>(t, t.next, next);
@@ -420,7 +432,7 @@ __device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, in
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (j == 0) x.a[(f + kAhead) % kRing] = S::A::fragment8(past ? nxt : cur, a_at, (f + kAhead) % FA);
-            if (f == FA - 1) x.b[j] = S::B::fragment8(nxt + S::A::kBytes, b_at, j);
+            if (f == FA - 1) x.b[j] = S::B::fragment8(nxt_b, b_at, j);
             if (past) {
                 const int step = (f + kAhead - FA) * FB + j;
                 constexpr int kEach = (S::kLoads + kAhead * FB - 1) / (kAhead * FB);
@@ -443,11 +455,11 @@ __device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, in
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_turn8(S &t, char *slot0, char *slot1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_turn8(S &t, char *slot0, char *slot1, char *b0, char *b1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
     static_assert(S::kSlots == 2, "operands along c");
-    tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, ask, x, acc);
-    tile_stage8<ACTIVE, 0, GATED>(t, slot1, slot0, ask + 1, x, acc);
+    tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, b0, b1, ask, x, acc);
+    tile_stage8<ACTIVE, 0, GATED>(t, slot1, slot0, b1, b0, ask + 1, x, acc);
 }
 
 // One turn through the slots, while stage ask, ask + 1, ... of this tile or the next are asked for.  STORES: stores that were issued after
@@ -594,7 +606,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
-    __shared__ __align__(1024) char slot0[State::kStageBytes], slot1[State::kStageBytes], slot2[kMore], slot3[kMore];
+    constexpr int kSlotBytes = EIGHT ? State::A::kBytes : State::kStageBytes, kRowsB = EIGHT ? State::B::kBytes : 16;   // e4m3: operand B has slots of its own
+    __shared__ __align__(1024) char slot0[kSlotBytes], slot1[kSlotBytes], slot2[kMore], slot3[kMore], rows0[kRowsB], rows1[kRowsB];
     __shared__ int offsets[FUSCO_MAX_E + 1], prefix[kByRows ? FUSCO_MAX_E + 1 : 1];
     __shared__ int part[kTileThreads / kWave];
 
@@ -944,12 +957,16 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(0, i, slot0);
     if constexpr (EIGHT) {
+        s.load_b(0, rows0);
         s.load_scales(0);
         s.next = s.asked;
     }
 #pragma unroll
     for (int i = 0; i < State::kLoads; ++i) s.load(1, i, slot1);
-    if constexpr (EIGHT) s.load_scales(1);
+    if constexpr (EIGHT) {
+        s.load_b(1, rows1);
+        s.load_scales(1);
+    }
     if constexpr (State::kSlots == 4) {
         // kept rows are asked for before the other operand of their stage, as in the loop: the waits count on that order
         __builtin_amdgcn_sched_barrier(0);
@@ -975,7 +992,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         for (int f = 0; f < kAhead; ++f) x.a[f] = State::A::fragment8(slot0, s.a_lane, f);
 #pragma unroll
         for (int j = 0; j < 2 * FB; ++j) {
-            x.b[j] = State::B::fragment8(slot0 + State::A::kBytes, s.b_lane, j);
+            x.b[j] = State::B::fragment8(rows0, s.b_lane, j);
             x.scale[j] = 0.0f;
         }
         read_scales<kGated>(s, s.next, x.of);
@@ -989,7 +1006,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     auto turn = [&](auto multiplied, auto stores, int ask) {
         constexpr bool kMultiplied = decltype(multiplied)::value;
         constexpr int kBehind = decltype(stores)::value;
-        if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, ask, x, acc);
+        if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, rows0, rows1, ask, x, acc);
         else if constexpr (KEPT) tile_turn_kept<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc, held);
         else tile_turn<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc);
     };
