@@ -10,6 +10,7 @@
 #define FUSCO_CSRC_FEW_H
 
 #include "products.h"
+#include <float.h>
 
 namespace {
 
@@ -32,6 +33,7 @@ struct FewArgs {
 };
 
 constexpr int kParts = 3;
+constexpr float kMaxBf16 = 0x1.fep127f;
 constexpr int kFive = 5;       // pairs: kParts columns each of the sixteen of a matrix instruction
 constexpr int kManyFives = 3;
 static_assert(FUSCO_MAX_E <= 1 << 10 && kFive * kManyFives < 1 << 4 && FUSCO_MAX_FEW_TOKENS * FUSCO_MAX_K <= 1 << 17, "a group in 31 bits");
@@ -144,7 +146,7 @@ template <bool EIGHT, int F, int WAVES, int G, int DEPTH, int SIMD>
 __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p)
 {
     typedef FewPiece<EIGHT, 2> Piece;
-    constexpr int kUnits = 8 * F, kCols = 16 * G;
+    constexpr int kUnits = 8 * F, kCols = 16 * G, kFragments = F == 1 ? 1 : F / 2;   // of gate rows
     static_assert(F == 1 || F % 2 == 0, "gate and up rows");
     typedef f32x4 Sums[WAVES][F][G][kWave];
     __shared__ int16_t pairs[kFewTokens * FUSCO_MAX_K];
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
     uint32_t w_at[F];
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-        const int unit = F == 1 ? lane & 7 : f % (F / 2) * 16 + (lane & 15);
+        const int unit = F == 1 ? lane & 7 : f % kFragments * 16 + (lane & 15);
         const bool up = F == 1 ? (lane & 8) != 0 : f >= F / 2;
         w_at[f] = a0 + unit < p.I ? (uint32_t)((unit + (up ? p.I : 0)) * ld) : kNowhere;
     }
@@ -263,10 +265,9 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
 #pragma unroll
             for (int g = 0; g < G; ++g) sums[wave][f][g][lane] = acc[f][g];
         __syncthreads();
-        constexpr int kOut = F == 1 ? 1 : F / 2;
-        for (int fg = wave; fg < kOut * G; fg += WAVES) {
+        for (int fg = wave; fg < kFragments * G; fg += WAVES) {
             const int f = fg / G, g = fg % G, col = first + g * 16 + (lane & 15), a = a0 + f * 16 + (lane >> 4) * 4;
-            const int up_f = F == 1 ? 0 : f + kOut, up_lane = F == 1 ? lane ^ 32 : lane;
+            const int up_f = F == 1 ? 0 : f + kFragments, up_lane = F == 1 ? lane ^ 32 : lane;
             f32x4 gate = sums[0][f][g][lane], up = sums[0][up_f][g][up_lane];
 #pragma unroll
             for (int v = 1; v < WAVES; ++v) {
@@ -283,8 +284,10 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
                 bf16x4 part;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    part[q] = (__bf16)rest[q];
-                    rest[q] -= (float)part[q];
+                    // the largest number of bf16 for what would round to infinity; of an infinity, nothing is left
+                    const bool finite = fabsf(rest[q]) <= FLT_MAX;
+                    part[q] = (__bf16)(finite ? __builtin_amdgcn_fmed3f(rest[q], -kMaxBf16, kMaxBf16) : rest[q]);
+                    rest[q] = fabsf(rest[q]) == INFINITY ? 0.0f : rest[q] - (float)part[q];
                 }
                 *(bf16x4 *)(p.h + ((int64_t)i * P * p.I + at) * 2) = part;
             }

@@ -132,6 +132,34 @@ def test_an_experts_values_stay_its_own(eights, N):
     assert bool(out[~sick].isfinite().all()) and not bool(out[sick].isfinite().any())
 
 
+@pytest.mark.parametrize("N,k", [(2, 1), (40, 4)])
+def test_largest_activations(N, k):
+    """silu(g) u at the ends of fp32: infinities stay what they are, and what is finite in fp32 but would round to an infinity of bf16 stays finite."""
+    f = fusco()
+    E, H, I = 4, 64, 32
+    x, w_in, w_out = torch.zeros((N, H)), torch.zeros((E, 2 * I, H)), torch.zeros((E, H, I))
+    x[:, :3] = 1.0
+    # unit 0: g = 2^64, u = 2^64 - 2^55, and 2^128 (1 - 2^-9) is the middle between bf16's largest number and the next power
+    w_in[:, 0, 0], w_in[:, I, 0], w_in[:, I, 1] = 2.0 ** 64, 2.0 ** 64, -2.0 ** 55
+    w_out[:, 0, 0] = 2.0 ** -120
+    chosen = torch.arange(N * k).remainder(E).int().view(N, k)
+    w = torch.full((N, k), 1.0 / k)
+    out = torch.empty((N, H), device="cuda")
+
+    def run():
+        f.fusco_moe_few(x.bfloat16().cuda(), chosen.cuda(), w.cuda(), w_in.bfloat16().cuda(), w_out.bfloat16().cuda(), out)
+
+    run()
+    assert bool((out[:, 0] == 255.5).all()) and not bool(out[:, 1:].any())
+    w_in[:, 1, 0], w_in[:, I + 1, 0] = 2.0 ** 100, 2.0 ** 100
+    w_out[:] = 1.0
+    run()
+    assert bool((out == float("inf")).all())
+    w_in[:, 1, 1] = float("nan")
+    run()
+    assert bool(out.isnan().all())
+
+
 def test_as_the_calls_one_by_one():
     """The same layer by plan and dispatch, products and combine: both are within their roundings of the same number."""
     f = fusco()
