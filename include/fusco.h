@@ -459,7 +459,8 @@ int fusco_experts_linear(const fusco_layout *L, const void *d_x, const void *d_w
  * contiguous; d_scale fp32: [rows, scale_stride] for rows (columns behind the last block's are left as they are: dispatch moves
  * them as its second plane, whose rows are multiples of 16 bytes), [rows / matrix_rows, ceil(matrix_rows / 128), ceil(columns / 128)]
  * for matrices.  fusco_from_fp8 writes x = q * s for any scales, rounded once; with the powers of two above bf16 holds it exactly.
- * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, and less than 2^31 blocks of 128 columns.
+ * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, less than 2^29 blocks of 128 columns of
+ * rows, and less than 2^24 blocks of matrices.
  */
 #define FUSCO_MAX_SCALE_STRIDE 65536
 typedef struct fusco_fp8 {
@@ -525,7 +526,8 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
  * nothing; a token's equal experts count together.  An expert's weights reach only the tokens that chose it.
  * d_x [N, H] bf16, d_topk_idx and d_w [N, k], d_out [N, H] of out_dtype (FUSCO_BF16 or FUSCO_F32).  weight_dtype FUSCO_BF16: d_w_in [E, 2 I, H] and
  * d_w_out [E, H, I] as for fusco_experts_gated and fusco_experts_linear, H and I multiples of 8, scales NULL.  FUSCO_E4M3: weights and scales as for
- * fusco_experts_gated_fp8 and fusco_experts_linear_fp8, H and I multiples of 16.  d_scratch: fusco_moe_few_scratch_bytes() bytes, contents
+ * fusco_experts_gated_fp8 and fusco_experts_linear_fp8, H and I multiples of 16.  An expert's w_in has less than 2^31 - 2^24 bytes, and
+ * min(N k, E) I / 8 is less than 2^24 - 1.  Infinite weights of w_out give infinities or NaN.  d_scratch: fusco_moe_few_scratch_bytes() bytes, contents
  * irrelevant before and after.
  */
 #define FUSCO_E4M3 2

@@ -6,7 +6,7 @@
 // and s would keep no more bits of any value that is not among the block's smallest.  A block is 128 columns of a row, or 128 x 128 of a matrix.
 // Infinities and NaN become NaN and take no part in the maximum; a block of zeros has scale 1.  Scales are at least 2^-126.
 //
-// Bound by memory.
+// Bound by memory: x read once, q and scales written once, or the other way round; of a few rows by the launch (128 rows of 4096 4 us).
 #ifndef FUSCO_CSRC_EIGHT_H
 #define FUSCO_CSRC_EIGHT_H
 
@@ -18,6 +18,7 @@ constexpr int kBlockColumns = 128;
 constexpr int kBlockLanes = kBlockColumns / kEight;   // lanes that hold one row of a block
 constexpr int kEightThreads = 256;
 constexpr int kEightGroups = kEightThreads / kBlockLanes;
+constexpr int kEightEach = 2;                         // blocks per group of lanes
 
 struct EightArgs {
     const char *in;
@@ -101,20 +102,21 @@ struct EightPlace {
     __device__ __forceinline__ size_t element(const EightArgs &a) const { return (size_t)row * a.columns + column; }
 };
 
-// Rows: 16 lanes per block, EACH blocks per group of lanes
-template <bool BF16, bool PAST, int EACH>
+// Rows: 16 lanes per block, two blocks per group of lanes (bf16, one / two / four / eight, us: 2048 rows of 4096 6.6 / 6.4 / 6.9 / 7.8, 9222 of 1040 7.3 / 7.5 / 8.3 / 9.3, 131072 of
+// 4096 284 / 271 / 278 / 278, 5.9 TB/s; back 269 / 265 / 273 / 280)
+template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kEightThreads) void rows_to_eight_kernel(EightArgs a)
 {
-    const uint32_t first = blockIdx.x * (kEightGroups * EACH) + threadIdx.x / kBlockLanes;
-    RawEight<BF16> raw[EACH];
+    const uint32_t first = blockIdx.x * (kEightGroups * kEightEach) + threadIdx.x / kBlockLanes;
+    RawEight<BF16> raw[kEightEach];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
+    for (int i = 0; i < kEightEach; ++i) {
         const EightPlace at(a, first + i * kEightGroups);
         raw[i] = {};
         if (at.in) raw[i] = load_raw<BF16, PAST>(a.in, at.element(a));
     }
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
+    for (int i = 0; i < kEightEach; ++i) {
         const EightPlace at(a, first + i * kEightGroups);
         const Eight e = wide<BF16>(raw[i]);
         const uint32_t exponent = scale_exponent(sixteen_max(largest(e)));
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(kEightThreads) void rows_to_eight_kernel(EightArgs 
     }
 }
 
-// Matrices: a workgroup per block of 128 x 128, which it holds in registers
+// Matrices: a workgroup per block of 128 x 128, which it holds in registers, so that x is read once (64 fp32 matrices of 2048 x 1408: 178 us, 5.2 TB/s; as bf16 back 91, 6.1)
 template <bool BF16, bool PAST>
 __global__ __launch_bounds__(kEightThreads) void matrix_to_eight_kernel(EightArgs a)
 {
@@ -158,14 +160,14 @@ __global__ __launch_bounds__(kEightThreads) void matrix_to_eight_kernel(EightArg
 }
 
 // Back, for rows and matrices: values times their block's scale, whatever it is, rounded once
-template <bool BF16, int EACH>
+template <bool BF16>
 __global__ __launch_bounds__(kEightThreads) void from_eight_kernel(EightArgs a)
 {
-    const uint32_t first = blockIdx.x * (kEightGroups * EACH) + threadIdx.x / kBlockLanes;
-    u32x2 q[EACH];
-    float scale[EACH];
+    const uint32_t first = blockIdx.x * (kEightGroups * kEightEach) + threadIdx.x / kBlockLanes;
+    u32x2 q[kEightEach];
+    float scale[kEightEach];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
+    for (int i = 0; i < kEightEach; ++i) {
         const EightPlace at(a, first + i * kEightGroups);
         q[i] = u32x2{0, 0};
         scale[i] = 0.0f;
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(kEightThreads) void from_eight_kernel(EightArgs a)
         scale[i] = a.scale[(size_t)row * a.scale_stride + at.block];
     }
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) {
+    for (int i = 0; i < kEightEach; ++i) {
         const EightPlace at(a, first + i * kEightGroups);
         if (at.in) store_eight<BF16>(a.out, at.element(a), from_eight(q[i], scale[i]));
     }

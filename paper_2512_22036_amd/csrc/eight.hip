@@ -15,8 +15,11 @@ bool scale_stride_ok(int32_t stride, int32_t columns) { return stride >= blocks_
 int fp8_check(const fusco_fp8 *f)
 {
     if (!f || f->rows < 0 || !eight_row_ok(f->columns) || f->matrix_rows < 0 || !scale_stride_ok(f->scale_stride, f->columns)) return FUSCO_ERR_INVALID_ARG;
-    if (f->rows > INT32_MAX || f->rows * blocks_of(f->columns) > INT32_MAX) return FUSCO_ERR_INVALID_ARG;
+    if (f->rows > INT32_MAX) return FUSCO_ERR_INVALID_ARG;
     if (f->matrix_rows && (f->rows % f->matrix_rows != 0 || f->scale_stride != blocks_of(f->columns))) return FUSCO_ERR_INVALID_ARG;
+    // a launch has fewer than 2^32 threads
+    if (f->rows * blocks_of(f->columns) >= ((int64_t)1 << 32) / (kBlockLanes / kEightEach)) return FUSCO_ERR_INVALID_ARG;
+    if (f->matrix_rows && f->rows / f->matrix_rows * blocks_of(f->matrix_rows) * blocks_of(f->columns) >= ((int64_t)1 << 32) / kEightThreads) return FUSCO_ERR_INVALID_ARG;
     return dtype_ok(f->dtype) ? FUSCO_OK : FUSCO_ERR_UNSUPPORTED;
 }
 
@@ -27,24 +30,13 @@ EightArgs eight_args(const fusco_fp8 *f, const void *in, void *out, const float 
             f->matrix_rows, blocks_of(f->matrix_rows)};
 }
 
-// blocks per group of lanes: one where that leaves compute units without work
-constexpr int kEachMany = 4;
-bool few_blocks(const EightArgs &a) { return a.blocks < (uint32_t)(kCus * kEightGroups * kEachMany); }
-dim3 block_grid(const EightArgs &a, int each) { return dim3((a.blocks + kEightGroups * each - 1) / (kEightGroups * each)); }
+dim3 block_grid(const EightArgs &a) { return dim3((a.blocks + kEightGroups * kEightEach - 1) / (kEightGroups * kEightEach)); }
 
 template <bool BF16, bool PAST>
 void launch_to_eight(const fusco_fp8 *f, const EightArgs &a, hipStream_t s)
 {
     if (f->matrix_rows) hipLaunchKernelGGL((matrix_to_eight_kernel<BF16, PAST>), dim3((unsigned)(f->rows / f->matrix_rows * a.scale_rows * a.per_row)), dim3(kEightThreads), 0, s, a);
-    else if (few_blocks(a)) hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST, 1>), block_grid(a, 1), dim3(kEightThreads), 0, s, a);
-    else hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST, kEachMany>), block_grid(a, kEachMany), dim3(kEightThreads), 0, s, a);
-}
-
-template <bool BF16>
-void launch_from_eight(const EightArgs &a, hipStream_t s)
-{
-    if (few_blocks(a)) hipLaunchKernelGGL((from_eight_kernel<BF16, 1>), block_grid(a, 1), dim3(kEightThreads), 0, s, a);
-    else hipLaunchKernelGGL((from_eight_kernel<BF16, kEachMany>), block_grid(a, kEachMany), dim3(kEightThreads), 0, s, a);
+    else hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST>), block_grid(a), dim3(kEightThreads), 0, s, a);
 }
 
 // arguments of a product of e4m3 rows [P, C] with e4m3 weights; gated: `outputs` units
@@ -71,6 +63,9 @@ int few_check(const fusco_few *f)
     // loads inside one expert's weights, inside x and inside h are addressed with 31 bits
     if (2 * (int64_t)f->I * f->H * (eight ? 1 : 2) >= (int64_t)kNowhere || (int64_t)f->N * f->k * f->I * 2 * kParts >= (int64_t)kNowhere || (int64_t)f->N * f->H * 2 >= (int64_t)kNowhere)
         return FUSCO_ERR_INVALID_ARG;
+    // blocks of eight units of all experts that can be chosen, a workgroup of 256 threads each: fewer than 2^32 threads
+    const int64_t experts = f->N * f->k < f->E ? f->N * f->k : f->E;
+    if (experts * ((f->I + 7) / 8) >= ((int64_t)1 << 24) - 1) return FUSCO_ERR_INVALID_ARG;
     return FUSCO_OK;
 }
 
@@ -173,8 +168,8 @@ int fusco_from_fp8(const fusco_fp8 *f, const void *d_q, const float *d_scale, vo
     if (check_pointers(f->rows == 0, p, 3) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
     if (f->rows == 0) return FUSCO_OK;
     const EightArgs a = eight_args(f, d_q, d_x, d_scale);
-    if (f->dtype == FUSCO_BF16) launch_from_eight<true>(a, (hipStream_t)stream);
-    else launch_from_eight<false>(a, (hipStream_t)stream);
+    if (f->dtype == FUSCO_BF16) hipLaunchKernelGGL(from_eight_kernel<true>, block_grid(a), dim3(kEightThreads), 0, (hipStream_t)stream, a);
+    else hipLaunchKernelGGL(from_eight_kernel<false>, block_grid(a), dim3(kEightThreads), 0, (hipStream_t)stream, a);
     return launch_status();
 }
 

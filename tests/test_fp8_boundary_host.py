@@ -30,7 +30,8 @@ def test_there_and_back(lib, name):  # noqa: F811
     call = lambda f, *a: getattr(lib, name)(ctypes.byref(f), *a)
     for bad in (dict(rows=-1), dict(columns=0), dict(columns=-16), dict(columns=8), dict(columns=24), dict(columns=(1 << 20) + 16), dict(matrix_rows=-1), dict(scale_stride=1), dict(scale_stride=-1),
                 dict(scale_stride=65537), dict(matrix_rows=60), dict(matrix_rows=32, scale_stride=3), dict(rows=1 << 31), dict(rows=1 << 30, columns=512, scale_stride=4),
-                dict(rows=1 << 62)):
+                dict(rows=1 << 62), dict(rows=1 << 29, columns=16, scale_stride=1), dict(rows=1 << 24, matrix_rows=1, columns=16, scale_stride=1),
+                dict(rows=1 << 27, matrix_rows=1 << 7, columns=2048, scale_stride=16)):   # more threads than a launch has
         assert call(fp8(**bad), BUF, BUF, BUF, None) == -1, bad
     for bad in (dict(dtype=2), dict(dtype=-1)):
         assert call(fp8(**bad), BUF, BUF, BUF, None) == -3, bad
@@ -106,7 +107,7 @@ def test_few(lib):  # noqa: F811
     assert need >= 4 * 2 * 32 * 4 and lib.fusco_moe_few_scratch_bytes(65, 2, 32) == lib.fusco_moe_few_scratch_bytes(-1, 2, 32) == lib.fusco_moe_few_scratch_bytes(4, 65, 32) == 0
     call = lambda f, *a: lib.fusco_moe_few(ctypes.byref(f), *a)
     good = [BUF, BUF, BUF, BUF, None, BUF, None, BUF, BUF, need, None]
-    for bad in (dict(N=-1), dict(N=65), dict(E=0), dict(E=1025), dict(k=0), dict(k=65), dict(H=0), dict(H=12), dict(I=4), dict(I=-8), dict(H=1 << 20), dict(H=1 << 15, I=1 << 15)):
+    for bad in (dict(N=-1), dict(N=65), dict(E=0), dict(E=1025), dict(k=0), dict(k=65), dict(H=0), dict(H=12), dict(I=4), dict(I=-8), dict(H=1 << 20), dict(H=1 << 15, I=1 << 15), dict(N=64, k=64, E=256, H=8, I=1 << 19)):
         assert call(few(**bad), *good[:9], 1 << 40, None) == -1, bad
     for bad in (dict(weight_dtype=1), dict(weight_dtype=3), dict(out_dtype=2), dict(out_dtype=-1)):
         assert call(few(**bad), *good) == -3, bad
