@@ -832,23 +832,35 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
         const uint32_t second = (uint32_t)p.NA * kSize;
         int lane = tid & 63;
         asm volatile("" : "+v"(lane));   // places are worked out here, not kept in registers over the sums
+        // Kept pre-activations, all at once: sixteen of a lane's are one load, and lie in one block of scales.  A wave's gates lie in one, its ups in two neighbours at the
+        // most (32768 uneven rows of 64 experts, 2048 x 1408: 285 us; a fragment's at a time, each with its scale, 304).
+        words4 kept[STORE == kStoreGatedGradKept ? FB : 1][kOutA][2];
+        float scale[STORE == kStoreGatedGradKept ? FB : 1][3];
+        static_assert(128 % (kOutA * 32) == 0, "a wave's gates in one block of scales");
+        const int first_up = (a0 + wa * kOutA * 32 + p.NA) / 128;
+        if constexpr (STORE == kStoreGatedGradKept) {
 #pragma unroll
-        for (int j = 0; j < FB; ++j) {
-            const int b = (wb * FB + j) * 32 + (lane & 31);
-            bf16x8 gates[STORE == kStoreGatedGrad ? kOutA : 1][2], ups[STORE == kStoreGatedGrad ? kOutA : 1][2];
-            words4 kept[STORE == kStoreGatedGradKept ? kOutA : 1][2];      // sixteen of a lane's are one load, and lie in one block of scales
-            float scale[STORE == kStoreGatedGradKept ? kOutA : 1][2];
-            if constexpr (STORE == kStoreGatedGradKept) {
+            for (int j = 0; j < FB; ++j) {
+                const int b = (wb * FB + j) * 32 + (lane & 31);
 #pragma unroll
                 for (int f = 0; f < kOutA; ++f)
 #pragma unroll
                     for (int up = 0; up < 2; ++up) {
-                        const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16, column = a0 + a + up * p.NA;
-                        const bool in = a < a_left && b < b_left;
-                        kept[f][up] = __builtin_amdgcn_raw_buffer_load_b128(pre.to, in ? (int)(b * pre.ld + a + up * p.NA) : (int)kNowhere, 0, 0);
-                        scale[f][up] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(kept_scale, in ? (b * p.row_scales + column / 128) * 4 : (int)kNowhere, 0, 0));
+                        const int a = (wa * kOutA + f) * 32 + (lane >> 5) * 16;
+                        kept[j][f][up] = __builtin_amdgcn_raw_buffer_load_b128(pre.to, a < a_left && b < b_left ? (int)(b * pre.ld + a + up * p.NA) : (int)kNowhere, 0, 0);
                     }
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    const int block = i == 0 ? (a0 + wa * kOutA * 32) / 128 : min(first_up + i - 1, p.row_scales - 1);
+                    scale[j][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(kept_scale, b < b_left ? (b * p.row_scales + block) * 4 : (int)kNowhere, 0, 0));
+                }
             }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int j = 0; j < FB; ++j) {
+            const int b = (wb * FB + j) * 32 + (lane & 31);
+            bf16x8 gates[STORE == kStoreGatedGrad ? kOutA : 1][2], ups[STORE == kStoreGatedGrad ? kOutA : 1][2];
             if constexpr (STORE == kStoreGatedGrad) {   // all pre-activations at once, not one after the other
 #pragma unroll
                 for (int f = 0; f < kOutA; ++f)
@@ -905,8 +917,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
                     } else {
                         float dup[8], gate[8], up[8];
                         if constexpr (STORE == kStoreGatedGradKept) {
-                            wide_eight(kept[f][0][2 * h], kept[f][0][2 * h + 1], scale[f][0], gate);
-                            wide_eight(kept[f][1][2 * h], kept[f][1][2 * h + 1], scale[f][1], up);
+                            wide_eight(kept[j][f][0][2 * h], kept[j][f][0][2 * h + 1], scale[j][0], gate);
+                            wide_eight(kept[j][f][1][2 * h], kept[j][f][1][2 * h + 1], (a0 + a + p.NA) / 128 == first_up ? scale[j][1] : scale[j][2], up);
                         } else {
 #pragma unroll
                             for (int q = 0; q < 8; ++q) {
