@@ -254,8 +254,9 @@ struct TileState {
     }
     __device__ __forceinline__ void load_b(int s, char *slot) const
     {
+        const typename B::Place place = b.place();
 #pragma unroll
-        for (int i = 0; i < B::kLoads; ++i) b.load(stage_of(s), i, slot, wave, b.place());
+        for (int i = 0; i < B::kLoads; ++i) b.load(stage_of(s), i, slot, wave, place);
     }
     // The scales of a stage that is asked for; where they will lie is known by then (asked, -1 past the last stage)
     __device__ __forceinline__ void load_scales(int s)
