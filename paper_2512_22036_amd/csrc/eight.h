@@ -87,6 +87,14 @@ __device__ __forceinline__ Eight from_eight(u32x2 q, float scale)
     return e;
 }
 
+// STREAMED: past the caches
+template <bool STREAMED>
+__device__ __forceinline__ void put_eight(char *to, u32x2 q)
+{
+    if (STREAMED) __builtin_nontemporal_store(q, (u32x2 *)to);
+    else *(u32x2 *)to = q;
+}
+
 // Block b of a row-major list of rows: its row, and the column of this lane's eight values; false where there are none
 struct EightPlace {
     uint32_t row, block;
@@ -104,7 +112,7 @@ struct EightPlace {
 
 // Rows: 16 lanes per block, two blocks per group of lanes (bf16, one / two / four / eight, us: 2048 rows of 4096 6.6 / 6.4 / 6.9 / 7.8, 9222 of 1040 7.3 / 7.5 / 8.3 / 9.3, 131072 of
 // 4096 284 / 271 / 278 / 278, 5.9 TB/s; back 269 / 265 / 273 / 280)
-template <bool BF16, bool PAST>
+template <bool BF16, bool PAST, bool STREAMED>
 __global__ __launch_bounds__(kEightThreads) void rows_to_eight_kernel(EightArgs a)
 {
     const uint32_t first = blockIdx.x * (kEightGroups * kEightEach) + threadIdx.x / kBlockLanes;
@@ -121,23 +129,25 @@ __global__ __launch_bounds__(kEightThreads) void rows_to_eight_kernel(EightArgs 
         const Eight e = wide<BF16>(raw[i]);
         const uint32_t exponent = scale_exponent(sixteen_max(largest(e)));
         if (!at.in) continue;
-        *(u32x2 *)(a.out + at.element(a)) = to_eight(e, exponent);
+        put_eight<STREAMED>(a.out + at.element(a), to_eight(e, exponent));
         if (threadIdx.x % kBlockLanes == 0) a.scale[(size_t)at.row * a.scale_stride + at.block] = __uint_as_float(exponent << 23);
     }
 }
 
-// Matrices: a workgroup per block of 128 x 128, which it holds in registers, so that x is read once (64 fp32 matrices of 2048 x 1408: 178 us, 5.2 TB/s; as bf16 back 91, 6.1)
-template <bool BF16, bool PAST>
-__global__ __launch_bounds__(kEightThreads) void matrix_to_eight_kernel(EightArgs a)
+// Matrices: a workgroup per block of 128 x 128, which it holds in registers, so that x is read once (64 fp32 matrices of 2048 x 1408 with 256 / 512 / 1024 threads 178 / 175 / 173 us, q
+// past the caches 512 / 1024 165 / 171, 5.6 TB/s; of bf16 107 / 97 / 96 and 93 / 96; back to bf16 87, 6.3)
+constexpr int kMatrixThreads = 512;
+template <bool BF16, bool PAST, bool STREAMED>
+__global__ __launch_bounds__(kMatrixThreads) void matrix_to_eight_kernel(EightArgs a)
 {
-    constexpr int kRows = kBlockColumns / kEightGroups;   // per thread
-    __shared__ uint32_t part[kEightThreads / kWave];
+    constexpr int kGroups = kMatrixThreads / kBlockLanes, kRows = kBlockColumns / kGroups;   // per thread
+    __shared__ uint32_t part[kMatrixThreads / kWave];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t block = blockIdx.x % a.per_row, down = blockIdx.x / a.per_row, matrix = down / a.scale_rows;
     const int row0 = (int)(down - matrix * a.scale_rows) * kBlockColumns + (int)threadIdx.x / kBlockLanes;
     const int column = (int)block * kBlockColumns + (int)(threadIdx.x % kBlockLanes) * kEight;
-    auto element = [&](int i) { return ((size_t)matrix * a.matrix_rows + row0 + i * kEightGroups) * a.columns + column; };
-    auto in = [&](int i) { return column < a.columns && row0 + i * kEightGroups < a.matrix_rows; };
+    auto element = [&](int i) { return ((size_t)matrix * a.matrix_rows + row0 + i * kGroups) * a.columns + column; };
+    auto in = [&](int i) { return column < a.columns && row0 + i * kGroups < a.matrix_rows; };
     RawEight<BF16> raw[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
@@ -152,10 +162,13 @@ __global__ __launch_bounds__(kEightThreads) void matrix_to_eight_kernel(EightArg
                               max((uint32_t)__builtin_amdgcn_readlane((int)m, 32), (uint32_t)__builtin_amdgcn_readlane((int)m, 48)));
     if (lane == 0) part[wave] = here;
     __syncthreads();
-    const uint32_t exponent = scale_exponent(max(max(part[0], part[1]), max(part[2], part[3])));
+    uint32_t all = part[0];
+#pragma unroll
+    for (int v = 1; v < kMatrixThreads / kWave; ++v) all = max(all, part[v]);
+    const uint32_t exponent = scale_exponent(all);
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
-        if (in(i)) *(u32x2 *)(a.out + element(i)) = to_eight(wide<BF16>(raw[i]), exponent);
+        if (in(i)) put_eight<STREAMED>(a.out + element(i), to_eight(wide<BF16>(raw[i]), exponent));
     if (threadIdx.x == 0) a.scale[(size_t)down * a.scale_stride + block] = __uint_as_float(exponent << 23);
 }
 

@@ -19,7 +19,7 @@ int fp8_check(const fusco_fp8 *f)
     if (f->matrix_rows && (f->rows % f->matrix_rows != 0 || f->scale_stride != blocks_of(f->columns))) return FUSCO_ERR_INVALID_ARG;
     // a launch has fewer than 2^32 threads
     if (f->rows * blocks_of(f->columns) >= ((int64_t)1 << 32) / (kBlockLanes / kEightEach)) return FUSCO_ERR_INVALID_ARG;
-    if (f->matrix_rows && f->rows / f->matrix_rows * blocks_of(f->matrix_rows) * blocks_of(f->columns) >= ((int64_t)1 << 32) / kEightThreads) return FUSCO_ERR_INVALID_ARG;
+    if (f->matrix_rows && f->rows / f->matrix_rows * blocks_of(f->matrix_rows) * blocks_of(f->columns) >= ((int64_t)1 << 32) / kMatrixThreads) return FUSCO_ERR_INVALID_ARG;
     return dtype_ok(f->dtype) ? FUSCO_OK : FUSCO_ERR_UNSUPPORTED;
 }
 
@@ -32,11 +32,22 @@ EightArgs eight_args(const fusco_fp8 *f, const void *in, void *out, const float 
 
 dim3 block_grid(const EightArgs &a) { return dim3((a.blocks + kEightGroups * kEightEach - 1) / (kEightGroups * kEightEach)); }
 
-template <bool BF16, bool PAST>
+template <bool BF16, bool PAST, bool STREAMED>
 void launch_to_eight(const fusco_fp8 *f, const EightArgs &a, hipStream_t s)
 {
-    if (f->matrix_rows) hipLaunchKernelGGL((matrix_to_eight_kernel<BF16, PAST>), dim3((unsigned)(f->rows / f->matrix_rows * a.scale_rows * a.per_row)), dim3(kEightThreads), 0, s, a);
-    else hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST>), block_grid(a), dim3(kEightThreads), 0, s, a);
+    if (f->matrix_rows) hipLaunchKernelGGL((matrix_to_eight_kernel<BF16, PAST, STREAMED>), dim3((unsigned)(f->rows / f->matrix_rows * a.scale_rows * a.per_row)), dim3(kMatrixThreads), 0, s, a);
+    else hipLaunchKernelGGL((rows_to_eight_kernel<BF16, PAST, STREAMED>), block_grid(a), dim3(kEightThreads), 0, s, a);
+}
+
+// x past the caches where they cannot hold it, q where little of it would still be there when it is read, rows by the next call, matrices later.  To and back, q through / past the caches,
+// us: rows 131072 x 4096 549 / 512, 131072 x 1280 (q 168 MB) 153 / 162; fp32 matrices 64 x 1408 x 2048 (q 185 MB) 261 / 251, 128 x 4096 x 1280 1053 / 975, 8 x 2560 x 4096 (q 84 MB) 110 / 115.
+template <bool BF16>
+void launch_to_eight(const fusco_fp8 *f, const EightArgs &a, hipStream_t s)
+{
+    const int64_t elements = f->rows * f->columns;
+    if (elements > (f->matrix_rows ? kCacheBytes / 2 : kCacheBytes)) launch_to_eight<BF16, true, true>(f, a, s);
+    else if (elements * (BF16 ? 2 : 4) > kCacheBytes) launch_to_eight<BF16, true, false>(f, a, s);
+    else launch_to_eight<BF16, false, false>(f, a, s);
 }
 
 // arguments of a product of e4m3 rows [P, C] with e4m3 weights; gated: `outputs` units
@@ -153,10 +164,8 @@ int fusco_to_fp8(const fusco_fp8 *f, const void *d_x, void *d_q, float *d_scale,
     if (check_pointers(f->rows == 0, p, 3) != FUSCO_OK) return FUSCO_ERR_INVALID_ARG;
     if (f->rows == 0) return FUSCO_OK;
     const EightArgs a = eight_args(f, d_x, d_q, d_scale);
-    const bool bf16 = f->dtype == FUSCO_BF16, past = f->rows * f->columns * (bf16 ? 2 : 4) > kCacheBytes;
-    hipStream_t s = (hipStream_t)stream;
-    if (bf16) past ? launch_to_eight<true, true>(f, a, s) : launch_to_eight<true, false>(f, a, s);
-    else past ? launch_to_eight<false, true>(f, a, s) : launch_to_eight<false, false>(f, a, s);
+    if (f->dtype == FUSCO_BF16) launch_to_eight<true>(f, a, (hipStream_t)stream);
+    else launch_to_eight<false>(f, a, (hipStream_t)stream);
     return launch_status();
 }
 

@@ -140,3 +140,16 @@ def test_far_weights(gen, eights):
     assert bool(out[0][0].any())
     for a, b in zip(*out):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("E,M,C", [(300, 520, 1040), (40, 1408, 2064)])     # e4m3 of more and of less than half of what the caches hold
+def test_matrices_by_one(gen, E, M, C, dtype):
+    f = fusco()
+    x = torch.randn((E, M, C), generator=gen, device="cuda").mul_(torch.rand((E, 1, 1), generator=gen, device="cuda")).to(dtype)
+    shape = (E, fp8.blocks(M), fp8.blocks(C))
+    q, scale, one, its = torch.zeros((E, M, C), dtype=torch.uint8, device="cuda"), torch.zeros(shape, device="cuda"), torch.zeros((1, M, C), dtype=torch.uint8, device="cuda"), torch.zeros((1,) + shape[1:], device="cuda")
+    f.fusco_to_fp8(x, q.view(FP8), scale)
+    for e in range(E):
+        f.fusco_to_fp8(x[e:e + 1], one.view(FP8), its)
+        assert torch.equal(q[e:e + 1], one) and torch.equal(scale[e:e + 1], its)
