@@ -244,7 +244,13 @@ struct TileState {
         typename A::Place a;
         typename B::Place b;
     };
-    __device__ __forceinline__ Places places() const { return {a.place(), b.place()}; }
+    Places kept;           // even and paired places of all stages
+    __device__ __forceinline__ Places places() const { return kSpared ? kept : Places{}; }
+    __device__ __forceinline__ void keep_places()
+    {
+        kept = {a.place(), b.place()};
+        asm volatile("" : "+v"(kept.a.chunk), "+v"(kept.a.at), "+v"(kept.b.chunk), "+v"(kept.b.at));
+    }
     __device__ __forceinline__ void load(int s, int i, char *slot) const { load(s, i, slot, places()); }
     __device__ __forceinline__ void load(int s, int i, char *slot, const Places &place) const
     {
@@ -254,7 +260,7 @@ struct TileState {
     }
     __device__ __forceinline__ void load_b(int s, char *slot) const
     {
-        const typename B::Place place = b.place();
+        const typename B::Place place = places().b;
 #pragma unroll
         for (int i = 0; i < B::kLoads; ++i) b.load(stage_of(s), i, slot, wave, place);
     }
@@ -964,6 +970,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     if (t >= total) return;
     clear();
     begin(t);
+    if constexpr (State::kSpared) s.keep_places();
     typename std::conditional<KEPT, typename State::Held[2], char>::type held;
     if constexpr (KEPT) {
         held[0] = s.hold(0);
