@@ -211,7 +211,7 @@ __device__ __forceinline__ void wide_eight(uint32_t first, uint32_t second, floa
 template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false>
 struct TileState {
     static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
-    static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no register to spare
+    static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no registers for places of its own
     static constexpr int kRun = GATED && FA == 2 ? 8 : 16;   // a lane's neighbouring outputs
     typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
     typedef Operand<BMODE, BB, kStageC, false, kSpared ? kEvenPlaces : kOwnPlaces> B;
@@ -366,7 +366,8 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
 // Stages of e4m3 operands: a matrix instruction takes a whole stage of 16 x 16 outputs, and its result, scaled, is added to the pair's sums two instructions
 // later.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
 // fragments ahead.)  In the middle of a stage all waves hold their fragments of b, and b's slot is asked for again: its loads then have one and a half stages, those of a one (131072
-// rows, linear 898 -> 799 us, gated 1408 -> 1390; the loads one by one over four instructions 816 and 1430; half of a's loads with them, in slots apart, 827 and 1510).
+// rows, linear 898 -> 799 us, gated 1408 -> 1390, 785 and 1357 with their places worked out once a stage, 779 and 1347 once a launch; with half of a's loads beside them, in slots
+// apart, 810 and 1450).
 constexpr int kRing = 2, kAhead = 1;   // fragments of a in registers, and how far ahead of their use they are read
 constexpr int kLate = 2, kParts8 = 4;  // instructions between a product and its use, products in registers
 
@@ -603,7 +604,7 @@ __device__ __forceinline__ int tile_in_list(int i)
 // with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
 // of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
 //
-// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1357 us, 2.03 PFLOP/s; linear, 1280 x 4096, 785 us, 1.75.  Matrix instructions run 53 and 43 % of the cycles, at 1.9 of 2.4 GHz,
+// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 53 and 43 % of the cycles, at 1.9 of 2.4 GHz,
 // the vector ones that scale their results beside them 52 and 45 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
 // stores the linear one four fifths.
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false>
