@@ -53,6 +53,7 @@ int launch_few(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 // 601; 16 of 2048 x 1408 with 128 rows, gradient of the pre-activations 32 / 48 / 61; 16 of 4096 x (2 x 1280) with 230 rows 224 / 185 / 127, its
 // gradient of the pre-activations 120 / 90 / 136.  E4m3 keeps the rule (20 products measured, of evenly spread rows, the worst choice 8 % slower): 128 experts of
 // 4096 x (2 x 1280) gated, 8 rows 232 / 248 / 283, 64 rows 268 / 267 / 294, 256 rows 806 / 513 / 392.
+inline double tiles_of_rows(const fusco_layout *L, int rows) { return fmax((double)L->E, (double)L->P / rows + 0.4 * L->E); }
 template <int STORE>
 int tile_rows(const fusco_layout *L, const ProductArgs &a)
 {
@@ -62,7 +63,7 @@ int tile_rows(const fusco_layout *L, const ProductArgs &a)
     double least = INFINITY;
     for (int i = 2; i >= 0; --i) {
         const int rows = 64 << i;
-        const double tiles = fmax((double)L->E, (double)L->P / rows + 0.4 * L->E) * across;
+        const double tiles = tiles_of_rows(L, rows) * across;
         const double time = ceil(tiles / kCus) * takes[i];
         if (time < least) {
             least = time;
@@ -82,6 +83,12 @@ int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
     return tile_rows<STORE>(L, a);
 }
 
+// Input gradients: tiles of 64 rows and 128 outputs, where a compute unit has one of them at the most.  Their stages take 64 elements of the sum, three of them under way, where a stage of 256
+// outputs has room for 32, and a single tile waits for its loads; sums keep their order.  Through the activation / without it, us, 256 outputs / 128: 8 experts, 2048 x 768, 32 rows each, 48
+// tiles 30 / 22 and 25 / 19; 16 of 1040 x 528, 38 rows, 80 tiles 21 / 16 and 16.6 / 13.5; 8 of 4096 x 1280, 64 rows, 130 tiles 67 / 46 and 60 / 43; 64 of 1024 x 512, 32 rows, 256 tiles
+// 29 / 19 and 24.6 / 16.5; more tiles than compute units, 64 of 2048 x 768, 384, 49 / 53.
+inline bool narrow(const fusco_layout *L, const ProductArgs &a) { return tiles_of_rows(L, 64) * ((a.NA + 127) / 128) <= kCus; }
+
 template <int AMODE, int STORE, bool EIGHT = false>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
@@ -91,6 +98,7 @@ int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
     }
     if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE, EIGHT>, a, s);
     else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE, EIGHT>, a, s);
+    else if constexpr (AMODE == kAcross) launch_product(narrow(L, a) ? product_kernel<AMODE, kAlongC, 64, 1, 1, STORE, false, false, 128> : product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
     else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE, EIGHT>, a, s);
     return launch_status();
 }

@@ -134,6 +134,21 @@ struct Operand {
         }
     }
 
+    // Stages of two halves of 32 elements that lie apart.  kAcross: load i is half i, of 32 rows; kAlongC: chunks 0 to 3 of a row are the first half, the others the second
+    __device__ __forceinline__ void load_half(int half, int i, char *lds, int wave) const
+    {
+        static_assert(MODE != kAcross || KC != 64 || kLoads == 2, "a half each");
+        const int left = min(max(c_size - half * 32, 0), 32);
+        const int bytes = __builtin_amdgcn_readfirstlane(max(left * (int)ld - (int)limit, 0));
+        to_lds(__builtin_amdgcn_make_buffer_rsrc((void *)(base + (int64_t)half * (int64_t)(32 * (int)ld)), 0, bytes, 0x00020000), lds + (i * kTileThreads + wave * kWave) * 16, at[0], 0);
+    }
+    __device__ __forceinline__ void load_halves(int first, int second, char *lds, int wave) const
+    {
+        static_assert(MODE != kAlongC || W != 64 || kLoads == 1, "one load");
+        const int of = chunk >> 2, half = of ? second : first;
+        to_lds(view(base, limit), lds + wave * (kWave * 16), half * 32 + (chunk & 3) * 8 < c_size ? at[0] + (half - of) * 64 : kNowhere, 0);
+    }
+
     // Load i of thread tid: which row of the stage's LDS (an output for kAlongC, a c for kAcross), and the first output (kAcross)
     static __device__ __forceinline__ int row_of(int i, int tid) { return MODE == kAlongC ? (i * kTileThreads + tid) / kRowLanes : (i * kTileThreads + tid) / (W / 8); }
     static __device__ __forceinline__ int swizzle(int row)
@@ -208,16 +223,18 @@ __device__ __forceinline__ void wide_eight(uint32_t first, uint32_t second, floa
 //
 // KEPT: operand A is rows of e4m3 with their scales, across c.  They pass registers on their way to LDS, where they become bf16 (with scales that are powers of two without
 // a rounding): a thread holds 16 outputs of one row of two stages.
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false>
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false, int AA = kTileA>
 struct TileState {
-    static constexpr int kStageC = AMODE == kAlongC ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
+    static constexpr int kStageC = AMODE == kAlongC || AA < kTileA ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
     static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no registers for places of its own
     static constexpr int kRun = GATED && FA == 2 ? 8 : 16;   // a lane's neighbouring outputs
-    typedef Operand<AMODE, kTileA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
+    typedef Operand<AMODE, AA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
     typedef Operand<BMODE, BB, kStageC, false, kSpared ? kEvenPlaces : kOwnPlaces> B;
     static constexpr int kStageBytes = A::kBytes + B::kBytes, kLoads = A::kLoads;
     static constexpr int kScaleLoads = EIGHT ? 1 : 0, kScaleStages = 4, kScaleBytes = (BB + kWave) * kScaleStages * 4;
     static_assert(A::kLoads >= B::kLoads, "the wider operand");
+    static constexpr bool kHalved = AA < kTileA;   // stages of two halves that are counted and come one by one: sums have the order of tiles whose stages are half as long
+    static constexpr int kCountC = kHalved ? 32 : kStageC;
     A a;
     B b;
     uint32_t a_lane, b_lane;
@@ -231,7 +248,7 @@ struct TileState {
     int32_t side, asked, next;                    // which of the two places is in use; where the scales of the stage asked for last lie, and of the next one to come
 
     // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
-    __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots - 1) / kSlots : 1; }
+    __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots * (kStageC / kCountC) - 1) / (kSlots * (kStageC / kCountC)) : 1; }
 
     // stages are taken in the order turn, turn + 1, ..., turn - 1; past the last one loads fetch nothing, but they are made, so that
     // the number of loads behind a stage is always the same
@@ -254,6 +271,11 @@ struct TileState {
     __device__ __forceinline__ void load(int s, int i, char *slot) const { load(s, i, slot, places()); }
     __device__ __forceinline__ void load(int s, int i, char *slot, const Places &place) const
     {
+        if (kHalved) {
+            a.load_half(stage_of(2 * s + i), i, slot, wave);
+            if (i == 0) b.load_halves(stage_of(2 * s), stage_of(2 * s + 1), slot + A::kBytes, wave);
+            return;
+        }
         const int at = stage_of(s);
         if (!KEPT && i < A::kLoads) a.load(at, i, slot, wave, place.a);
         if (!EIGHT && i < B::kLoads) b.load(at, i, slot + A::kBytes, wave, place.b);
@@ -597,7 +619,7 @@ __device__ __forceinline__ int tile_in_list(int i)
     return (i * kXcds + blockIdx.x % kXcds) * (kCus / kXcds) + blockIdx.x / kXcds;
 }
 
-// FA x FB fragments of 32 x 32 outputs per wave, kTileA / (32 * FA) waves along a
+// Tiles of AA x BB outputs, FA x FB fragments of 32 x 32 outputs per wave, AA / (32 * FA) waves along a
 //
 // Bound by the matrix instructions under the card's power limit where experts have many rows (8 experts of 16384 rows, 4096 x 2560: 1.21 to 1.29 PFLOP/s
 // forward, 1.15 to 1.20 input gradient, 1.20 to 1.38 weight gradient; 128 uneven ones of 1024 rows gated 1.13), by the weights where they have few (128 experts
@@ -607,14 +629,14 @@ __device__ __forceinline__ int tile_in_list(int i)
 // E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 53 and 43 % of the cycles, at 1.9 of 2.4 GHz,
 // the vector ones that scale their results beside them 52 and 45 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
 // stores the linear one four fifths.
-template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false>
+template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false, int AA = kTileA>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
-    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated, KEPT> State;
-    constexpr int kWavesA = kTileA / (32 * FA), kWavesB = BB / (32 * FB);
+    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated, KEPT, AA> State;
+    constexpr int kWavesA = AA / (32 * FA), kWavesB = BB / (32 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
     constexpr bool kGated = STORE == kStoreGated, kGatedGrad = STORE == kStoreGatedGrad || STORE == kStoreGatedGradKept;
-    constexpr int kUnitsA = kGated ? kTileA / 2 : kTileA;  // outputs along a per tile: a gated tile holds both rows of a unit
+    constexpr int kUnitsA = kGated ? AA / 2 : AA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
     constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
@@ -745,7 +767,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             s.b.left = b_left < BB ? b_left : BB;
 #pragma unroll
             for (int j = 0; !State::kSpared && j < State::B::kLoads; ++j) s.b.at[j] = (uint32_t)(State::B::row_of(j, tid) * s.b.ld) + (s.b.chunk << 4);
-            s.stages = (p.C + State::kStageC - 1) / State::kStageC;
+            s.stages = (p.C + State::kCountC - 1) / State::kCountC;
         } else {
             s.b.ld = (int64_t)p.NB * 2;
             s.b.limit = (int64_t)b0 * 2;
@@ -772,7 +794,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             }
         }
         // tiles begin at different stages, as in few_rows_kernel; neighbours along a, which share rows in an L2, at the same one
-        s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / 8) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
+        s.turn = s.stages > 0 ? (int)(((uint32_t)(e * 64 + ta / (8 * (kTileA / AA))) * 2654435761u >> 12) % (uint32_t)s.stages) : 0;
     };
 
     // Lane l holds, of fragment (f, j), the outputs a = 32 * f + l / 32 * 16 + 0 .. 15 of b = 32 * j + l % 32.

@@ -89,3 +89,17 @@ def test_scales_of_a_tile_stay_its_own(N, E, C):
         for e in range(L.E):
             part = y[bounds[e]:bounds[e + 1]]
             assert bool(part.isnan().all() if e % 2 == 0 else part.isfinite().all()), e
+
+
+@pytest.mark.parametrize("N,k,E,I,M,routing", [(2400, 2, 120, 256, 1040, "skewed"), (300, 2, 16, 528, 1040, "normal"), (64, 1, 60, 272, 72, "invalid"), (9, 2, 8, 2048, 64, "normal"), (5808, 1, 88, 256, 336, "round")])
+def test_input_grad_of_few_tiles(monkeypatch, N, k, E, I, M, routing):
+    """Tiles of 128 outputs, up to as many as there are workgroups by the mean of the rows; with 66 rows for every expert there are more."""
+    if routing == "round":
+        f, gen = fusco(), torch.Generator(device="cuda").manual_seed(16)
+        L = f.Layout(N, k, E, 1)
+        f.fusco_plan(L, torch.arange(N, device="cuda").remainder(E).int().view(N, 1))
+        bounds = L.array("exp_off").tolist()
+        assert sum((b - a + 63) // 64 for a, b in zip(bounds, bounds[1:])) * 2 > WORKGROUPS
+        monkeypatch.setattr(kept, "make", lambda *a: (L, gen, bounds))
+    assert max(E, N * k / 64 + 0.4 * E) * ((I + 127) // 128) <= WORKGROUPS
+    kept.test_input_grad(N, k, E, I, M, routing, True)
