@@ -89,6 +89,15 @@ int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
 // 29 / 19 and 24.6 / 16.5; more tiles than compute units, 64 of 2048 x 768, 384, 49 / 53.
 inline bool narrow(const fusco_layout *L, const ProductArgs &a) { return tiles_of_rows(L, 64) * ((a.NA + 127) / 128) <= kCus; }
 
+// E4m3 in tiles of 64 rows: three stages in LDS instead of two, where filling up the last turn costs hardly a stage.  Gated / linear, us, two / three: 60 experts of 2880 x (2 x 1040) with 12 rows 112
+// / 93 and 55 / 47; 256 of 7168 x (2 x 1024) with 9 664 / 614 and 361 / 358; 128 of 4096 x (2 x 1280) with 8 228 / 225; 64 of 2048 x 1408 with 20 linear 44.4 / 42.2; where a turn is filled up, sums of
+// 512 19.4 / 22.2, of 1024 31.3 / 32.9, of 2048 27.3 / 26.6, 73.6 / 75.0 and 22.3 / 23.0.
+inline bool three(const ProductArgs &a)
+{
+    const int stages = (a.C + 63) / 64;   // of 128 elements of one byte
+    return 100 * ((stages + 2) / 3 * 3) <= 107 * ((stages + 1) / 2 * 2);
+}
+
 template <int AMODE, int STORE, bool EIGHT = false>
 int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
 {
@@ -99,7 +108,8 @@ int launch_by_rows(const fusco_layout *L, const ProductArgs &a, hipStream_t s)
     if (rows == 256) launch_product(product_kernel<AMODE, kAlongC, 256, 4, 2, STORE, EIGHT>, a, s);
     else if (rows == 128) launch_product(product_kernel<AMODE, kAlongC, 128, 2, 2, STORE, EIGHT>, a, s);
     else if constexpr (AMODE == kAcross) launch_product(narrow(L, a) ? product_kernel<AMODE, kAlongC, 64, 1, 1, STORE, false, false, 128> : product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
-    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE, EIGHT>, a, s);
+    else if constexpr (EIGHT) launch_product(three(a) ? product_kernel<AMODE, kAlongC, 64, 2, 1, STORE, true, false, kTileA, true> : product_kernel<AMODE, kAlongC, 64, 2, 1, STORE, true>, a, s);
+    else launch_product(product_kernel<AMODE, kAlongC, 64, 2, 1, STORE>, a, s);
     return launch_status();
 }
 

@@ -217,15 +217,15 @@ __device__ __forceinline__ void wide_eight(uint32_t first, uint32_t second, floa
 // gradient 1103 / 1150, weight gradient 1206 / 1345).
 //
 // EIGHT: operands of e4m3, both along c, in the same LDS rows of 128 bytes, so that a stage is one block of scales.  Those of rows lie far apart, a line of the L2 each, and
-// come four stages at once, into one of two places of their own in turn: the first waves load those of 64 rows each (as many as the tile has rows), the next one the weights',
+// come four stages at once, into one of two (three) places of their own in turn: the first waves load those of 64 rows each (as many as the tile has rows), the next one the weights',
 // the others nothing (every wave counts the same loads).  One stage at a time they cost half as many requests to the L2 as the operands: 131072 rows, gated 1510
 // us / 1410.
 //
 // KEPT: operand A is rows of e4m3 with their scales, across c.  They pass registers on their way to LDS, where they become bf16 (with scales that are powers of two without
 // a rounding): a thread holds 16 outputs of one row of two stages.
-template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false, int AA = kTileA>
+template <int AMODE, int BMODE, int BB, int FA, int FB, bool EIGHT = false, bool GATED = false, bool KEPT = false, int AA = kTileA, bool THREE = false>
 struct TileState {
-    static constexpr int kStageC = AMODE == kAlongC || AA < kTileA ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAlongC ? 2 : 4;
+    static constexpr int kStageC = AMODE == kAlongC || AA < kTileA ? 64 : 32, kSlices = kStageC / 16, kSlots = AMODE == kAcross ? 4 : THREE ? 3 : 2;
     static constexpr bool kSpared = EIGHT && FA == 4;   // the tile that has no registers for places of its own
     static constexpr int kRun = GATED && FA == 2 ? 8 : 16;   // a lane's neighbouring outputs
     typedef Operand<AMODE, AA, kStageC, true, !kSpared ? kOwnPlaces : GATED ? kPairedPlaces : kEvenPlaces, EIGHT ? kRun : 0> A;
@@ -245,7 +245,8 @@ struct TileState {
     uint32_t scale_at;     // KEPT: this thread's byte offset
     uint32_t row_scale_lane, weight_scale_wave;   // where a lane and a wave read them
     char *groups;                                 // LDS of the scales, and behind both places room where nobody reads
-    int32_t side, asked, next;                    // which of the two places is in use; where the scales of the stage asked for last lie, and of the next one to come
+    int32_t side, asked, next, soon;              // which of the places is in use; where the scales of the stage asked for last lie, of the next one to come and (three slots) of the one after it
+    static constexpr int kSides = kSlots;         // stages that are asked for and not read yet may each be the first of a place of their own
 
     // turns through the slots of a tile: a tile has whole turns, at least one, and what is missing is filled up with stages of zeros
     __device__ __forceinline__ int turns() const { return stages > 0 ? (stages + kSlots * (kStageC / kCountC) - 1) / (kSlots * (kStageC / kCountC)) : 1; }
@@ -290,10 +291,10 @@ struct TileState {
     __device__ __forceinline__ void load_scales(int s)
     {
         const int at = stage_of(s), in = at < stages, fresh = in & (s == 0 | at % kScaleStages == 0);   // numbers: a branch would part the stage's instructions
-        side ^= fresh;
+        side = kSides == 2 ? side ^ fresh : side + fresh - (side + fresh == kSides ? kSides : 0);
         asked = in ? side * kScaleBytes + at % kScaleStages * 4 : -1;
         const uint32_t place = (threadIdx.x & 63) * (uint32_t)scale_step;
-        to_lds(view(scales, scale_bytes), groups + ((fresh & (wave <= BB / kWave)) ? side * kScaleBytes + wave * (kWave * 16) : 2 * kScaleBytes), fresh ? place : kNowhere,
+        to_lds(view(scales, scale_bytes), groups + ((fresh & (wave <= BB / kWave)) ? side * kScaleBytes + wave * (kWave * 16) : kSides * kScaleBytes), fresh ? place : kNowhere,
                at / kScaleStages * (kScaleStages * 4));
     }
     struct Held {
@@ -481,15 +482,20 @@ __device__ __forceinline__ void tile_stage8(S &t, char *cur, const char *nxt, ch
         }
     }
     x.of = next;
-    t.next = t.asked;
+    t.next = S::kSlots == 3 ? t.soon : t.asked;
+    t.soon = t.asked;
 }
 
 template <bool ACTIVE, int STORES, bool GATED, int FA, int FB, typename S>
-__device__ __forceinline__ void tile_turn8(S &t, char *slot0, char *slot1, char *b0, char *b1, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
+__device__ __forceinline__ void tile_turn8(S &t, char *slot0, char *slot1, char *slot2, char *b0, char *b1, char *b2, int ask, Eights<FB> &x, f32x4 (&acc)[FA][FB])
 {
-    static_assert(S::kSlots == 2, "operands along c");
     tile_stage8<ACTIVE, STORES, GATED>(t, slot0, slot1, b0, b1, ask, x, acc);
-    tile_stage8<ACTIVE, 0, GATED>(t, slot1, slot0, b1, b0, ask + 1, x, acc);
+    if constexpr (S::kSlots == 2) {
+        tile_stage8<ACTIVE, 0, GATED>(t, slot1, slot0, b1, b0, ask + 1, x, acc);
+    } else {
+        tile_stage8<ACTIVE, STORES, GATED>(t, slot1, slot2, b1, b2, ask + 1, x, acc);
+        tile_stage8<ACTIVE, 0, GATED>(t, slot2, slot0, b2, b0, ask + 2, x, acc);
+    }
 }
 
 // One turn through the slots, while stage ask, ask + 1, ... of this tile or the next are asked for.  STORES: stores that were issued after
@@ -629,19 +635,19 @@ __device__ __forceinline__ int tile_in_list(int i)
 // E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 53 and 43 % of the cycles, at 1.9 of 2.4 GHz,
 // the vector ones that scale their results beside them 52 and 45 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
 // stores the linear one four fifths.
-template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false, int AA = kTileA>
+template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false, int AA = kTileA, bool THREE = false>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
-    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated, KEPT, AA> State;
+    typedef TileState<AMODE, BMODE, BB, FA, FB, EIGHT, STORE == kStoreGated, KEPT, AA, THREE> State;
     constexpr int kWavesA = AA / (32 * FA), kWavesB = BB / (32 * FB);
     constexpr bool kByRows = BMODE == kAlongC;             // b is a token row (forward, input gradient), or a weight row
     constexpr bool kGated = STORE == kStoreGated, kGatedGrad = STORE == kStoreGatedGrad || STORE == kStoreGatedGradKept;
     constexpr int kUnitsA = kGated ? AA / 2 : AA;  // outputs along a per tile: a gated tile holds both rows of a unit
     static_assert(kWavesA * kWavesB * kWave == kTileThreads, "eight waves");
     static_assert(!kGated || FA % 2 == 0, "gate and up rows of a unit in one wave");
-    constexpr int kMore = State::kSlots == 4 ? State::kStageBytes : 16;
-    constexpr int kSlotBytes = EIGHT ? State::A::kBytes : State::kStageBytes, kRowsB = EIGHT ? State::B::kBytes : 16;   // e4m3: operand B has slots of its own
-    __shared__ __align__(1024) char slot0[kSlotBytes], slot1[kSlotBytes], slot2[kMore], slot3[kMore], rows0[kRowsB], rows1[kRowsB];
+    constexpr int kSlotBytes = EIGHT ? State::A::kBytes : State::kStageBytes, kRowsBytes = EIGHT ? State::B::kBytes : 16;   // e4m3: operand B has slots of its own
+    constexpr int kThird = State::kSlots >= 3 ? kSlotBytes : 16, kFourth = State::kSlots == 4 ? kSlotBytes : 16, kThirdRows = State::kSlots == 3 ? kRowsBytes : 16;
+    __shared__ __align__(1024) char slot0[kSlotBytes], slot1[kSlotBytes], slot2[kThird], slot3[kFourth], rows0[kRowsBytes], rows1[kRowsBytes], rows2[kThirdRows];
     __shared__ int offsets[FUSCO_MAX_E + 1], prefix[kByRows ? FUSCO_MAX_E + 1 : 1];
     __shared__ int part[kTileThreads / kWave];
 
@@ -669,7 +675,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     s.a_lane = EIGHT ? State::A::lane_at8(lane, wa * FA * 32) : State::A::lane_at(lane, wa * FA * 32);
     s.b_lane = EIGHT ? State::B::lane_at8(lane, wb * FB * 32) : State::B::lane_at(lane, wb * FB * 32);
     asm volatile("" : "+v"(s.a_lane), "+v"(s.b_lane));
-    __shared__ __align__(16) char groups[EIGHT ? 2 * State::kScaleBytes + kWave * 16 : 16];
+    __shared__ __align__(16) char groups[EIGHT ? State::kSides * State::kScaleBytes + kWave * 16 : 16];
     if constexpr (EIGHT) {
         s.groups = groups;
         s.side = 0;
@@ -1013,6 +1019,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     if constexpr (EIGHT) {
         s.load_b(1, rows1);
         s.load_scales(1);
+        s.soon = s.asked;
+    }
+    if constexpr (State::kSlots == 3) {
+        const int second = s.asked;
+#pragma unroll
+        for (int i = 0; i < State::kLoads; ++i) s.load(2, i, slot2);
+        s.load_b(2, rows2);
+        s.load_scales(2);
+        s.soon = second;
     }
     if constexpr (State::kSlots == 4) {
         // kept rows are asked for before the other operand of their stage, as in the loop: the waits count on that order
@@ -1043,7 +1058,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
             x.scale[j] = 0.0f;
         }
         read_scales<kGated>(s, s.next, x.of);
-        s.next = s.asked;
+        s.next = s.soon;
+        s.soon = s.asked;
 #pragma unroll
         for (int m = 0; m < kParts8; ++m) x.part[m] = {};
     } else {
@@ -1053,7 +1069,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
     auto turn = [&](auto multiplied, auto stores, int ask) {
         constexpr bool kMultiplied = decltype(multiplied)::value;
         constexpr int kBehind = decltype(stores)::value;
-        if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, rows0, rows1, ask, x, acc);
+        if constexpr (EIGHT) tile_turn8<kMultiplied, kBehind, kGated>(s, slot0, slot1, slot2, rows0, rows1, rows2, ask, x, acc);
         else if constexpr (KEPT) tile_turn_kept<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc, held);
         else tile_turn<kMultiplied, kBehind>(s, slot0, slot1, slot2, slot3, ask, x, acc);
     };

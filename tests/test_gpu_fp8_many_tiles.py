@@ -10,8 +10,8 @@ from test_gpu_experts_many_tiles import SIZES, WORKGROUPS, holds
 
 pytestmark = pytest.mark.gpu
 
-# products summed per output: a part of a block (one turn), a block and a bit, several turns with and without a ragged end
-SUMS = [(80, "normal"), (144, "skewed"), (912, "skewed"), (912, "invalid"), (1024, "normal")]
+# products summed per output: a part of a block (one turn), a block and a bit, several turns with and without a ragged end; and, for tiles of 64 rows, turns of three stages, whole and filled up
+SUMS = [(80, "normal"), (144, "skewed"), (912, "skewed"), (912, "invalid"), (1024, "normal"), (304, "normal"), (1040, "invalid"), (1408, "skewed"), (2896, "normal")]
 
 
 @pytest.mark.parametrize("total,routing", SUMS)
