@@ -632,8 +632,8 @@ __device__ __forceinline__ int tile_in_list(int i)
 // with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
 // of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
 //
-// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 53 and 43 % of the cycles, at 1.9 of 2.4 GHz,
-// the vector ones that scale their results beside them 52 and 45 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
+// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 54 and 44 % of the cycles, at 1.9 of 2.4 GHz,
+// the vector ones that scale their results beside them 48 and 41 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
 // stores the linear one four fifths.
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false, int AA = kTileA, bool THREE = false>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
