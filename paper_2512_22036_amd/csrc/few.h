@@ -231,7 +231,7 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
             for (int g = 0; g < G; ++g) acc[f][g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         for (int i0 = 0; i0 < mine; i0 += DEPTH) {
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {   // pieces past the last one are zeros
+            for (int d = 0; d < DEPTH; ++d) {   // pieces past the last one are zeros, and so is their scale: another one's may be infinite
                 bf16x8 xn[G][Piece::kSteps];
 #pragma unroll
                 for (int g = 0; g < G; ++g)
@@ -241,7 +241,8 @@ __global__ __launch_bounds__(WAVES *kWave, SIMD) void few_gated_kernel(FewArgs p
 #pragma unroll
                 for (int f = 0; f < F; ++f) wn[f] = w[d][f];
                 // of both scales, that of this lane's four rows of the results
-                const float now[2] = {EIGHT && F == 1 && lane >= 32 ? scale[d][1] : scale[d][0], scale[d][1]};
+                const bool in = i0 + d < mine;
+                const float now[2] = {!EIGHT || !in ? 0.0f : F == 1 && lane >= 32 ? scale[d][1] : scale[d][0], EIGHT && in ? scale[d][1] : 0.0f};
                 load_x(i0 + d + 1);
                 load(i0 + d + DEPTH, d);
 #pragma unroll

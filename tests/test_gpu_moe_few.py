@@ -247,3 +247,21 @@ def test_refusals():
     with pytest.raises(f.FuscoError):
         f.fusco_moe_few(x=bf16(gen, many, H), topk_idx=chosen, w=w, out=torch.empty((many, H), device="cuda"), **weights, scratch=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
     f.fusco_moe_few(x=bf16(gen, 0, H), topk_idx=chosen[:0], w=w[:0], out=torch.empty((0, H), device="cuda"), **weights)
+
+
+@pytest.mark.parametrize("N,E,k,H,I", [(1, 2, 1, 256, 16), (3, 12, 2, 144, 80), (40, 4, 2, 272, 48), (64, 128, 8, 400, 272)])   # every instance of the first product
+def test_infinite_scales(N, E, k, H, I):
+    """An infinite scale of one block of w_in: what is multiplied there is positive, and so are infinite the results of the tokens that chose the expert, and finite all others.  Waves
+    have pieces past their last one here."""
+    f = fusco()
+    gen = torch.Generator(device="cuda").manual_seed(37)
+    ones = lambda *s: torch.ones(s, device="cuda")
+    w_in_scale = ones(E, 2 * blocks(I), blocks(H))
+    chosen, w = routing(gen, N, E, k, "any")
+    chosen[0, 0] = 1
+    chosen[0, 1:] = 0
+    w_in_scale[1, 0, 0] = float("inf")
+    out = torch.empty((N, H), device="cuda")
+    f.fusco_moe_few(ones(N, H).bfloat16(), chosen, w, ones(E, 2 * I, H).to(FP8), ones(E, H, I).to(FP8), out, w_in_scale=w_in_scale, w_out_scale=ones(E, blocks(H), blocks(I)))
+    sick = (chosen == 1).any(dim=1)
+    assert bool((out[sick] == float("inf")).all()) and bool(out[~sick].isfinite().all())
