@@ -459,8 +459,8 @@ int fusco_experts_linear(const fusco_layout *L, const void *d_x, const void *d_w
  * contiguous; d_scale fp32: [rows, scale_stride] for rows (columns behind the last block's are left as they are: dispatch moves
  * them as its second plane, whose rows are multiples of 16 bytes), [rows / matrix_rows, ceil(matrix_rows / 128), ceil(columns / 128)]
  * for matrices.  fusco_from_fp8 writes x = q * s for any scales, rounded once; with the powers of two above bf16 holds it exactly.
- * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, less than 2^29 blocks of 128 columns of
- * rows, and less than 2^23 blocks of matrices.
+ * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, at most 2^29 - 32 blocks of 128 columns of
+ * rows (of matrices too), and less than 2^23 blocks of matrices.
  */
 #define FUSCO_MAX_SCALE_STRIDE 65536
 typedef struct fusco_fp8 {

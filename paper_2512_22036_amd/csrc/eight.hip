@@ -17,8 +17,9 @@ int fp8_check(const fusco_fp8 *f)
     if (!f || f->rows < 0 || !eight_row_ok(f->columns) || f->matrix_rows < 0 || !scale_stride_ok(f->scale_stride, f->columns)) return FUSCO_ERR_INVALID_ARG;
     if (f->rows > INT32_MAX) return FUSCO_ERR_INVALID_ARG;
     if (f->matrix_rows && (f->rows % f->matrix_rows != 0 || f->scale_stride != blocks_of(f->columns))) return FUSCO_ERR_INVALID_ARG;
-    // a launch has fewer than 2^32 threads
-    if (f->rows * blocks_of(f->columns) >= ((int64_t)1 << 32) / (kBlockLanes / kEightEach)) return FUSCO_ERR_INVALID_ARG;
+    // a launch has fewer than 2^32 threads, in whole workgroups
+    constexpr int kEach = kEightGroups * kEightEach;   // blocks of a workgroup
+    if (f->rows * blocks_of(f->columns) > UINT32_MAX / kEightThreads * kEach) return FUSCO_ERR_INVALID_ARG;
     if (f->matrix_rows && f->rows / f->matrix_rows * blocks_of(f->matrix_rows) * blocks_of(f->columns) >= ((int64_t)1 << 32) / kMatrixThreads) return FUSCO_ERR_INVALID_ARG;
     return dtype_ok(f->dtype) ? FUSCO_OK : FUSCO_ERR_UNSUPPORTED;
 }

@@ -43,6 +43,14 @@ def test_there_and_back(lib, name):  # noqa: F811
     assert call(fp8(rows=0, columns=8), None, None, None, None) == -1
 
 
+@pytest.mark.parametrize("name", ["fusco_to_fp8", "fusco_from_fp8"])
+def test_whole_workgroups_of_a_launch(lib, name):  # noqa: F811
+    """A workgroup has 32 blocks of rows and 256 threads: with 2^29 - 31 blocks the launch would come to 2^32 threads."""
+    for size in (dict(rows=(1 << 29) - 1, columns=16, scale_stride=1), dict(rows=(1 << 29) - 31, columns=16, scale_stride=1), dict(rows=(1 << 28) - 1, columns=256, scale_stride=2),
+                 dict(rows=(1 << 29) - 16, columns=16, scale_stride=1, matrix_rows=(1 << 29) - 16)):
+        assert getattr(lib, name)(ctypes.byref(fp8(**size)), BUF, BUF, BUF, None) == -1, size
+
+
 def test_products(lib):  # noqa: F811
     L, empty = layout(lib), layout(lib, N=0)
     g = lambda *a: lib.fusco_experts_gated_fp8(ctypes.byref(L), *a)
