@@ -164,6 +164,12 @@ int fusco_probe_segments_wide(uint64_t stream_capacity, uint64_t slice_bytes);
 int fusco_probe_experts_tile_rows(const fusco_layout *L, int which, int32_t outputs, int32_t sum);
 
 /*
+ * The same for the outputs that a tile holds (units of fusco_experts_gated): 32 where it holds 16 rows, else 256, or 128 of an input
+ * gradient that comes to few tiles; half as many units.
+ */
+int fusco_probe_experts_tile_outputs(const fusco_layout *L, int which, int32_t outputs, int32_t sum);
+
+/*
  * Measurement aid: kernel time without stream events between the kernels.  The next fusco_plan,
  * fusco_dispatch (fused modes), fusco_plan_dispatch or fusco_combine call made by the calling thread attaches the two HIP
  * events (hipEvent_t passed as void*, created with timing enabled) to its own kernels: start_event

@@ -25,7 +25,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfusco.so")
 
 EXPORTS = ("fusco_version", "fusco_status_string", "fusco_layout_bytes", "fusco_scratch_bytes",
-           "fusco_layout_bind", "fusco_plan", "fusco_plan_static", "fusco_dispatch", "fusco_dispatch_in_transfer_order", "fusco_combine", "fusco_plan_dispatch", "fusco_probe_copy", "fusco_probe_rows", "fusco_probe_pieces", "fusco_probe_consume_slices", "fusco_probe_time_next_call", "fusco_probe_source_chunk_bytes", "fusco_probe_dispatch_kernel", "fusco_probe_dispatch_occupancy", "fusco_probe_dispatch_pull", "fusco_probe_dispatch_walk", "fusco_probe_dispatch_route", "fusco_probe_plan_through", "fusco_probe_plan_dispatch_through", "fusco_probe_segments_wide", "fusco_probe_experts_tile_rows",
+           "fusco_layout_bind", "fusco_plan", "fusco_plan_static", "fusco_dispatch", "fusco_dispatch_in_transfer_order", "fusco_combine", "fusco_plan_dispatch", "fusco_probe_copy", "fusco_probe_rows", "fusco_probe_pieces", "fusco_probe_consume_slices", "fusco_probe_time_next_call", "fusco_probe_source_chunk_bytes", "fusco_probe_dispatch_kernel", "fusco_probe_dispatch_occupancy", "fusco_probe_dispatch_pull", "fusco_probe_dispatch_walk", "fusco_probe_dispatch_route", "fusco_probe_plan_through", "fusco_probe_plan_dispatch_through", "fusco_probe_segments_wide", "fusco_probe_experts_tile_rows", "fusco_probe_experts_tile_outputs",
            "fusco_combine_two_hop", "fusco_balance_groups", "fusco_cross_node_load", "fusco_segments_scan", "fusco_segments_copy",
            "fusco_disaggregated_plan", "fusco_disaggregated_dispatch", "fusco_disaggregated_combine",
            "fusco_combine_backward", "fusco_route", "fusco_route_backward", "fusco_norm_before", "fusco_norm_after", "fusco_norm_scratch_bytes",
@@ -128,6 +128,8 @@ def load_library() -> ctypes.CDLL:
     lib.fusco_probe_segments_wide.argtypes = [ctypes.c_uint64, ctypes.c_uint64]
     lib.fusco_probe_experts_tile_rows.restype = ctypes.c_int
     lib.fusco_probe_experts_tile_rows.argtypes = [ctypes.POINTER(_CLayout), ctypes.c_int, i32, i32]
+    lib.fusco_probe_experts_tile_outputs.restype = ctypes.c_int
+    lib.fusco_probe_experts_tile_outputs.argtypes = [ctypes.POINTER(_CLayout), ctypes.c_int, i32, i32]
     lib.fusco_probe_plan_dispatch_through.restype = ctypes.c_int
     lib.fusco_probe_plan_dispatch_through.argtypes = [ctypes.POINTER(_CLayout), sz, sz, vp]
     lib.fusco_probe_plan_through.restype = ctypes.c_int
@@ -1019,6 +1021,14 @@ def fusco_probe_experts_tile_rows(layout: Layout, which: int, outputs: int, sum:
     rc = int(load_library().fusco_probe_experts_tile_rows(ctypes.byref(layout.c), which, outputs, sum))
     if rc < 0:
         _check(rc, "fusco_probe_experts_tile_rows")
+    return rc
+
+
+def fusco_probe_experts_tile_outputs(layout: Layout, which: int, outputs: int, sum: int) -> int:
+    """Outputs per tile of the same products (PRODUCT_GATED: units) (fusco_probe.h).  Host-only."""
+    rc = int(load_library().fusco_probe_experts_tile_outputs(ctypes.byref(layout.c), which, outputs, sum))
+    if rc < 0:
+        _check(rc, "fusco_probe_experts_tile_outputs")
     return rc
 
 

@@ -153,6 +153,24 @@ void with_route_shape(const fusco_router *R, F f)
 
 bool aligned(const void *p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
+// ---- host-only queries: f(operand A's layout, how results are stored, arguments) of one of FUSCO_PROBE_PRODUCT_*
+
+template <typename F>
+int of_product(const fusco_layout *L, int which, int32_t outputs, int32_t sum, F f)
+{
+    const bool gated = which == FUSCO_PROBE_PRODUCT_GATED, activation = which == FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION;
+    if (!layout_ok(L) || which < 0 || which > FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION || !row_ok(outputs) || !row_ok(sum)) return FUSCO_ERR_INVALID_ARG;
+    if (((gated || activation) && !row_ok(2 * outputs)) || !weights_ok((gated ? 2 : 1) * (int64_t)outputs, sum)) return FUSCO_ERR_INVALID_ARG;
+    ProductArgs a = {};
+    a.E = L->E; a.NA = outputs; a.C = sum;
+    const std::integral_constant<int, kAlongC> along;
+    const std::integral_constant<int, kAcross> across;
+    if (gated) return f(along, std::integral_constant<int, kStoreGated>(), a);
+    if (which == FUSCO_PROBE_PRODUCT_LINEAR) return f(along, std::integral_constant<int, kStoreBf16>(), a);
+    if (activation) return f(across, std::integral_constant<int, kStoreGatedGrad>(), a);
+    return f(across, std::integral_constant<int, kStoreBf16>(), a);
+}
+
 }   // namespace
 
 extern "C" {
@@ -371,14 +389,12 @@ int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const voi
 
 int fusco_probe_experts_tile_rows(const fusco_layout *L, int which, int32_t outputs, int32_t sum)
 {
-    const bool gated = which == FUSCO_PROBE_PRODUCT_GATED, activation = which == FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION;
-    if (!layout_ok(L) || which < 0 || which > FUSCO_PROBE_PRODUCT_INPUT_GRAD_ACTIVATION || !row_ok(outputs) || !row_ok(sum)) return FUSCO_ERR_INVALID_ARG;
-    if (((gated || activation) && !row_ok(2 * outputs)) || !weights_ok((gated ? 2 : 1) * (int64_t)outputs, sum)) return FUSCO_ERR_INVALID_ARG;
-    ProductArgs a = {};
-    a.E = L->E; a.NA = outputs; a.C = sum;
-    if (gated) return rows_per_tile<kAlongC, kStoreGated>(L, a);
-    if (which == FUSCO_PROBE_PRODUCT_LINEAR) return rows_per_tile<kAlongC, kStoreBf16>(L, a);
-    return activation ? rows_per_tile<kAcross, kStoreGatedGrad>(L, a) : rows_per_tile<kAcross, kStoreBf16>(L, a);
+    return of_product(L, which, outputs, sum, [&](auto amode, auto stored, const ProductArgs &a) { return rows_per_tile<decltype(amode)::value, decltype(stored)::value>(L, a); });
+}
+
+int fusco_probe_experts_tile_outputs(const fusco_layout *L, int which, int32_t outputs, int32_t sum)
+{
+    return of_product(L, which, outputs, sum, [&](auto amode, auto stored, const ProductArgs &a) { return outputs_per_tile<decltype(amode)::value, decltype(stored)::value>(L, a); });
 }
 
 }   // extern "C"

@@ -84,10 +84,16 @@ int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
 }
 
 // Input gradients: tiles of 64 rows and 128 outputs, where a compute unit has one of them at the most.  Their stages take 64 elements of the sum, three of them under way, where a stage of 256
-// outputs has room for 32, and a single tile waits for its loads; sums keep their order.  Through the activation / without it, us, 256 outputs / 128: 8 experts, 2048 x 768, 32 rows each, 48
-// tiles 30 / 22 and 25 / 19; 16 of 1040 x 528, 38 rows, 80 tiles 21 / 16 and 16.6 / 13.5; 8 of 4096 x 1280, 64 rows, 130 tiles 67 / 46 and 60 / 43; 64 of 1024 x 512, 32 rows, 256 tiles
-// 29 / 19 and 24.6 / 16.5; more tiles than compute units, 64 of 2048 x 768, 384, 49 / 53.
-inline bool narrow(const fusco_layout *L, const ProductArgs &a) { return tiles_of_rows(L, 64) * ((a.NA + 127) / 128) <= kCus; }
+// outputs has room for 32, and a single tile waits for its loads; sums keep their order.  Tiles are counted as the mean number of rows has them, where all experts may have one row too many
+// for their last but one, and as above.  Through the activation / without it, us, 256 outputs / 128: 8 experts, 2048 x 768, 32 rows each, 48 tiles 29 / 21 and 24 / 19; 16 of 1040 x 528, 38 rows,
+// 80 tiles 20 / 15 and 15.6 / 12.6; 8 of 4096 x 1280, 64 rows, 80 tiles 71 / 46 and 65 / 43; 64 of 1024 x 512, 32 rows, 256 tiles 28 / 20 and 24 / 17; 64 of 1024 x 256, 66 rows, 256 tiles
+// 22 / 15 and 17 / 12.  More tiles than compute units: 88 of 336 x 256, 66 rows, 352 tiles 15.8 / 17.9 and 9.5 / 13.4; 40 of 1024 x 512, 66 rows, 320 tiles 22 / 23 and 15.8 / 18.3.  Segments so uneven
+// that the count is too low lose less than one so counted gains: 120 of 1024 x 256, 66 and 14 rows in turn, 360 tiles counted as 246, 25 / 25 and 19.7 / 20.9.
+inline bool narrow(const fusco_layout *L, const ProductArgs &a)
+{
+    const int64_t even = L->E * (((int64_t)L->P + 64 * (int64_t)L->E - 1) / (64 * (int64_t)L->E));
+    return fmax((double)even, tiles_of_rows(L, 64)) * ((a.NA + 127) / 128) <= kCus;
+}
 
 // E4m3 in tiles of 64 rows: three stages in LDS instead of two, where filling up the last turn costs hardly a stage.  Gated / linear, us, two / three: 60 experts of 2880 x (2 x 1040) with 12 rows 112
 // / 93 and 55 / 47; 256 of 7168 x (2 x 1024) with 9 664 / 614 and 361 / 358; 128 of 4096 x (2 x 1280) with 8 228 / 225; 64 of 2048 x 1408 with 20 linear 44.4 / 42.2; where a turn is filled up, sums of
@@ -96,6 +102,14 @@ inline bool three(const ProductArgs &a)
 {
     const int stages = (a.C + 63) / 64;   // of 128 elements of one byte
     return 100 * ((stages + 2) / 3 * 3) <= 107 * ((stages + 1) / 2 * 2);
+}
+
+// Outputs of a tile (gated: units)
+template <int AMODE, int STORE>
+int outputs_per_tile(const fusco_layout *L, const ProductArgs &a)
+{
+    const int rows = rows_per_tile<AMODE, STORE>(L, a), whole = rows == 16 ? 16 * kFewF : AMODE == kAcross && rows == 64 && narrow(L, a) ? 128 : kTileA;
+    return STORE == kStoreGated ? whole / 2 : whole;
 }
 
 template <int AMODE, int STORE, bool EIGHT = false>

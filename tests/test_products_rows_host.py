@@ -56,3 +56,35 @@ def test_rounds_of_tiles(rows):
 def test_bad_sizes(rows):
     for which, outputs, total in ((-1, 64, 64), (4, 64, 64), (GATED, 0, 64), (GATED, 64, 12), (GATED, 1 << 19, 8), (ACTIVATION, 1 << 19, 8), (LINEAR, (1 << 19) + 8, 8), (LINEAR, 1 << 16, 1 << 15)):
         assert rows(16, 2, 8, which, outputs, total) == -1, (which, outputs, total)
+
+
+@pytest.fixture(scope="module")
+def outputs_of(rows):
+    from paper_2512_22036_amd import binding
+    lib = binding.load_library()
+
+    def ask(N, k, E, which, outputs, total):
+        L = binding._CLayout()
+        assert lib.fusco_layout_bind(ctypes.byref(L), N, k, E, 1, 0x10000000, lib.fusco_layout_bytes(N, k, E, 1)) == 0
+        return lib.fusco_probe_experts_tile_outputs(ctypes.byref(L), which, outputs, total)
+
+    return ask
+
+
+def test_outputs_of_a_tile(rows, outputs_of):
+    assert [outputs_of(1, 8, 128, which, 1280, 4096) for which in (GATED, LINEAR)] == [16, 32]
+    assert [outputs_of(4096, 8, 128, which, 1280, 4096) for which in (GATED, LINEAR, INPUT_GRAD, ACTIVATION)] == [128, 256, 256, 256]
+    for which, outputs, total in ((-1, 64, 64), (4, 64, 64), (GATED, 0, 64), (GATED, 1 << 19, 8), (ACTIVATION, 1 << 19, 8)):
+        assert outputs_of(16, 2, 8, which, outputs, total) == -1, (which, outputs, total)
+
+
+def test_gradients_of_few_tiles(rows, outputs_of):
+    """Tiles of 64 rows and 128 outputs where each compute unit has one of them at the most: N, E and outputs with k = 1, and the tiles if all experts have as many rows."""
+    for which in (INPUT_GRAD, ACTIVATION):
+        for N, E, outputs, tiles in ((256, 8, 768, 48), (608, 16, 528, 80), (512, 8, 1280, 80), (2048, 64, 512, 256), (64 * 66, 64, 256, 256), (20 * 66, 20, 528, 200)):
+            assert rows(N, 1, E, which, outputs, 1024) == 64 and outputs_of(N, 1, E, which, outputs, 1024) == 128, (N, E, outputs)
+            assert E * -(-N // (64 * E)) * -(-outputs // 128) == tiles <= 256
+        # an expert's last two or three rows make a tile of their own
+        for N, E, outputs, tiles in ((88 * 66, 88, 256, 352), (40 * 66, 40, 512, 320), (65 * 66, 65, 256, 260), (33 * 130, 33, 384, 297)):
+            assert rows(N, 1, E, which, outputs, 1024) == 64 and outputs_of(N, 1, E, which, outputs, 1024) == 256, (N, E, outputs)
+            assert E * -(-N // (64 * E)) * -(-outputs // 128) == tiles > 256
