@@ -118,7 +118,12 @@ def from_eight(q, scale):
 
 class EightBlock(MoEBlock):
     """The block with weights of e4m3, rows sent and multiplied in e4m3, and in e4m3 what backward needs of them.  Gradients are those of the
-    products as they were computed: roundings to e4m3 count as constants (w_in and w_out are here the rounded weights)."""
+    products as they were computed: roundings to e4m3 count as constants (w_in and w_out are here the rounded weights).
+
+    FEW: tokens up to which the layer for a few tokens is taken, which needs no rows in e4m3 but passes over an expert's weights again for every few of its tokens.  Experts alone,
+    that way / scaling, plan, dispatch, products and combine, us: 128 experts of 4096 x 1280, 8 per token: 1 token 36 / 55, 8 159 / 162, 16 264 / 258, 64 479 / 382; 32 such
+    experts, 8 tokens 99 / 98, 64 285 / 138; 64 of 2048 x 1408, 6 per token, 8 tokens 67 / 70, 64 181 / 126; 64 of 7168 x 2048, 8 per token, 1 token 80 / 85, 8 347 / 314."""
+    FEW = 8
 
     def __init__(self, *sizes, **named):
         super().__init__(*sizes, **named)
@@ -130,10 +135,9 @@ class EightBlock(MoEBlock):
     def forward(self, r, y, keep=False):
         N = r.shape[0]
         s, x, logits, idx, w = self.before_experts(r, y)
+        if N <= self.FEW and not keep:
+            return s, self.few(x, idx, w)
         out = _empty(N, self.H)
-        if N <= 64 and not keep:
-            fusco.fusco_moe_few(x, idx, w, self.in8[0], self.out8[0], out, w_in_scale=self.in8[1], w_out_scale=self.out8[1])
-            return s, out
         x8, x_scale = to_eight(x)
         L = fusco.Layout(N, self.k, self.E, self.D)
         rows, rows_scale = _empty(L.P, self.H, like=x8), _empty(L.P, x_scale.shape[1], like=x_scale)
@@ -146,6 +150,11 @@ class EightBlock(MoEBlock):
         fusco.fusco_experts_linear_fp8(L, *h, *self.out8, out_rows)
         fusco.fusco_combine(L, out_rows, w, out)
         return (s, out, (r, y, s, x, logits, idx, w, L, (rows, rows_scale), to_eight(pre), h, out_rows)) if keep else (s, out)
+
+    def few(self, x, idx, w):
+        out = _empty(*x.shape)
+        fusco.fusco_moe_few(x, idx, w, self.in8[0], self.out8[0], out, w_in_scale=self.in8[1], w_out_scale=self.out8[1])
+        return out
 
     def through_experts(self, L, d_rows, rows, pre, h):
         dpre, dw_out = _empty(L.P, 2 * self.I), torch.empty_like(self.w_out)
@@ -226,8 +235,8 @@ def check_eight(N=96, H=256, I=128, E=16, k=4, D=4, keep_groups=2):
     score = torch.sigmoid(x @ p["router"].t()).gather(1, kept[5].long())
     want.update(zip(p, torch.autograd.grad([want_s, x, score / score.sum(dim=1, keepdim=True)], list(p.values()), [ds.double(), dx, dw])))
     want.update(s=want_s.detach(), out=results["out"])
-    if N <= 64:   # decode: rows and activations as they are
-        got["few"] = block.forward(r, y)[1]
+    if N <= 64:   # the layer for a few tokens: rows and activations as they are
+        got["few"] = block.few(kept[3], kept[5], kept[6])
         rows = torch.zeros_like(want["out"])
         for e in range(E):
             t, j = (kept[5] == e).nonzero(as_tuple=True)

@@ -63,3 +63,16 @@ def test_captured(example, N, train):
         want = step()
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,few", [(1, True), (8, True), (9, False), (64, False)])
+def test_way_of_a_forward_pass(example, monkeypatch, N, few):
+    """Where the products on e4m3 rows are faster than the layer for a few tokens, they are taken."""
+    block = example.EightBlock(256, 128, 16, 4, 4, 2)
+    calls = []
+    whole = example.fusco.fusco_moe_few
+    monkeypatch.setattr(example.fusco, "fusco_moe_few", lambda *a, **kw: (calls.append(1), whole(*a, **kw)))
+    r, y = torch.randn((N, 256), device="cuda"), torch.randn((N, 256), device="cuda").bfloat16()
+    block.forward(r, y)
+    block.forward(r, y, keep=True)
+    assert len(calls) == (1 if few else 0)
