@@ -265,3 +265,11 @@ def test_infinite_scales(N, E, k, H, I):
     f.fusco_moe_few(ones(N, H).bfloat16(), chosen, w, ones(E, 2 * I, H).to(FP8), ones(E, H, I).to(FP8), out, w_in_scale=w_in_scale, w_out_scale=ones(E, blocks(H), blocks(I)))
     sick = (chosen == 1).any(dim=1)
     assert bool((out[sick] == float("inf")).all()) and bool(out[~sick].isfinite().all())
+
+
+@pytest.mark.parametrize("eights", [False, True])
+@pytest.mark.parametrize("kind", ["any", "one", "invalid"])
+@pytest.mark.parametrize("N,E,k,H,I", [(1, 16, 8, 4096, 144), (5, 12, 4, 4112, 80), (20, 24, 4, 7168, 48), (64, 8, 2, 4096, 272), (47, 64, 8, 5120, 48)])
+def test_long_rows(N, E, k, H, I, kind, eights):
+    """As many blocks of outputs as there are compute units and more: the list of groups is whole, a workgroup's waves alone share it."""
+    test_layer(N, E, k, H, I, kind, eights, torch.float32)
