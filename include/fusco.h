@@ -458,7 +458,7 @@ int fusco_experts_linear(const fusco_layout *L, const void *d_x, const void *d_w
  * 128 columns of a matrix (weights); the last ones of a row or matrix end with it.  d_x [rows, columns] of dtype, d_q [rows, columns] e4m3, both
  * contiguous; d_scale fp32: [rows, scale_stride] for rows (columns behind the last block's are left as they are: dispatch moves
  * them as its second plane, whose rows are multiples of 16 bytes), [rows / matrix_rows, ceil(matrix_rows / 128), ceil(columns / 128)]
- * for matrices.  fusco_from_fp8 writes x = q * s for any scales, rounded once; with the powers of two above bf16 holds it exactly.
+ * for matrices.  fusco_from_fp8 writes x = q * s for any scales, rounded once; with the powers of two above, from 2^-124 on, bf16 holds it exactly.
  * columns: a multiple of 16, at most FUSCO_MAX_ROW_BYTES; less than 2^31 rows, at most 2^29 - 32 blocks of 128 columns of
  * rows (of matrices too), and less than 2^23 blocks of matrices.
  */
@@ -474,10 +474,14 @@ int fusco_to_fp8(const fusco_fp8 *f, const void *d_x, void *d_q, float *d_scale,
 int fusco_from_fp8(const fusco_fp8 *f, const void *d_q, const float *d_scale, void *d_x, void *stream);
 
 /*
- * fusco_experts_gated and fusco_experts_linear on rows and weights of e4m3 with scales per block, which may be any fp32 numbers:
- *     sum over blocks b of 128 columns of   x_scale[r, b] * w_scale[e, m / 128, b] * sum over c in b of x[r, c] w[e, m, c]
+ * fusco_experts_gated and fusco_experts_linear on rows and weights of e4m3 with scales per block, which may be any fp32 numbers whose products are
+ * ordinary ones (zero, or from 2^-126 to the largest):
+ *     sum over blocks b of 128 columns of   (x_scale[r, b] * w_scale[e, m / 128, b]) * sum over c in b of x[r, c] w[e, m, c]
+ * The product of the two scales is rounded to fp32 first: below 2^-126 it has fewer digits, and where it is infinite so is the result, or NaN for a sum of zero.
  * Sums and scales are fp32 and results are rounded once to bf16; the matrix instructions for e4m3 cut each product, before eight neighbours are added, to
- * a multiple of 2^-13 of the largest one's power of two (2^-16 of a result on the average, where its rounding to bf16 is 2^-9.7).  d_x [P, H] or [P, C] and d_x_scale [P, x_scale_stride] as
+ * a multiple of 2^-13 of the largest one's power of two (2^-16 of a result on the average, where its rounding to bf16 is 2^-9.7).  A result
+ * that this carries over a border of e4m3 moves by a whole step when it is brought to e4m3 in turn: both products with fusco_to_fp8 between them
+ * are 2.0e-3 to 2.1e-3 off in the norm, where exact products are 1.7e-3.  d_x [P, H] or [P, C] and d_x_scale [P, x_scale_stride] as
  * fusco_dispatch moves the two planes of such rows; weights [E, 2 I, H] or [E, M, C]; d_w_scale [E, 2 ceil(I / 128), ceil(H / 128)] (gate rows
  * and up rows begin blocks of their own: the weights are 2 E matrices of I rows) or [E, ceil(M / 128), ceil(C / 128)].  d_h, d_pre
  * and d_y are bf16 as there.  H (gated) and C (linear): multiples of 16.  I and M: multiples of 8.
@@ -511,7 +515,7 @@ int fusco_experts_weight_grad(const fusco_layout *L, const void *d_dy, const voi
  * whole row of 2 C columns), used as fp32.  C: a multiple of 16.
  *
  * fusco_experts_weight_grad_fp8: fusco_experts_weight_grad with d_x [P, C] of e4m3, d_x_scale [P, x_scale_stride].  x * scale is rounded to bf16 before
- * the product, which changes nothing for scales that are powers of two.  C: a multiple of 16.
+ * the product, which changes nothing for scales that are powers of two, from 2^-124 on.  C: a multiple of 16.
  */
 int fusco_experts_input_grad_fp8(const fusco_layout *L, const void *d_dy, const void *d_w, void *d_dpre, const void *d_pre, const float *d_pre_scale,
                                  int32_t pre_scale_stride, int32_t M, int32_t C, void *stream);
@@ -521,14 +525,15 @@ int fusco_experts_weight_grad_fp8(const fusco_layout *L, const void *d_dy, const
 /*
  * The experts of an MoE layer for a few tokens (one to FUSCO_MAX_FEW_TOKENS), from their rows and routing to the weighted sum, without a layout:
  *     out[t, :] = sum_j w[t, j] * W_out[e] (silu(g) * u),   g and u = gate and up rows of W_in[e] times x[t, :],   e = topk_idx[t, j]
- * as fusco_plan_dispatch, fusco_experts_gated, fusco_experts_linear and fusco_combine compute it, in two launches that read the weights of the chosen
- * experts once.  Sums and silu(g) * u are fp32, the result is rounded once.  Pairs whose expert is not in [0, E) count
+ * as fusco_plan_dispatch, fusco_experts_gated, fusco_experts_linear and fusco_combine compute it, in two launches.  The first passes over w_in of a chosen expert once
+ * for every 16 of its pairs (32 if N k >= 8 E), the second over w_out once for every 5 (15 if N k >= 3 E): up to some 8 tokens that is the faster way, from
+ * 16 on the calls one by one are in most sizes.  Sums and silu(g) * u are fp32, the result is rounded once.  Pairs whose expert is not in [0, E) count
  * nothing; a token's equal experts count together.  An expert's weights reach only the tokens that chose it.
  * d_x [N, H] bf16, d_topk_idx and d_w [N, k], d_out [N, H] of out_dtype (FUSCO_BF16 or FUSCO_F32).  weight_dtype FUSCO_BF16: d_w_in [E, 2 I, H] and
  * d_w_out [E, H, I] as for fusco_experts_gated and fusco_experts_linear, H and I multiples of 8, scales NULL.  FUSCO_E4M3: weights and scales as for
  * fusco_experts_gated_fp8 and fusco_experts_linear_fp8, H and I multiples of 16.  An expert's w_in has less than 2^31 - 2^24 bytes, and
- * min(N k, E) I / 8 is less than 2^24 - 1.  Infinite weights of w_out give infinities or NaN.  d_scratch: fusco_moe_few_scratch_bytes() bytes, contents
- * irrelevant before and after.
+ * min(N k, E) I / 8 is less than 2^24 - 1, and 6 N k I bytes are below 2032 MiB.  Infinite weights of w_out give infinities or NaN.
+ * d_scratch: fusco_moe_few_scratch_bytes() bytes, contents irrelevant before and after; calls that may run at the same time have scratch of their own.
  */
 #define FUSCO_E4M3 2
 #define FUSCO_MAX_FEW_TOKENS 64

@@ -764,7 +764,8 @@ def _fp8_weights(layout: Layout, w: torch.Tensor, w_scale: torch.Tensor, matrice
 def fusco_experts_gated_fp8(layout: Layout, x: torch.Tensor, x_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
                             h: torch.Tensor, pre: Optional[torch.Tensor] = None, stream=None) -> None:
     """fusco_experts_gated on float8_e4m3fn: x [P, H] with x_scale float32 [P, S] as fusco_dispatch moves both, w [E, 2 I, H] with
-    w_scale [E, 2 ceil(I / 128), ceil(H / 128)] (gate and up rows are matrices of their own); h [P, I] and pre [P, 2 I] bfloat16."""
+    w_scale [E, 2 ceil(I / 128), ceil(H / 128)] (gate and up rows are matrices of their own); h [P, I] and pre [P, 2 I] bfloat16.
+    Scales: any numbers whose products x_scale * w_scale float32 holds."""
     if w.dim() == 3 and w.shape[1] % 2:
         raise FuscoError("w must have an even number of rows per expert")
     _fp8_weights(layout, w, w_scale, 2)
@@ -801,7 +802,8 @@ def fusco_moe_few(x: torch.Tensor, topk_idx: torch.Tensor, w: torch.Tensor, w_in
     """The experts of a layer for a few tokens, N of 1 to 64: x [N, H] bfloat16, topk_idx [N, k] int32, w [N, k] float32 as
     fusco_route writes them, out [N, H] bfloat16 or float32.  Weights w_in [E, 2 I, H] and w_out [E, H, I] are bfloat16, or
     float8_e4m3fn with the scales that fusco_experts_gated_fp8 and fusco_experts_linear_fp8 take.  scratch:
-    fusco_moe_few_scratch_bytes(N, k, I) bytes, made here on the call's stream if not given."""
+    fusco_moe_few_scratch_bytes(N, k, I) bytes, made here on the call's stream if not given.  Up to some 8 tokens this is faster than
+    the calls one by one, from 16 on they are in most sizes."""
     if stream is None and scratch is not None and _fast is not None:
         rc = _fast.moe_few(x, topk_idx, w, w_in, w_out, out, w_in_scale, w_out_scale, scratch)
         if rc is not None:

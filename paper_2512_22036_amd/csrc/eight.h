@@ -2,8 +2,8 @@
 //
 //     s = 2^n, n the smallest whole number with max |x| <= 448 * 2^n over the block        q = x / s rounded to e4m3 (nearest even)
 //
-// Powers of two, so that x / s is exact and q * s is a number of bf16 (four significant bits): the only rounding is that to e4m3, and another scale between s / 2
-// and s would keep no more bits of any value that is not among the block's smallest.  A block is 128 columns of a row, or 128 x 128 of a matrix.
+// Powers of two, so that x / s is exact and q * s is a number of bf16 (four significant bits; from s = 2^-124 on, below which it may be smaller than the smallest of them): the only rounding is
+// that to e4m3, and another scale between s / 2 and s would keep no more bits of any value that is not among the block's smallest.  A block is 128 columns of a row, or 128 x 128 of a matrix.
 // Infinities and NaN become NaN and take no part in the maximum; a block of zeros has scale 1.  Scales are at least 2^-126.
 //
 // Bound by memory: x read once, q and scales written once, or the other way round; of a few rows by the launch (128 rows of 4096 4 us).

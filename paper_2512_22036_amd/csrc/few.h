@@ -1,7 +1,9 @@
 // The whole layer for a few tokens: out[t] = sum over j of w[t, j] * W_out[e] (silu(g) * u), g and u = W_in[e] x[t], e = topk_idx[t, j].
 //
-// Bound by the weights of the chosen experts, every one of which is read once: few_gated_kernel reads those of the gated product, finds an expert's tokens in the
-// routing itself and leaves h in scratch memory; few_linear_kernel reads those of the down product and adds up a token's experts in registers.
+// Bound by the weights of the chosen experts where those have few tokens: few_gated_kernel reads those of the gated product, finds an expert's tokens in the
+// routing itself and leaves h in scratch memory; few_linear_kernel reads those of the down product and adds up a token's experts in registers.  Both pass over an expert's weights once for as
+// many of its pairs as a matrix instruction has columns for, 16 or 32 and 5 or 15, from the caches if they still hold them, and few_linear_kernel reads all of h for every 16 outputs: with
+// more pairs than that it is these passes that bound (e4m3, 4096 x 1280, 64 tokens: 8 experts, two per token, 71 us, eight per token 210, where the weights take 20; 128 experts 516, weights 312).
 // Nothing is moved in between; the pairs are sorted by expert beside the first product.  h is kept as three numbers of bf16, its rounding and those of what is left, which hold an fp32 number: nothing is rounded to fewer
 // bits but a result of bf16.  (Two of them, 17 bits, were 2.5e-6 off in the norm where fp32 throughout is 8e-7.)
 //

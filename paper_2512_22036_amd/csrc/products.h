@@ -41,8 +41,8 @@ struct ProductArgs {
     int32_t row_scales, scale_rows, scales;
 };
 
-// 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal: off by some (|g| + 4) * 2^-23 of itself, below 2^-16 where it is not 0 (g > -87), and what comes
-// of it is rounded to bf16, 2^-8
+// 1 / (1 + exp(-g)) from the hardware's exponential and reciprocal: off by some (|g| + 4) * 2^-23 of itself, below 2^-16 where it is not 0 (g > -87).  What comes of it is rounded to bf16,
+// 2^-8, but for the layer for a few tokens, whose h and results of fp32 are off by as much.
 __device__ __forceinline__ float sigmoid(float g) { return __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 __device__ __forceinline__ float silu(float g) { return g * sigmoid(g); }
 
@@ -387,7 +387,8 @@ __device__ __forceinline__ void tile_stage(const S &t, char *cur, const char *nx
 }
 
 // Stages of e4m3 operands: a matrix instruction takes a whole stage of 16 x 16 outputs, and its result, scaled, is added to the pair's sums two instructions
-// later.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
+// later.  The instruction cuts each of eight neighbouring products, towards zero, to a multiple of 2^-13 of the power of two that the largest begins with, before it adds them: what e4m3 at twice
+// the rate of bf16 costs, 2^-16 of a result on the average.  (Instructions of 32 x 32, two of them per stage and pair, hold four times the registers between the product and the sum, which then leave none to read
 // fragments ahead.)  In the middle of a stage all waves hold their fragments of b, and b's slot is asked for again: its loads then have one and a half stages, those of a one (131072
 // rows, linear 898 -> 799 us, gated 1408 -> 1390, 785 and 1357 with their places worked out once a stage, 779 and 1347 once a launch; with half of a's loads beside them, in slots
 // apart, 810 and 1450).
@@ -632,9 +633,9 @@ __device__ __forceinline__ int tile_in_list(int i)
 // with 32 rows, 4096 x (2 x 1280): 470 us, 5.7 TB/s).  Tiles of 256 x 256 read an operand half as often as those of 128; the list and the loads
 // of the next tile under the last turn of one leave no gap between tiles (gated 2447 us with one, 2361 without).
 //
-// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), 1347 us, 2.04 PFLOP/s; linear, 1280 x 4096, 779 us, 1.76.  Matrix instructions run 54 and 44 % of the cycles, at 1.9 of 2.4 GHz,
-// the vector ones that scale their results beside them 48 and 41 %; the rest is waiting: without its loads the gated product took two thirds of its time, without the tiles'
-// stores the linear one four fifths.
+// E4m3 (128 experts, 131072 rows): gated, 4096 x (2 x 1280), called again and again 1345 us, 2.04 PFLOP/s, in turn with the calls around it 1372 on average; linear, 1280 x 4096, 779 us, 1.76, in turn
+// 825.  Matrix instructions run 53 and 44 % of the cycles, at 1.9 of 2.4 GHz, the vector ones that scale their results beside them 47 and 42 %; the rest is waiting: without its loads the gated product
+// took two thirds of its time, without the tiles' stores the linear one four fifths.
 template <int AMODE, int BMODE, int BB, int FA, int FB, int STORE, bool EIGHT = false, bool KEPT = false, int AA = kTileA, bool THREE = false>
 __global__ __launch_bounds__(kTileThreads, 2) void product_kernel(ProductArgs p)
 {
@@ -1248,6 +1249,8 @@ __global__ __launch_bounds__(WAVES *kWave) void few_rows_kernel(ProductArgs p)
 #pragma unroll
             for (int f = 0; f < F; ++f) {
                 const f32x4 zero = {};
+                // cuts products as in tiles.  Exact ones, both operands widened to bf16, us: 4096 x (2 x 1280), 128 experts, 4 / 16 / 32 tokens 58 / 62, 154 / 159, 200 / 205; 1280 x 4096 30.5 /
+                // 30.9, 86 / 85, 113 / 111; 512 x 1024 6.2 / 6.5, 12.3 / 13.0, 15.9 / 16.6
                 const f32x4 part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(joined(wn[f]), joined(xn), zero, 0, 0, 0, 0, 0, 0);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) acc[f][q] = fmaf(scale[kGated && f >= kOut], part[q], acc[f][q]);

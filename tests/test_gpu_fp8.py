@@ -342,3 +342,20 @@ def test_refusals():
             f.fusco_to_fp8(*bad)
     with pytest.raises(f.FuscoError):
         f.fusco_from_fp8(q, s, b.half())
+
+
+@pytest.mark.parametrize("rows,weights", [(2.0 ** 90, 2.0 ** -85), (2.0 ** -120, 2.0 ** 118), (2.0 ** 60, 2.0 ** 50), (2.0 ** -30, 2.0 ** -40)])
+@pytest.mark.parametrize("N", [6, 24, 300, 900])   # tiles of every height
+def test_scales_far_apart(N, rows, weights):
+    """Scales of any size whose product, which is rounded first, is an ordinary number."""
+    f = fusco()
+    L, gen, bounds = make(N, 2, 4, 17, "normal")
+    C, M = 400, 136
+    x, xs = eight(gen, L.P, C, scales=(L.P, blocks(C)), std=1.0, whole=True)
+    w, ws = eight(gen, 4, M, C, scales=(4, blocks(M), blocks(C)), std=1.0, whole=True)
+    xs, ws = xs * rows, ws * weights
+    y = torch.empty((L.P, M), dtype=torch.bfloat16, device="cuda")
+    f.fusco_experts_linear_fp8(L, x, xs, w, ws, y)
+    for e, r in segments(bounds, x):
+        want, err = product8(x[r], xs[r], w[e], by_row(ws[e], M), True)
+        within(y[r], want, err + BF16 * (want.abs() + err))
