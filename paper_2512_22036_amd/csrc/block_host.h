@@ -84,8 +84,8 @@ int rows_per_tile(const fusco_layout *L, const ProductArgs &a)
 }
 
 // Input gradients: tiles of 64 rows and 128 outputs, where a compute unit has one of them at the most.  Their stages take 64 elements of the sum, three of them under way, where a stage of 256
-// outputs has room for 32, and a single tile waits for its loads; sums keep their order.  Tiles are counted as the mean number of rows has them, where all experts may have one row too many
-// for their last but one, and as above.  Through the activation / without it, us, 256 outputs / 128: 8 experts, 2048 x 768, 32 rows each, 48 tiles 29 / 21 and 24 / 19; 16 of 1040 x 528, 38 rows,
+// outputs has room for 32, and a single tile waits for its loads; sums keep their order.  Tiles are counted in two ways, by the mean as above and as if all experts had equally many rows (a few more
+// than 64 make two tiles of each), and the larger count decides.  Through the activation / without it, us, 256 outputs / 128: 8 experts, 2048 x 768, 32 rows each, 48 tiles 29 / 21 and 24 / 19; 16 of 1040 x 528, 38 rows,
 // 80 tiles 20 / 15 and 15.6 / 12.6; 8 of 4096 x 1280, 64 rows, 80 tiles 71 / 46 and 65 / 43; 64 of 1024 x 512, 32 rows, 256 tiles 28 / 20 and 24 / 17; 64 of 1024 x 256, 66 rows, 256 tiles
 // 22 / 15 and 17 / 12.  More tiles than compute units: 88 of 336 x 256, 66 rows, 352 tiles 15.8 / 17.9 and 9.5 / 13.4; 40 of 1024 x 512, 66 rows, 320 tiles 22 / 23 and 15.8 / 18.3.  Segments so uneven
 // that the count is too low lose less than one so counted gains: 120 of 1024 x 256, 66 and 14 rows in turn, 360 tiles counted as 246, 25 / 25 and 19.7 / 20.9.
